@@ -43,6 +43,7 @@ typedef enum cvlc_status {
 #define CVLC_DEV_STREAM 2u    /* malformed stream: header, code length, PID >= d, order */
 #define CVLC_DEV_INTERNAL 4u  /* an internal consistency check failed                   */
 #define CVLC_DEV_WORKSPACE 8u /* encode: a vector needs more candidate room than given  */
+#define CVLC_DEV_INDEX 16u    /* a token or a teacher's entry names a row beyond the vocabulary */
 
 #define CVLC_MAX_CODED 31u    /* at most 31 coded groups plus the implicit 0-bit tail   */
 #define CVLC_STATS_STRIDE 32u /* stats entries per client: groups 1..R, then the tail   */
@@ -317,6 +318,129 @@ int cvlc_depacketize(const void* d_packets, uint32_t n_packets, uint32_t mtu_byt
 /* Waits for hip_stream and copies the workspace's device status word to
  * *status_out (0 = clean, else CVLC_DEV_* bits). */
 int cvlc_device_status(const void* d_workspace, void* hip_stream, uint32_t* status_out);
+
+/* ---- the local step of a language-model client ------------------------------
+ * What such a client computes lands in the update vector that cvlc_encode reads:
+ * the gradients of the embedding table and of the norms' weights are fp32 and go
+ * straight to their slices of it.  The loss is distillation from a teacher's top
+ * logits, what clients and server send each other instead of whole logits.
+ *
+ * Matrices are rows of elements of one type, `stride` elements from one row to
+ * the next (at least the row's length); they need no more alignment than their
+ * elements.  Everything is computed in 32 bits and rounded to the output's type
+ * once, to nearest.  Sums have a fixed order: the same call on the same device
+ * gives the same bits.  n = 0 is allowed everywhere (its matrices may be NULL).
+ * Buffers that a call writes must not overlap others of the call, except where
+ * it says so. */
+#define CVLC_F32 0u
+#define CVLC_BF16 1u
+#define CVLC_F16 2u
+
+/* GPU.  Embedding lookup: out[i,:] = scale * table[id_i,:].
+ *   d_ids      n tokens of id_bytes = 4 or 8 bytes, signed.  A negative one is
+ *              padding: its row is zeros.  One at or beyond `vocab` sets
+ *              CVLC_DEV_INDEX; its row is zeros too.
+ *   d_table    vocab rows of dim elements
+ *   d_out      n rows of dim elements, of the table's type or, where that is
+ *              fp32, of any
+ *   d_status   device or NULL: status bits are OR-ed into this word, which the
+ *              caller clears */
+int cvlc_embed(uint32_t n, const void* d_ids, uint32_t id_bytes, const void* d_table, uint32_t table_type,
+               uint64_t table_stride, uint32_t vocab, uint32_t dim, float scale, void* d_out,
+               uint32_t out_type, uint64_t out_stride, uint32_t* d_status, void* hip_stream);
+
+/* GPU.  Its gradient: dtable[v,:] = scale * sum of dout[i,:] over the i with
+ * id_i = v, taken in ascending order of i (in pieces that are added up in order).
+ * Tokens are sorted first, so that a frequent token is no bottleneck.  Every row
+ * is written, untouched ones with zeros.
+ *   d_dout     n rows of dim elements of any type
+ *   d_dtable   vocab rows of dim fp32
+ *   flags      CVLC_GRAD_ACCUMULATE: add to d_dtable instead (its untouched rows
+ *              are not even read; the second use of a table whose transpose also
+ *              makes the logits)
+ *   d_workspace  device, 256-byte aligned, ws_bytes >=
+ *              cvlc_embed_grad_workspace_bytes(n, vocab, dim); its status word
+ *              tells of tokens beyond the vocabulary (CVLC_DEV_INDEX), which are
+ *              left out, as negative ones are */
+#define CVLC_GRAD_ACCUMULATE 1u
+size_t cvlc_embed_grad_workspace_bytes(uint32_t n, uint32_t vocab, uint32_t dim);
+int cvlc_embed_grad(uint32_t n, const void* d_ids, uint32_t id_bytes, const void* d_dout, uint32_t dout_type,
+                    uint64_t dout_stride, uint32_t vocab, uint32_t dim, float scale, float* d_dtable,
+                    uint64_t dtable_stride, uint32_t flags, void* d_workspace, size_t ws_bytes,
+                    void* hip_stream);
+
+/* GPU.  Layer norm of rows: y = (x - mean) * r * gamma + beta with
+ * r = 1 / sqrt(mean of (x - mean)^2 + eps).
+ *   d_x, d_y   n rows of dim elements; y has x's type or, where that is fp32, any.
+ *              d_y may be d_x (same type and stride).
+ *   d_gamma, d_beta   dim fp32 each, or NULL (1 and 0)
+ *   eps        >= 0 (a constant row with eps = 0 gives NaN)
+ *   d_stats    NULL, or n times {mean, r}, fp32, for the backward pass */
+int cvlc_layer_norm(uint32_t n, uint32_t dim, const void* d_x, uint32_t x_type, uint64_t x_stride,
+                    const float* d_gamma, const float* d_beta, float eps, void* d_y, uint32_t y_type,
+                    uint64_t y_stride, float* d_stats, void* hip_stream);
+
+/* GPU.  Its backward pass from the kept statistics, h = (x - mean) * r, g = dy * gamma:
+ *   dx = r * (g - mean of g - h * mean of (g * h)),
+ *   dgamma = sum of dy * h over the rows, dbeta = sum of dy.
+ *   d_dy       n rows, of x's type or, where that is fp32, of any
+ *   d_dx       n rows of x's type, or NULL; may be d_dy or d_x (same type and stride)
+ *   d_dgamma, d_dbeta   dim fp32 each, either may be NULL (not both together with d_dx)
+ *   flags      CVLC_GRAD_ACCUMULATE: add to d_dgamma and d_dbeta
+ *   d_workspace  device, 256-byte aligned, ws_bytes >=
+ *              cvlc_layer_norm_grad_workspace_bytes(n, dim); holds no status word */
+size_t cvlc_layer_norm_grad_workspace_bytes(uint32_t n, uint32_t dim);
+int cvlc_layer_norm_grad(uint32_t n, uint32_t dim, const void* d_dy, uint32_t dy_type, uint64_t dy_stride,
+                         const void* d_x, uint32_t x_type, uint64_t x_stride, const float* d_stats,
+                         const float* d_gamma, void* d_dx, uint64_t dx_stride, float* d_dgamma,
+                         float* d_dbeta, uint32_t flags, void* d_workspace, size_t ws_bytes,
+                         void* hip_stream);
+
+/* GPU.  Distillation from a teacher's top logits, loss and gradient in one pass
+ * over the student's logits.  Row i has the student's logits z (vocab of them)
+ * and the teacher's list of k pairs (id_j, t_j); with temperature T and weight w:
+ *   p_j = exp(t_j / T) / sum over the list (CVLC_DISTILL_LOGPROBS: exp(t_j)),
+ *   q = softmax(z / T) over the whole vocabulary, P = sum of the p_j,
+ *   loss_i = w T^2 sum_j p_j (ln p_j - ln q[id_j]),
+ *   dlogits[i,v] = w T (P q[v] - sum of the p_j with id_j = v), its derivative.
+ *   d_logits   n rows of vocab elements of any type.  -inf masks a logit (q = 0;
+ *              the loss is +inf where the teacher wants it); NaN or +inf makes
+ *              the row's results NaN.
+ *   d_ids, d_values   n rows of k entries, no gaps; ids of id_bytes = 4 or 8
+ *              bytes.  An entry with a negative id or the value -inf is not
+ *              there; one at or beyond vocab sets CVLC_DEV_INDEX and is not there
+ *              either.  An id may come more than once.
+ *   k          1 .. CVLC_DISTILL_MAX_K
+ *   flags      CVLC_DISTILL_LOGPROBS: the values are log-probabilities at this
+ *              temperature; the list is not normalised (P <= 1 is its share)
+ *   d_weights  n fp32 or NULL (all 1)
+ *   d_loss     NULL, or n fp32
+ *   d_stats    NULL, or n times {m, S}, fp32, for cvlc_distill_grad: the largest
+ *              logit and the sum of exp((z - m) / T)
+ *   d_dlogits  NULL, or n rows of vocab elements of the logits' type; may be
+ *              d_logits (same stride)
+ *   d_workspace  device, 256-byte aligned, ws_bytes >=
+ *              cvlc_distill_workspace_bytes(n, vocab); holds no status word
+ *   d_status   as for cvlc_embed
+ * A row with weight 0 or an empty list is not looked at: loss, statistics and
+ * gradient are zeros. */
+#define CVLC_DISTILL_MAX_K 1024u
+#define CVLC_DISTILL_LOGPROBS 1u
+size_t cvlc_distill_workspace_bytes(uint32_t n, uint32_t vocab);
+int cvlc_distill(uint32_t n, uint32_t vocab, const void* d_logits, uint32_t type, uint64_t stride, uint32_t k,
+                 const void* d_ids, uint32_t id_bytes, const void* d_values, uint32_t value_type,
+                 float temperature, uint32_t flags, const float* d_weights, float* d_loss, float* d_stats,
+                 void* d_dlogits, uint64_t dlogits_stride, void* d_workspace, size_t ws_bytes,
+                 uint32_t* d_status, void* hip_stream);
+
+/* GPU.  The gradient alone, from the statistics of an earlier cvlc_distill on the
+ * same logits, lists, temperature and flags; the weights may be others (a mean
+ * over a count known only then), but a row that had none has no statistics. */
+int cvlc_distill_grad(uint32_t n, uint32_t vocab, const void* d_logits, uint32_t type, uint64_t stride,
+                      uint32_t k, const void* d_ids, uint32_t id_bytes, const void* d_values,
+                      uint32_t value_type, float temperature, uint32_t flags, const float* d_weights,
+                      const float* d_stats, void* d_dlogits, uint64_t dlogits_stride, uint32_t* d_status,
+                      void* hip_stream);
 
 /* Profiling aid (not part of the hot path).  Between cvlc_profile_start and
  * cvlc_profile_stop every cvlc_encode_batch / cvlc_decode_aggregate / cvlc_fit_alpha call of this

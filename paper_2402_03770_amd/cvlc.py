@@ -12,12 +12,16 @@ import torch
 
 MAX_CODED = 31
 STATS_STRIDE = 32
-DEV_NONFINITE, DEV_STREAM, DEV_INTERNAL, DEV_WORKSPACE = 1, 2, 4, 8
+DEV_NONFINITE, DEV_STREAM, DEV_INTERNAL, DEV_WORKSPACE, DEV_INDEX = 1, 2, 4, 8, 16
+ERR_ARG = -1
 DECODE_ACCUMULATE = 1
 DECODE_QSGD = 2
 QUANT_PQ, QUANT_QSGD = 0, 1
 ENCODE_ERROR_STATS = 1
 FIT_RANKS_MAX = 32
+GRAD_ACCUMULATE = 1
+DISTILL_LOGPROBS = 1
+DISTILL_MAX_K = 1024
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libcvlc.so")
@@ -119,6 +123,21 @@ def lib() -> C.CDLL:
         L.cvlc_fit_workspace_bytes_for.argtypes = [C.c_uint32, C.c_uint32]
         L.cvlc_fit_workspace_bytes_for.restype = C.c_size_t
         L.cvlc_fit_alpha.argtypes = [C.c_uint32, C.POINTER(vp), C.c_uint32, vp, vp, vp, C.c_size_t, vp]
+        u32, u64, f32 = C.c_uint32, C.c_uint64, C.c_float
+        L.cvlc_embed.argtypes = [u32, vp, u32, vp, u32, u64, u32, u32, f32, vp, u32, u64, vp, vp]
+        L.cvlc_embed_grad_workspace_bytes.argtypes = [u32, u32, u32]
+        L.cvlc_embed_grad_workspace_bytes.restype = C.c_size_t
+        L.cvlc_embed_grad.argtypes = [u32, vp, u32, vp, u32, u64, u32, u32, f32, vp, u64, u32, vp, C.c_size_t, vp]
+        L.cvlc_layer_norm.argtypes = [u32, u32, vp, u32, u64, vp, vp, f32, vp, u32, u64, vp, vp]
+        L.cvlc_layer_norm_grad_workspace_bytes.argtypes = [u32, u32]
+        L.cvlc_layer_norm_grad_workspace_bytes.restype = C.c_size_t
+        L.cvlc_layer_norm_grad.argtypes = [u32, u32, vp, u32, u64, vp, u32, u64, vp, vp, vp, u64, vp, vp, u32, vp,
+                                           C.c_size_t, vp]
+        L.cvlc_distill_workspace_bytes.argtypes = [u32, u32]
+        L.cvlc_distill_workspace_bytes.restype = C.c_size_t
+        L.cvlc_distill.argtypes = [u32, u32, vp, u32, u64, u32, vp, u32, vp, u32, f32, u32, vp, vp, vp, vp, u64, vp,
+                                   C.c_size_t, vp, vp]
+        L.cvlc_distill_grad.argtypes = [u32, u32, vp, u32, u64, u32, vp, u32, vp, u32, f32, u32, vp, vp, vp, u64, vp, vp]
         L.cvlc_profile_start.argtypes = [C.c_uint32]
         L.cvlc_profile_stop.argtypes = [C.POINTER(C.c_float), u32p]
         L.cvlc_status_string.argtypes = [C.c_int]
@@ -339,6 +358,208 @@ def fit_alpha(updates: Sequence[torch.Tensor], alpha_out: torch.Tensor, workspac
     d = updates[0].numel() if n else 0
     _check(lib().cvlc_fit_alpha(n, upd, d, alpha_out.data_ptr(), keys_out.data_ptr() if keys_out is not None else None,
                                 workspace.data_ptr(), workspace.numel(), _stream_handle()), "cvlc_fit_alpha")
+
+
+# ----------------------------------------------------------------------------- the local step of a language-model client
+# Tensors are checked against each other here, since the library sees addresses only; nothing is copied, cast or
+# allocated, so a tensor that does not fit is refused.
+_TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+_ID_BYTES = {torch.int32: 4, torch.int64: 8}
+
+
+def _refuse(what: str, why: str) -> None:
+    raise CvlcError(ERR_ARG, f"{what}: {why}")
+
+
+def _matrix(what: str, name: str, t: torch.Tensor, rows: int, width: int):
+    """(address, type, stride) of a matrix whose rows are contiguous."""
+    if t.shape != (rows, width):
+        _refuse(what, f"{name} is {tuple(t.shape)}, not ({rows}, {width})")
+    kind = _TYPES.get(t.dtype)
+    if kind is None:
+        _refuse(what, f"{name} is {t.dtype}, not float32, bfloat16 or float16")
+    stride, step = t.stride()
+    if rows <= 1:
+        stride = max(stride, width)
+    if (step != 1 and width > 1) or stride < width:
+        _refuse(what, f"the rows of {name} are not contiguous, or overlap")
+    return t.data_ptr(), kind, stride
+
+
+def _vector(what: str, name: str, t: Optional[torch.Tensor], shape, dtype=torch.float32):
+    """Address of a contiguous tensor of one type; None stays None."""
+    if t is None:
+        return None
+    if t.shape != shape or t.dtype != dtype or not t.is_contiguous():
+        _refuse(what, f"{name} is not a contiguous {dtype} tensor of {tuple(shape)}")
+    return t.data_ptr()
+
+
+def _id_bytes(what: str, name: str, ids: torch.Tensor, dims: int) -> int:
+    size = _ID_BYTES.get(ids.dtype)
+    if size is None or ids.dim() != dims or not ids.is_contiguous():
+        _refuse(what, f"{name} is not a contiguous int32 or int64 tensor of {dims} dimension(s)")
+    return size
+
+
+def _on_device(what: str, *tensors: Optional[torch.Tensor]) -> None:
+    """All tensors lie on the current device, the one that the call's stream belongs to."""
+    here = torch.cuda.current_device() if tensors[0].is_cuda else -1
+    for t in tensors:
+        if t is not None and (here < 0 or t.get_device() != here):
+            _refuse(what, f"a tensor is on {t.device}, not on the current GPU")
+
+
+def _status(what: str, status: Optional[torch.Tensor]):
+    if status is None:
+        return None
+    if status.dtype != torch.int32 or status.numel() != 1:
+        _refuse(what, "status is not an int32 tensor of one entry")
+    return status.data_ptr()
+
+
+def embed_grad_workspace_bytes(n: int, vocab: int, dim: int) -> int:
+    return int(lib().cvlc_embed_grad_workspace_bytes(n, vocab, dim))
+
+
+def layer_norm_grad_workspace_bytes(n: int, dim: int) -> int:
+    return int(lib().cvlc_layer_norm_grad_workspace_bytes(n, dim))
+
+
+def distill_workspace_bytes(n: int, vocab: int) -> int:
+    return int(lib().cvlc_distill_workspace_bytes(n, vocab))
+
+
+def embed(ids: torch.Tensor, table: torch.Tensor, out: torch.Tensor, scale: float = 1.0,
+          status: Optional[torch.Tensor] = None) -> None:
+    """cvlc_embed on the current stream: out[i] = scale * table[ids[i]], zeros for a negative id.  `ids` is an int32
+    or int64 tensor of n tokens, `table` (vocab, dim), `out` (n, dim) of the table's type or, where that is float32,
+    of any.  `status` is an optional int32 tensor of one entry that receives DEV_INDEX for an id beyond the table."""
+    what = "cvlc_embed"
+    size, n = _id_bytes(what, "ids", ids, 1), ids.numel()
+    if table.dim() != 2:
+        _refuse(what, "table is not a matrix")
+    vocab, dim = table.shape
+    tp, tt, ts = _matrix(what, "table", table, vocab, dim)
+    op, ot, os_ = _matrix(what, "out", out, n, dim)
+    st = _status(what, status)
+    _on_device(what, ids, table, out, status)
+    _check(lib().cvlc_embed(n, ids.data_ptr(), size, tp, tt, ts, vocab, dim, scale, op, ot, os_, st, _stream_handle()), what)
+
+
+def embed_grad(ids: torch.Tensor, dout: torch.Tensor, dtable: torch.Tensor, workspace: torch.Tensor, scale: float = 1.0,
+               accumulate: bool = False) -> None:
+    """cvlc_embed_grad on the current stream: dtable[v] = scale * sum of dout[i] over the i with ids[i] = v (added to
+    what is there with `accumulate`).  `dtable` is a float32 matrix (vocab, dim), as a slice of an update vector is;
+    `workspace` holds embed_grad_workspace_bytes(n, vocab, dim), and its status word tells of ids beyond the table."""
+    what = "cvlc_embed_grad"
+    size, n = _id_bytes(what, "ids", ids, 1), ids.numel()
+    if dtable.dim() != 2 or dtable.dtype != torch.float32:
+        _refuse(what, "dtable is not a float32 matrix")
+    vocab, dim = dtable.shape
+    dp, dt, ds = _matrix(what, "dout", dout, n, dim)
+    tp, _, ts = _matrix(what, "dtable", dtable, vocab, dim)
+    _on_device(what, ids, dout, dtable, workspace)
+    _check(lib().cvlc_embed_grad(n, ids.data_ptr(), size, dp, dt, ds, vocab, dim, scale, tp, ts,
+                                 GRAD_ACCUMULATE if accumulate else 0, workspace.data_ptr(), workspace.numel(),
+                                 _stream_handle()), what)
+
+
+def layer_norm(x: torch.Tensor, gamma: Optional[torch.Tensor], beta: Optional[torch.Tensor], y: torch.Tensor,
+               stats_out: Optional[torch.Tensor] = None, eps: float = 1e-5) -> None:
+    """cvlc_layer_norm on the current stream.  `x` and `y` are (n, dim), `y` of x's type or, where that is float32, of
+    any; `gamma` and `beta` float32 of dim entries or None; `stats_out` an optional float32 (n, 2) that receives every
+    row's mean and 1/deviation."""
+    what = "cvlc_layer_norm"
+    if x.dim() != 2:
+        _refuse(what, "x is not a matrix")
+    n, dim = x.shape
+    xp, xt, xs = _matrix(what, "x", x, n, dim)
+    yp, yt, ys = _matrix(what, "y", y, n, dim)
+    gp, bp = _vector(what, "gamma", gamma, (dim,)), _vector(what, "beta", beta, (dim,))
+    sp = _vector(what, "stats_out", stats_out, (n, 2))
+    _on_device(what, x, y, gamma, beta, stats_out)
+    _check(lib().cvlc_layer_norm(n, dim, xp, xt, xs, gp, bp, eps, yp, yt, ys, sp, _stream_handle()), what)
+
+
+def layer_norm_grad(dy: torch.Tensor, x: torch.Tensor, stats: torch.Tensor, gamma: Optional[torch.Tensor],
+                    dx: Optional[torch.Tensor], dgamma: Optional[torch.Tensor], dbeta: Optional[torch.Tensor],
+                    workspace: torch.Tensor, accumulate: bool = False) -> None:
+    """cvlc_layer_norm_grad on the current stream, from the statistics that layer_norm kept.  `dx` (x's type; may be dy
+    or x themselves), `dgamma` and `dbeta` (float32; added to with `accumulate`) may each be None."""
+    what = "cvlc_layer_norm_grad"
+    if x.dim() != 2:
+        _refuse(what, "x is not a matrix")
+    n, dim = x.shape
+    xp, xt, xs = _matrix(what, "x", x, n, dim)
+    yp, yt, ys = _matrix(what, "dy", dy, n, dim)
+    dp, ds = None, 0
+    if dx is not None:
+        dp, dt, ds = _matrix(what, "dx", dx, n, dim)
+        if dt != xt:
+            _refuse(what, "dx is not of x's type")
+    sp, gp = _vector(what, "stats", stats, (n, 2)), _vector(what, "gamma", gamma, (dim,))
+    dgp, dbp = _vector(what, "dgamma", dgamma, (dim,)), _vector(what, "dbeta", dbeta, (dim,))
+    _on_device(what, x, dy, stats, gamma, dx, dgamma, dbeta, workspace)
+    _check(lib().cvlc_layer_norm_grad(n, dim, yp, yt, ys, xp, xt, xs, sp, gp, dp, ds, dgp, dbp,
+                                      GRAD_ACCUMULATE if accumulate else 0, workspace.data_ptr(), workspace.numel(),
+                                      _stream_handle()), what)
+
+
+def _lists(what: str, logits: torch.Tensor, teacher_ids: torch.Tensor, teacher_values: torch.Tensor):
+    if logits.dim() != 2:
+        _refuse(what, "logits are not a matrix")
+    n, vocab = logits.shape
+    size = _id_bytes(what, "teacher_ids", teacher_ids, 2)
+    k = teacher_ids.shape[1]
+    if teacher_ids.shape[0] != n or teacher_values.shape != (n, k) or not teacher_values.is_contiguous():
+        _refuse(what, "teacher_ids and teacher_values are not contiguous matrices of as many rows as the logits")
+    kind = _TYPES.get(teacher_values.dtype)
+    if kind is None:
+        _refuse(what, f"teacher_values are {teacher_values.dtype}, not float32, bfloat16 or float16")
+    return n, vocab, k, size, kind
+
+
+def distill(logits: torch.Tensor, teacher_ids: torch.Tensor, teacher_values: torch.Tensor,
+            loss_out: Optional[torch.Tensor], workspace: torch.Tensor, temperature: float = 1.0,
+            weights: Optional[torch.Tensor] = None, dlogits: Optional[torch.Tensor] = None,
+            stats_out: Optional[torch.Tensor] = None, logprobs: bool = False,
+            status: Optional[torch.Tensor] = None) -> None:
+    """cvlc_distill on the current stream: every row's loss against its teacher's list (float32, n entries) and, in the
+    same pass, the gradient of the losses' sum (`dlogits`, the logits' type; may be `logits` itself).  `logits` is
+    (n, vocab), the lists (n, k); `weights` float32 of n entries or None; `stats_out` an optional float32 (n, 2) for
+    distill_grad; `workspace` holds distill_workspace_bytes(n, vocab)."""
+    what = "cvlc_distill"
+    n, vocab, k, size, kind = _lists(what, logits, teacher_ids, teacher_values)
+    zp, zt, zs = _matrix(what, "logits", logits, n, vocab)
+    dp, ds = None, 0
+    if dlogits is not None:
+        dp, dt, ds = _matrix(what, "dlogits", dlogits, n, vocab)
+        if dt != zt:
+            _refuse(what, "dlogits are not of the logits' type")
+    wp, lp = _vector(what, "weights", weights, (n,)), _vector(what, "loss_out", loss_out, (n,))
+    sp, st = _vector(what, "stats_out", stats_out, (n, 2)), _status(what, status)
+    _on_device(what, logits, teacher_ids, teacher_values, loss_out, workspace, weights, dlogits, stats_out, status)
+    _check(lib().cvlc_distill(n, vocab, zp, zt, zs, k, teacher_ids.data_ptr(), size, teacher_values.data_ptr(), kind,
+                              temperature, DISTILL_LOGPROBS if logprobs else 0, wp, lp, sp, dp, ds,
+                              workspace.data_ptr(), workspace.numel(), st, _stream_handle()), what)
+
+
+def distill_grad(logits: torch.Tensor, teacher_ids: torch.Tensor, teacher_values: torch.Tensor, stats: torch.Tensor,
+                 dlogits: torch.Tensor, temperature: float = 1.0, weights: Optional[torch.Tensor] = None,
+                 logprobs: bool = False, status: Optional[torch.Tensor] = None) -> None:
+    """cvlc_distill_grad on the current stream: the gradient from the statistics that distill kept."""
+    what = "cvlc_distill_grad"
+    n, vocab, k, size, kind = _lists(what, logits, teacher_ids, teacher_values)
+    zp, zt, zs = _matrix(what, "logits", logits, n, vocab)
+    dp, dt, ds = _matrix(what, "dlogits", dlogits, n, vocab)
+    if dt != zt:
+        _refuse(what, "dlogits are not of the logits' type")
+    wp, sp, st = _vector(what, "weights", weights, (n,)), _vector(what, "stats", stats, (n, 2)), _status(what, status)
+    _on_device(what, logits, teacher_ids, teacher_values, stats, dlogits, weights, status)
+    _check(lib().cvlc_distill_grad(n, vocab, zp, zt, zs, k, teacher_ids.data_ptr(), size, teacher_values.data_ptr(),
+                                   kind, temperature, DISTILL_LOGPROBS if logprobs else 0, wp, sp, dp, ds, st,
+                                   _stream_handle()), what)
 
 
 def device_status(workspace: torch.Tensor) -> int:

@@ -1,0 +1,649 @@
+"""The operators of a language-model client's local step: embedding lookup and gradient, layer norm, distillation.
+
+Against the same formulas in 64 bits (oracle/local_step.py, which also says how far fp32 arithmetic may be off), with
+half a step of the output's type on top.
+"""
+import ctypes as C
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2402_03770_amd.cvlc as cv
+from oracle import local_step as ref
+
+DEV = "cuda:0"
+F32, BF16, F16 = torch.float32, torch.bfloat16, torch.float16
+SMALLEST = {F32: 2.0 ** -149, BF16: 2.0 ** -133, F16: 2.0 ** -24}
+gpu = pytest.mark.gpu
+
+
+def matrix(rows, width, dtype, extra=0, offset=0, fill=None):
+    """A matrix on the GPU whose rows lie `extra` apart and start `offset` elements into their buffer; the buffer too."""
+    stride = width + extra
+    flat = torch.empty(offset + rows * stride + 8, dtype=dtype, device=DEV)
+    if fill is not None:
+        flat.fill_(fill)
+    return flat[offset: offset + rows * stride].view(rows, stride)[:, :width], flat
+
+
+def random_matrix(rows, width, dtype, seed, extra=0, offset=0, scale=1.0, shift=0.0):
+    m, _ = matrix(rows, width, dtype, extra, offset, fill=float("nan"))
+    g = torch.Generator().manual_seed(seed)
+    m.copy_((torch.randn(rows, width, generator=g) * scale + shift).to(dtype))
+    return m
+
+
+def f64(t):
+    return t.detach().cpu().to(torch.float64).numpy()
+
+
+def assert_near(got, want, tol, dtype=F32, what=""):
+    got = f64(got)
+    assert got.shape == want.shape, what
+    with np.errstate(invalid="ignore"):
+        over = np.isfinite(want) & np.isinf(got) & (np.sign(got) == np.sign(want)) & (np.abs(want) + tol > torch.finfo(dtype).max)
+    want = np.where(over, got, want)          # beyond the type's largest value, or as near to it as rounding goes
+    fine = np.isfinite(want)
+    assert np.array_equal(np.isnan(got), np.isnan(want)) and np.array_equal(got[~fine & ~np.isnan(want)], want[~fine & ~np.isnan(want)]), what
+    err = np.abs(got[fine] - want[fine])
+    # the half step is taken of a value that is itself off by `tol`
+    allowed = tol[fine] + ref.half_step(np.abs(want[fine]) + tol[fine], torch.finfo(dtype).eps, SMALLEST[dtype])
+    worst = int(np.argmax(err - allowed)) if err.size else 0
+    assert np.all(err <= allowed), f"{what}: off by {err[worst]:.3e}, allowed {allowed[worst]:.3e}, value {want[fine][worst]:.3e}"
+
+
+def untouched(flat, m, fill):
+    """Nothing of the buffer outside the matrix was written."""
+    m.fill_(fill)
+    return bool((flat == fill).all())
+
+
+def tokens(n, vocab, seed, padding=0.2, kind=torch.int64):
+    rng = np.random.default_rng(seed)
+    ids = np.minimum((np.exp(rng.random(n) * np.log(vocab + 1.0)) - 1).astype(np.int64), vocab - 1)
+    ids[rng.random(n) < padding] = -1
+    return torch.from_numpy(ids).to(kind)
+
+
+# ----------------------------------------------------------------------------- embedding
+@gpu
+@pytest.mark.parametrize("types", [(F32, F32), (BF16, BF16), (F16, F16), (F32, BF16), (F32, F16)])
+@pytest.mark.parametrize("n,dim,vocab,extra,offset", [(1, 1, 1, 0, 0), (5, 7, 3, 1, 1), (64, 96, 1000, 0, 0), (300, 130, 50, 3, 1),
+                                                      (17, 513, 62, 8, 0), (1000, 64, 2048, 0, 0), (3, 5000, 11, 0, 0)])
+def test_embed(types, n, dim, vocab, extra, offset):
+    tt, to = types
+    table = random_matrix(vocab, dim, tt, 1, extra, offset)
+    ids = tokens(n, vocab, 2, kind=torch.int32 if n % 2 else torch.int64)
+    out, flat = matrix(n, dim, to, extra, offset, fill=3.0)
+    status = torch.zeros(1, dtype=torch.int32, device=DEV)
+    cv.embed(ids.to(DEV), table, out, scale=1.7, status=status)
+    want, tol = ref.embed(ids.numpy(), f64(table), 1.7)
+    assert_near(out, want, tol, to)
+    assert not bool(status.item()) and untouched(flat, out, 3.0)
+
+
+@gpu
+def test_embed_ids_beyond_the_table():
+    table = random_matrix(10, 33, F32, 1)
+    ids = torch.tensor([3, 10, -1, 2**40, -(2**40), 9])
+    out, status = torch.empty(6, 33, device=DEV), torch.zeros(1, dtype=torch.int32, device=DEV)
+    cv.embed(ids.to(DEV), table, out, status=status)
+    assert status.item() == cv.DEV_INDEX
+    want, tol = ref.embed(ids.numpy(), f64(table), 1.0)
+    assert_near(out, want, tol)
+    cv.embed(ids.to(DEV), table, out)                       # no status word: zeros all the same
+    assert_near(out, want, tol)
+
+
+SORTS = [(1, 1), (5, 3), (640, 1000), (4096, 2047), (4097, 2048), (5000, 32000), (20000, 5), (3000, 4_200_000)]
+
+
+def check_embed_grad(ids, dout, vocab, scale=1.0, start=None, extra=0, offset=0):
+    n, dim = dout.shape
+    dtable, flat = matrix(vocab, dim, F32, extra, offset, fill=5.0)
+    if start is not None:
+        dtable.copy_(start)
+    ws = cv.new_workspace(cv.embed_grad_workspace_bytes(n, vocab, dim), DEV)
+    ws.fill_(0xA5)
+    cv.embed_grad(ids.to(DEV), dout, dtable, ws, scale=scale, accumulate=start is not None)
+    status = cv.device_status(ws)
+    want, tol = ref.embed_grad(ids.numpy(), f64(dout), vocab, scale, None if start is None else f64(start))
+    assert_near(dtable, want, tol)
+    got = dtable.clone()
+    assert untouched(flat, dtable, 5.0)
+    return got, status
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("n,vocab", SORTS)
+def test_embed_grad(dtype, n, vocab):
+    dim = 9 if vocab > 100_000 else 41
+    dout = random_matrix(n, dim, dtype, 3, extra=2, offset=1)
+    ids = tokens(n, vocab, 4, kind=torch.int32 if n % 2 else torch.int64)
+    _, status = check_embed_grad(ids, dout, vocab, scale=0.3, extra=1, offset=3)
+    assert status == 0
+
+
+@gpu
+@pytest.mark.parametrize("n,dim,vocab", [(0, 12, 70), (1, 1, 5), (700, 1, 7), (130, 1025, 20), (9000, 128, 300), (300_000, 8, 900)])
+def test_embed_grad_sizes(n, dim, vocab):
+    dout = random_matrix(n, dim, BF16, 5)
+    check_embed_grad(tokens(n, vocab, 6), dout, vocab)
+
+
+@gpu
+@pytest.mark.parametrize("kind", ["one", "padding", "one beyond", "ends", "runs", "descending"])
+@pytest.mark.parametrize("n", [64, 65, 1000, 5000])
+def test_embed_grad_of_tokens_in_odd_order(kind, n):
+    """One token only, none, none but beyond the table, the table's ends, runs that end at and across chunks' borders."""
+    vocab, dim = 500, 36
+    i = torch.arange(n)
+    ids = {"one": torch.full((n,), 77), "padding": torch.full((n,), -1), "one beyond": torch.full((n,), 500),
+           "ends": torch.where(i % 3 == 0, 0, 499), "runs": (i // 64) % vocab, "descending": (n - i) // 37 % vocab}[kind]
+    dout = random_matrix(n, dim, F32, 7)
+    _, status = check_embed_grad(ids.long(), dout, vocab)
+    assert status == (cv.DEV_INDEX if kind == "one beyond" else 0)
+
+
+@gpu
+def test_embed_grad_adds_to_the_table_and_repeats_itself():
+    n, dim, vocab = 6000, 72, 800
+    ids, dout = tokens(n, vocab, 8), random_matrix(n, dim, BF16, 9)
+    start = random_matrix(vocab, dim, F32, 10)
+    a, _ = check_embed_grad(ids, dout, vocab, start=start)
+    b, _ = check_embed_grad(ids, dout, vocab, start=start)
+    assert torch.equal(a, b)
+    gone = torch.ones(vocab, dtype=torch.bool)
+    gone[ids[ids >= 0]] = False
+    assert torch.equal(a[gone.to(DEV)], start[gone.to(DEV)])
+    a, _ = check_embed_grad(ids, dout, vocab)
+    b, _ = check_embed_grad(ids, dout, vocab)
+    assert torch.equal(a, b)
+
+
+@gpu
+def test_embed_grad_is_the_lookups():
+    """<lookup(W), D> is linear in W: its derivative along V is <lookup(V), D> = <gradient, V>."""
+    n, dim, vocab, scale = 500, 24, 90, 3.0
+    ids, V, D = tokens(n, vocab, 11).to(DEV), random_matrix(vocab, dim, F32, 12), random_matrix(n, dim, F32, 13)
+    out, grad = torch.empty(n, dim, device=DEV), torch.empty(vocab, dim, device=DEV)
+    cv.embed(ids, V, out, scale=scale)
+    cv.embed_grad(ids, D, grad, cv.new_workspace(cv.embed_grad_workspace_bytes(n, vocab, dim), DEV), scale=scale)
+    left, right = f64(out) * f64(D), f64(grad) * f64(V)
+    _, tol = ref.embed_grad(ids.cpu().numpy(), f64(D), vocab, scale)
+    slack = (np.abs(left) * 2 * ref.U).sum() + ((tol + np.abs(f64(grad)) * ref.U) * np.abs(f64(V))).sum()
+    assert abs(left.sum() - right.sum()) <= slack
+
+
+# ----------------------------------------------------------------------------- layer norm
+NORMS = [(1, 1), (3, 2), (2, 7), (5, 64), (9, 100), (4, 255), (70, 256), (33, 1003), (6, 2048), (3, 4096), (5, 5000), (2, 8192), (2, 16384),
+         (2, 16385), (1, 40000)]
+
+
+@gpu
+@pytest.mark.parametrize("types", [(F32, F32), (BF16, BF16), (F16, F16), (F32, BF16), (F32, F16)])
+@pytest.mark.parametrize("n,dim", NORMS)
+def test_layer_norm(types, n, dim):
+    tx, ty = types
+    extra, offset = (0, 0) if n % 2 else (3, 1)
+    x = random_matrix(n, dim, tx, 20 + dim, extra, offset, scale=2.0, shift=3.0)
+    gamma = None if n == 5 else random_matrix(1, dim, F32, 21)[0].contiguous()
+    beta = None if n in (5, 9) else random_matrix(1, dim, F32, 22)[0].contiguous()
+    y, flat = matrix(n, dim, ty, extra, offset, fill=7.0)
+    stats = torch.empty(n, 2, device=DEV)
+    cv.layer_norm(x, gamma, beta, y, stats, eps=1e-3)
+    want, tol, s, s_tol = ref.layer_norm(f64(x), None if gamma is None else f64(gamma), None if beta is None else f64(beta), 1e-3)
+    assert_near(stats, s, s_tol, what="stats")
+    assert_near(y, want, tol, ty, what="y")
+    assert untouched(flat, y, 7.0)
+
+
+@gpu
+@pytest.mark.parametrize("n,dim", [(3, 100), (200, 512), (2, 20000)])
+def test_layer_norm_in_place_without_statistics(n, dim):
+    x = random_matrix(n, dim, BF16, 23)
+    want, tol, _, _ = ref.layer_norm(f64(x), None, None, 1e-5)
+    cv.layer_norm(x, None, None, x)
+    assert_near(x, want, tol, BF16)
+
+
+@gpu
+def test_layer_norm_of_odd_rows():
+    """Rows of equal values, with an infinity or a NaN: theirs alone; a mean far from zero costs the deviations nothing."""
+    x = random_matrix(6, 300, F32, 24)
+    x[1] = 4.0
+    x[2, 7] = float("inf")
+    x[3, 299] = float("nan")
+    x[4] += 4096.0
+    y, stats = torch.empty_like(x), torch.empty(6, 2, device=DEV)
+    cv.layer_norm(x, None, None, y, stats)
+    assert torch.isnan(y[2]).all() and torch.isnan(y[3]).all()
+    assert torch.equal(y[1], torch.zeros_like(y[1])) and stats[1].tolist() == [4.0, float(np.float32(1.0) / np.sqrt(np.float32(1e-5)))]
+    keep = [0, 4, 5]
+    want, tol, s, s_tol = ref.layer_norm(f64(x)[keep], None, None, 1e-5)
+    assert_near(y[keep], want, tol)
+    assert_near(stats[keep], s, s_tol)
+
+
+def check_norm_grad(n, dim, tx, ty, seed, extra=0, offset=0, affine=True, start=False, parts=("dx", "dgamma", "dbeta")):
+    x = random_matrix(n, dim, tx, seed, extra, offset, scale=2.0, shift=1.0)
+    dy = random_matrix(n, dim, ty, seed + 1, extra, offset)
+    gamma = random_matrix(1, dim, F32, seed + 2)[0].contiguous() if affine else None
+    if n:
+        _, _, s, _ = ref.layer_norm(f64(x), None, None, 1e-5)
+        stats = torch.from_numpy(s.astype(np.float32)).to(DEV)
+    else:
+        stats = torch.empty(0, 2, device=DEV)
+    dx, flat = matrix(n, dim, tx, extra, offset, fill=7.0)
+    first = torch.randn(2, dim, generator=torch.Generator().manual_seed(seed)).to(DEV)
+    sums = first.clone() if start else torch.full((2, dim), 9.0, device=DEV)
+    ws = cv.new_workspace(cv.layer_norm_grad_workspace_bytes(n, dim), DEV)
+    ws.fill_(0xA5)
+    cv.layer_norm_grad(dy, x, stats, gamma, dx if "dx" in parts else None, sums[0] if "dgamma" in parts else None,
+                       sums[1] if "dbeta" in parts else None, ws, accumulate=start)
+    want = ref.layer_norm_grad(f64(dy), f64(x), f64(stats), None if gamma is None else f64(gamma))
+    if "dx" in parts:
+        assert_near(dx, want[0], want[1], tx, "dx")
+        assert untouched(flat, dx, 7.0)
+    for k, name in enumerate(("dgamma", "dbeta")):
+        if name not in parts:
+            assert bool((sums[k] == (first[k] if start else 9.0)).all())
+            continue
+        w, tol = want[2 + 2 * k], want[3 + 2 * k]
+        if start:
+            w = w + f64(first[k])
+            tol = tol + 17 * ref.U * (np.abs(w) + np.abs(f64(first[k])))   # the old value is added first, sixteen sums after it
+        assert_near(sums[k], w, tol, what=name)
+    return sums
+
+
+@gpu
+@pytest.mark.parametrize("types", [(F32, F32), (BF16, BF16), (F16, F16), (F32, BF16), (F32, F16)])
+@pytest.mark.parametrize("n,dim", NORMS + [(300, 31), (1500, 129)])
+def test_layer_norm_grad(types, n, dim):
+    check_norm_grad(n, dim, *types, seed=30 + dim, extra=0 if n % 2 else 3, offset=0 if n % 2 else 1, affine=n != 5)
+
+
+@gpu
+@pytest.mark.parametrize("n,dim", [(0, 40), (40, 200), (2, 20000)])
+def test_layer_norm_grad_parts_and_sums(n, dim):
+    for parts in (("dx",), ("dgamma",), ("dbeta",), ("dx", "dbeta"), ("dgamma", "dbeta")):
+        check_norm_grad(n, dim, BF16, BF16, 40, parts=parts)
+    a = check_norm_grad(n, dim, F32, F32, 41, start=True)
+    b = check_norm_grad(n, dim, F32, F32, 41, start=True)
+    assert torch.equal(a, b)
+
+
+@gpu
+@pytest.mark.parametrize("n,dim", [(50, 96), (600, 768), (3, 20000)])
+@pytest.mark.parametrize("place", ["dy", "x"])
+def test_layer_norm_grad_in_place(n, dim, place):
+    x, dy = random_matrix(n, dim, BF16, 42), random_matrix(n, dim, BF16, 43)
+    _, _, s, _ = ref.layer_norm(f64(x), None, None, 1e-5)
+    stats = torch.from_numpy(s.astype(np.float32)).to(DEV)
+    want = ref.layer_norm_grad(f64(dy), f64(x), f64(stats), None)
+    dx, sums = {"dy": dy, "x": x}[place], torch.empty(2, dim, device=DEV)
+    cv.layer_norm_grad(dy, x, stats, None, dx, sums[0], sums[1], cv.new_workspace(cv.layer_norm_grad_workspace_bytes(n, dim), DEV))
+    assert_near(dx, want[0], want[1], BF16)
+    assert_near(sums[0], want[2], want[3])
+    assert_near(sums[1], want[4], want[5])
+
+
+def test_norm_formulas_against_differences():
+    """The oracle's gradients against differences of its forward pass, in 64 bits."""
+    rng = np.random.default_rng(5)
+    n, dim, h = 4, 33, 1e-5
+    x, dy, gamma, beta = (rng.standard_normal(s) for s in ((n, dim), (n, dim), dim, dim))
+    eps = float(np.float32(1e-3))
+    stats = ref.layer_norm(x, gamma, beta, eps)[2]
+    dx, _, dgamma, _, dbeta, _ = ref.layer_norm_grad(dy, x, stats, gamma)
+    value = lambda x, g, b: (ref.layer_norm(x, g, b, eps)[0] * dy).sum()    # noqa: E731
+    for _ in range(5):
+        vx, vg, vb = rng.standard_normal((n, dim)), rng.standard_normal(dim), rng.standard_normal(dim)
+        slope = (value(x + h * vx, gamma + h * vg, beta + h * vb) - value(x - h * vx, gamma - h * vg, beta - h * vb)) / (2 * h)
+        assert slope == pytest.approx((dx * vx).sum() + (dgamma * vg).sum() + (dbeta * vb).sum(), rel=1e-6, abs=1e-6)
+
+
+# ----------------------------------------------------------------------------- distillation
+def lists(n, vocab, k, seed, gaps=True, kind=torch.int32, dtype=F32):
+    rng = np.random.default_rng(seed)
+    ids = np.stack([rng.choice(vocab, size=k, replace=k > vocab) for _ in range(n)]) if n else np.zeros((0, k), np.int64)
+    values = np.sort(rng.standard_normal((n, k)) * 3, axis=1)[:, ::-1].copy()
+    if gaps and k > 2:
+        ids[:, 1] = np.where(rng.random(n) < 0.3, -1, ids[:, 1])
+        values[:, 2] = np.where(rng.random(n) < 0.3, -np.inf, values[:, 2])
+        ids[:, k - 1] = np.where(rng.random(n) < 0.3, ids[:, 0], ids[:, k - 1])          # a second time
+    return torch.from_numpy(ids).to(kind).to(DEV), torch.from_numpy(values).to(dtype).to(DEV)
+
+
+def check_distill(logits, ids, values, T=1.0, weights=None, logprobs=False, in_place=False, extra=0, offset=0, status=0):
+    n, vocab = logits.shape
+    dtype = logits.dtype
+    args = [f64(logits), ids.cpu().numpy(), f64(values)]
+    w = None if weights is None else f64(weights)
+    loss, loss_tol, stats, stats_tol, grad, grad_tol = ref.distill(*args, T=T, weights=w, logprobs=logprobs)
+    ws = cv.new_workspace(cv.distill_workspace_bytes(n, vocab), DEV)
+    ws.fill_(0xA5)
+
+    def fresh(*shape):
+        return torch.full(shape, 11.0, device=DEV)
+
+    word = torch.zeros(1, dtype=torch.int32, device=DEV)
+    got_loss, got_stats = fresh(n), fresh(n, 2)
+    cv.distill(logits, ids, values, got_loss, ws, temperature=T, weights=weights, stats_out=got_stats, logprobs=logprobs, status=word)
+    assert_near(got_loss, loss, loss_tol, what="loss alone")
+    assert_near(got_stats, stats, stats_tol, what="statistics")
+    assert word.item() == status
+
+    d, flat = matrix(n, vocab, dtype, extra, offset, fill=13.0)
+    cv.distill_grad(logits, ids, values, got_stats, d, temperature=T, weights=weights, logprobs=logprobs)
+    assert_near(d, grad, grad_tol, dtype, "gradient alone")
+    assert untouched(flat, d, 13.0)
+
+    got_loss, got_stats = fresh(n), fresh(n, 2)
+    d, flat = (logits, None) if in_place else matrix(n, vocab, dtype, extra, offset, fill=13.0)
+    cv.distill(logits, ids, values, got_loss, ws, temperature=T, weights=weights, dlogits=d, stats_out=got_stats, logprobs=logprobs)
+    assert_near(got_loss, loss, loss_tol, what="loss")
+    assert_near(got_stats, stats, stats_tol, what="statistics beside the gradient")
+    assert_near(d, grad, grad_tol, dtype, "gradient")
+    assert in_place or untouched(flat, d, 13.0)
+    return got_loss
+
+
+DISTILLS = [(1, 1, 1), (2, 2, 2), (3, 7, 5), (40, 10, 3), (64, 62, 10), (65, 100, 100), (9, 1000, 64), (5, 2047, 33), (4, 4096, 256),
+            (3, 8193, 1024), (3, 20011, 20), (2, 50001, 64), (1, 131072, 64), (2, 200003, 7), (1, 262144, 16)]
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("n,vocab,k", DISTILLS)
+def test_distill(dtype, n, vocab, k):
+    extra, offset = (0, 0) if n % 2 else (5, 1)
+    logits = random_matrix(n, vocab, dtype, 50 + vocab, extra, offset, scale=3.0)
+    ids, values = lists(n, vocab, k, 51, kind=torch.int64 if k % 2 else torch.int32)
+    check_distill(logits, ids, values, T=2.0 if n % 3 else 0.7, extra=extra, offset=offset, in_place=n % 2 == 0)
+
+
+@gpu
+@pytest.mark.parametrize("n,vocab", [(300, 62), (70, 9000), (300, 40000), (33, 131072)])
+def test_distill_with_weights(n, vocab):
+    """Rows without weight among others, weights below zero; their places in the outputs are zeros, their logits unread."""
+    logits = random_matrix(n, vocab, BF16, 60, scale=3.0)
+    ids, values = lists(n, vocab, 12, 61, dtype=BF16)
+    weights = torch.randn(n, generator=torch.Generator().manual_seed(62)).to(DEV)
+    weights[::3] = 0.0
+    plain = logits.clone()
+    logits[::3] = float("nan")
+    logits_f = torch.where((weights == 0)[:, None], plain, logits)
+    del plain
+    got = check_distill(logits_f.clone(), ids, values, T=1.5, weights=weights)
+    loss = torch.empty_like(got)
+    cv.distill(logits, ids, values, loss, cv.new_workspace(cv.distill_workspace_bytes(n, vocab), DEV), temperature=1.5, weights=weights)
+    assert torch.equal(loss, got)
+
+
+@gpu
+@pytest.mark.parametrize("vocab", [100, 6000, 70001, 150001])
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+def test_distill_masks(vocab, dtype):
+    """Masked logits (-inf, the type's lowest value), rows that are masked whole, lists that hold nothing."""
+    n, k = 9, 8
+    logits = random_matrix(n, vocab, dtype, 70, scale=3.0)
+    ids, values = lists(n, vocab, k, 71, gaps=False)
+    low = torch.finfo(dtype).min
+    logits[0, ::2] = float("-inf")
+    logits[0, ids[0].long()] = 1.0
+    logits[1] = float("-inf")                    # nothing left: q = 0
+    logits[2] = low                              # all alike, however low
+    logits[3, 1:] = low
+    logits[3, 0] = 30.0
+    ids[4] = -1                                  # no list
+    values[5] = float("-inf")
+    logits[6, int(ids[6, 0])] = float("-inf")    # the teacher wants what is masked
+    values[7, 3:] = torch.finfo(F32).min
+    logits[8] = torch.finfo(dtype).max
+    for T in (1.0, 0.25, 3.0):
+        got = check_distill(logits, ids, values, T=T)
+        assert got[1].item() == got[6].item() == float("inf") and got[4].item() == got[5].item() == 0.0
+    ids[8, 2] = vocab
+    check_distill(logits, ids, values, status=cv.DEV_INDEX)
+
+
+@gpu
+@pytest.mark.parametrize("vocab", [100, 6000, 150001])
+def test_distill_nan_stays_in_its_row(vocab):
+    n, k = 6, 5
+    logits = random_matrix(n, vocab, F32, 72)
+    ids, values = lists(n, vocab, k, 73, gaps=False)
+    logits[1, vocab // 2] = float("nan")
+    logits[2, vocab - 1] = float("inf")
+    values[3, 1] = float("nan")
+    values[4, 0] = float("inf")
+    values[5] = float("nan")
+    d, loss, stats = torch.empty_like(logits), torch.empty(n, device=DEV), torch.empty(n, 2, device=DEV)
+    ws = cv.new_workspace(cv.distill_workspace_bytes(n, vocab), DEV)
+    cv.distill(logits, ids, values, loss, ws, dlogits=d, stats_out=stats)
+    assert torch.isnan(loss).tolist() == [False] + [True] * 5
+    assert torch.isnan(d[1:]).all() and torch.isfinite(d[0]).all()
+    cv.distill_grad(logits, ids, values, stats, d)
+    assert torch.isnan(d[1:]).all() and torch.isfinite(d[0]).all()
+
+
+@gpu
+@pytest.mark.parametrize("n,vocab,k", [(50, 62, 20), (7, 5000, 64), (3, 140000, 30)])
+def test_distill_of_log_probabilities(n, vocab, k):
+    logits = random_matrix(n, vocab, BF16, 74, scale=2.0)
+    ids, values = lists(n, vocab, k, 75)
+    values = torch.log_softmax(values, 1) - 0.3          # three quarters of the teacher's mass are in the list
+    check_distill(logits, ids, values, T=2.0, logprobs=True)
+    same = torch.full_like(values, float("-inf"))        # and one whose list is empty
+    values[0] = same[0]
+    check_distill(logits, ids, values, T=1.0, logprobs=True)
+
+
+@gpu
+def test_distill_in_place_repeats_itself():
+    for n, vocab in ((500, 100), (300, 5001), (20, 100000), (3, 262143)):
+        logits = random_matrix(n, vocab, BF16, 76, scale=2.0)
+        ids, values = lists(n, vocab, 9, 77)
+        ws = cv.new_workspace(cv.distill_workspace_bytes(n, vocab), DEV)
+        a, b, la, lb = torch.empty_like(logits), logits.clone(), torch.empty(n, device=DEV), torch.empty(n, device=DEV)
+        cv.distill(logits, ids, values, la, ws, dlogits=a)
+        cv.distill(b, ids, values, lb, ws, dlogits=b)
+        assert torch.equal(a, b) and torch.equal(la, lb)
+
+
+def test_distill_formula_against_differences():
+    rng = np.random.default_rng(6)
+    n, vocab, k, h = 5, 40, 7, 1e-5
+    z, values = rng.standard_normal((n, vocab)), rng.standard_normal((n, k))
+    ids = np.stack([rng.choice(vocab, k, replace=True) for _ in range(n)])
+    w = rng.standard_normal(n)
+    for T, logprobs in ((1.0, False), (2.0, False), (0.5, True)):
+        grad = ref.distill(z, ids, values, T, w, logprobs)[4]
+        for _ in range(4):
+            v = rng.standard_normal(z.shape)
+            up, down = (ref.distill(z + s * h * v, ids, values, T, w, logprobs)[0].sum() for s in (1, -1))
+            assert (up - down) / (2 * h) == pytest.approx((grad * v).sum(), rel=1e-6, abs=1e-6)
+
+
+# ----------------------------------------------------------------------------- streams, graphs
+@gpu
+def test_local_step_on_a_side_stream_and_in_a_graph():
+    """Behind the kernels that make its inputs, on a stream of its own; then captured and replayed on fresh inputs, with
+    eager work in between."""
+    n, dim, vocab, k = 200, 160, 3001, 16
+    table, gamma, beta = random_matrix(vocab, dim, F32, 80, scale=0.1), torch.ones(dim, device=DEV), torch.zeros(dim, device=DEV)
+    ids, (tids, tvals) = tokens(n, vocab, 81).to(DEV), lists(n, vocab, k, 82)
+    x, y, stats = torch.empty(n, dim, device=DEV), torch.empty(n, dim, device=DEV), torch.empty(n, 2, device=DEV)
+    logits, loss = torch.empty(n, vocab, device=DEV), torch.empty(n, device=DEV)
+    dy, dx = torch.empty(n, dim, device=DEV), torch.empty(n, dim, device=DEV)
+    update = torch.empty(vocab * dim + 2 * dim, device=DEV)
+    wse = cv.new_workspace(cv.embed_grad_workspace_bytes(n, vocab, dim), DEV)
+    wsn = cv.new_workspace(cv.layer_norm_grad_workspace_bytes(n, dim), DEV)
+    wsd = cv.new_workspace(cv.distill_workspace_bytes(n, vocab), DEV)
+
+    def step():
+        cv.embed(ids, table, x, scale=4.0)
+        cv.layer_norm(x, gamma, beta, y, stats)
+        torch.mm(y, table.t(), out=logits)
+        cv.distill(logits, tids, tvals, loss, wsd, temperature=2.0, dlogits=logits)
+        torch.mm(logits, table, out=dy)
+        cv.layer_norm_grad(dy, x, stats, gamma, dx, update[vocab * dim: vocab * dim + dim], update[vocab * dim + dim:], wsn)
+        cv.embed_grad(ids, dx, update[: vocab * dim].view(vocab, dim), wse, scale=4.0)
+
+    def fresh(seed):
+        ids.copy_(tokens(n, vocab, seed))
+        a, b = lists(n, vocab, k, seed + 1)
+        tids.copy_(a)
+        tvals.copy_(b)
+
+    step()
+    torch.cuda.synchronize()
+    want = update.clone(), loss.clone()
+    update.fill_(1.0)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        table.mul_(2.0).mul_(0.5)
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    assert torch.equal(update, want[0]) and torch.equal(loss, want[1])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for seed in (90, 91, 92):
+        fresh(seed)
+        graph.replay()
+        torch.cuda.synchronize()
+        got = update.clone(), loss.clone()
+        update.fill_(2.0)
+        step()
+        assert torch.equal(update, got[0]) and torch.equal(loss, got[1])
+
+
+# ----------------------------------------------------------------------------- refusals (CPU)
+ARG, CAP = -1, -4
+P = 0x10000
+
+
+def test_refusals_of_the_library():
+    """What the host can see is refused before anything is launched: addresses here are made up."""
+    L, vp, inf, nan = cv.lib(), C.c_void_p, float("inf"), float("nan")
+
+    def embed(n=4, ids=P, size=8, table=P, tt=0, ts=8, vocab=10, dim=8, scale=1.0, out=P, ot=0, os_=8, status=None):
+        return L.cvlc_embed(n, vp(ids), size, vp(table), tt, ts, vocab, dim, scale, vp(out), ot, os_, vp(status), None)
+
+    for bad in (dict(ids=None), dict(table=None), dict(out=None), dict(size=2), dict(tt=3), dict(ot=7), dict(tt=1), dict(ts=7), dict(os_=7),
+                dict(vocab=0), dict(dim=0), dict(scale=inf), dict(scale=nan), dict(ids=P + 4), dict(table=P + 2), dict(out=P + 1), dict(status=P + 2),
+                dict(n=2**31), dict(vocab=2**31), dict(tt=1, ot=2)):
+        assert embed(**bad) == ARG, bad
+    assert embed(n=0, ids=None, table=None, out=None) == 0
+
+    need = cv.embed_grad_workspace_bytes(4, 10, 8)
+    assert need > 0 and cv.embed_grad_workspace_bytes(4, 0, 8) == 0
+
+    def embed_grad(n=4, ids=P, size=8, dout=P, dt=0, ds=8, vocab=10, dim=8, scale=1.0, dtable=P, ts=8, flags=0, ws=P, bytes_=need):
+        return L.cvlc_embed_grad(n, vp(ids), size, vp(dout), dt, ds, vocab, dim, scale, vp(dtable), ts, flags, vp(ws), bytes_, None)
+
+    for bad in (dict(ids=None), dict(dout=None), dict(dtable=None), dict(ws=None), dict(size=1), dict(dt=9), dict(ds=7), dict(ts=7), dict(flags=2),
+                dict(vocab=0), dict(dim=0), dict(scale=nan), dict(ids=P + 4), dict(dout=P + 2), dict(dtable=P + 2), dict(ws=P + 128), dict(n=2**31)):
+        assert embed_grad(**bad) == ARG, bad
+    assert embed_grad(bytes_=need - 1) == CAP
+
+    def norm(n=4, dim=8, x=P, xt=0, xs=8, gamma=P, beta=P, eps=1e-5, y=2 * P, yt=0, ys=8, stats=P):
+        return L.cvlc_layer_norm(n, dim, vp(x), xt, xs, vp(gamma), vp(beta), eps, vp(y), yt, ys, vp(stats), None)
+
+    for bad in (dict(x=None), dict(y=None), dict(dim=0), dict(xt=3), dict(yt=3), dict(xt=1), dict(xs=7), dict(ys=7), dict(eps=-1e-9), dict(eps=nan),
+                dict(eps=inf), dict(gamma=P + 2), dict(beta=P + 1), dict(stats=P + 2), dict(x=P + 2), dict(y=P + 2), dict(n=2**31),
+                dict(y=P, ys=9), dict(y=P, yt=1)):
+        assert norm(**bad) == ARG, bad
+    assert norm(n=0, x=None, y=None) == 0
+
+    need = cv.layer_norm_grad_workspace_bytes(4, 8)
+
+    def norm_grad(n=4, dim=8, dy=P, dyt=0, dys=8, x=2 * P, xt=0, xs=8, stats=P, gamma=P, dx=3 * P, dxs=8, dg=P, db=P, flags=0, ws=P, bytes_=need):
+        return L.cvlc_layer_norm_grad(n, dim, vp(dy), dyt, dys, vp(x), xt, xs, vp(stats), vp(gamma), vp(dx), dxs, vp(dg), vp(db), flags, vp(ws), bytes_,
+                                      None)
+
+    for bad in (dict(dy=None), dict(x=None), dict(stats=None), dict(ws=None), dict(dx=None, dg=None, db=None), dict(dim=0), dict(xt=4), dict(dyt=4),
+                dict(xt=1), dict(xs=7), dict(dys=7), dict(dxs=7), dict(flags=4), dict(gamma=P + 2), dict(dg=P + 2), dict(db=P + 2), dict(dx=P + 2),
+                dict(ws=P + 8), dict(dx=P, dxs=9), dict(dx=2 * P, dxs=9), dict(dyt=1, dx=P), dict(n=2**31)):
+        assert norm_grad(**bad) == ARG, bad
+    assert norm_grad(bytes_=need - 1) == CAP
+
+    need = cv.distill_workspace_bytes(4, 100)
+    good = dict(n=4, vocab=100, z=P, t=0, s=100, k=5, ids=P, size=4, values=P, vt=0, T=1.0, flags=0, w=P, loss=P, stats=P, d=2 * P, ds=100, ws=P,
+                bytes_=need, status=P)
+
+    def distill(**change):
+        a = {**good, **change}
+        return L.cvlc_distill(a["n"], a["vocab"], vp(a["z"]), a["t"], a["s"], a["k"], vp(a["ids"]), a["size"], vp(a["values"]), a["vt"], a["T"],
+                              a["flags"], vp(a["w"]), vp(a["loss"]), vp(a["stats"]), vp(a["d"]), a["ds"], vp(a["ws"]), a["bytes_"], vp(a["status"]), None)
+
+    def distill_grad(**change):
+        a = {**good, **change}
+        return L.cvlc_distill_grad(a["n"], a["vocab"], vp(a["z"]), a["t"], a["s"], a["k"], vp(a["ids"]), a["size"], vp(a["values"]), a["vt"], a["T"],
+                                   a["flags"], vp(a["w"]), vp(a["stats"]), vp(a["d"]), a["ds"], vp(a["status"]), None)
+
+    for bad in (dict(z=None), dict(ids=None), dict(values=None), dict(vocab=0), dict(k=0), dict(k=1025), dict(t=3), dict(vt=3), dict(s=99), dict(ds=99),
+                dict(size=3), dict(flags=2), dict(T=0.0), dict(T=-1.0), dict(T=inf), dict(T=nan), dict(T=1e-30), dict(w=P + 2), dict(stats=P + 2),
+                dict(d=P + 2), dict(z=P + 2), dict(ids=P + 2), dict(values=P + 2), dict(status=P + 2), dict(d=P, ds=101), dict(n=2**31)):
+        assert distill(**bad) == ARG and distill_grad(**bad) == ARG, bad
+    for bad in (dict(ws=None), dict(ws=P + 4), dict(loss=P + 2), dict(loss=None, stats=None, d=None)):
+        assert distill(**bad) == ARG, bad
+    assert distill(bytes_=need - 1) == CAP
+    assert distill_grad(stats=None) == ARG and distill_grad(d=None) == ARG
+    assert distill(n=0, z=None, ids=None, values=None) == 0 and distill_grad(n=0, z=None, ids=None, values=None) == 0
+
+
+def test_refusals_of_the_binding():
+    """Tensors that do not go together, and tensors that are not on the GPU."""
+    ids, table, out = torch.zeros(4, dtype=torch.int64), torch.zeros(10, 8), torch.zeros(4, 8)
+    ws, status = torch.zeros(1 << 16, dtype=torch.uint8), torch.zeros(1, dtype=torch.int32)
+
+    def refused(f, *args, **more):
+        with pytest.raises(cv.CvlcError) as e:
+            f(*args, **more)
+        assert e.value.code == ARG
+        return str(e.value)
+
+    assert "GPU" in refused(cv.embed, ids, table, out, status=status)
+    for a in ((ids.float(), table, out), (ids[None], table, out), (ids, table[0], out), (ids, table, out[:3]), (ids, table, out[:, :7]), (ids, table.t(), out),
+              (ids, table.double(), out), (ids, table, out[:1].expand(4, 8)), (ids, table, out.t().contiguous().t()), (torch.zeros(8, dtype=torch.int64)[::2], table, out)):
+        assert "GPU" not in refused(cv.embed, *a)
+    refused(cv.embed, ids, table, out, status=torch.zeros(2, dtype=torch.int32))
+    assert "GPU" in refused(cv.embed_grad, ids, out, table, ws)
+    for a in ((ids, out[:3], table), (ids, out, table.bfloat16()), (ids, out, table[0]), (ids[:3], out, table), (ids, out[:, ::2], table[:, :4])):
+        assert "GPU" not in refused(cv.embed_grad, *a, ws)
+    x, v, st = torch.zeros(4, 8), torch.zeros(8), torch.zeros(4, 2)
+    assert "GPU" in refused(cv.layer_norm, x, v, v, x, st)
+    for a in ((x[0], v, v, x), (x, v[:7], v, x), (x, v, v.double(), x), (x, v, v, x[:3]), (x, v, v, x, st[:3]), (x, v, v, x, st.t().contiguous().t())):
+        assert "GPU" not in refused(cv.layer_norm, *a)
+    assert "GPU" in refused(cv.layer_norm_grad, x, x, st, v, x, v, v, ws)
+    for a in ((x[:3], x, st, v, x, v, v), (x, x, st[:2], v, x, v, v), (x, x, st, v, x.bfloat16(), v, v), (x, x, st, v, x, v[:2], v), (x, x, st, v, x, v, v[::2])):
+        assert "GPU" not in refused(cv.layer_norm_grad, *a, ws)
+    z, tid, tv, loss = torch.zeros(4, 30), torch.zeros(4, 5, dtype=torch.int32), torch.zeros(4, 5), torch.zeros(4)
+    assert "GPU" in refused(cv.distill, z, tid, tv, loss, ws, weights=loss, dlogits=z, stats_out=st, status=status)
+    for a, more in (((z[0], tid, tv, loss), {}), ((z, tid[:3], tv, loss), {}), ((z, tid, tv[:, :4], loss), {}), ((z, tid, tv, loss[:3]), {}),
+                    ((z, tid.short(), tv, loss), {}), ((z, tid, tv.double(), loss), {}), ((z, tid, tv, loss), dict(dlogits=z.half())),
+                    ((z, tid, tv, loss), dict(weights=loss[:2])), ((z, tid, tv, loss), dict(stats_out=loss)), ((z, tid, tv, loss), dict(dlogits=z[:, :29]))):
+        assert "GPU" not in refused(cv.distill, *a, ws, **more)
+    assert "GPU" in refused(cv.distill_grad, z, tid, tv, st, z)
+    for a in ((z, tid, tv, st[:3], z), (z, tid, tv, st, z.half()), (z, tid, tv, st, z[:2])):
+        assert "GPU" not in refused(cv.distill_grad, *a)
+
+
+def test_workspaces_never_shrink():
+    """A workspace for larger sizes serves smaller ones."""
+    rng = np.random.default_rng(7)
+    for _ in range(300):
+        n, vocab, dim = (int(np.exp(rng.uniform(0, np.log(top)))) for top in (300_000, 3_000_000, 20_000))
+        base = cv.embed_grad_workspace_bytes(n, vocab, dim)
+        assert base > 0 and base <= cv.embed_grad_workspace_bytes(n + 1, vocab, dim) and base <= cv.embed_grad_workspace_bytes(n, vocab, dim + 1)
+        assert base <= cv.embed_grad_workspace_bytes(n, vocab + 1, dim)
+        assert cv.layer_norm_grad_workspace_bytes(n, dim) <= cv.layer_norm_grad_workspace_bytes(n + 1, dim)
+        assert cv.layer_norm_grad_workspace_bytes(n, dim) <= cv.layer_norm_grad_workspace_bytes(n, dim + 1)
+        assert cv.distill_workspace_bytes(n, vocab) <= cv.distill_workspace_bytes(n + 1, vocab)
