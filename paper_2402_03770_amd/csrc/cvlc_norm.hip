@@ -1,10 +1,17 @@
 // cvlc_norm.hip -- layer norm of rows and its backward pass.
 //
-// Forward, a workgroup per row: the mean, then the mean square of what is left
-// of it (not the difference of two large sums), then the row again for y.
-// Backward, a workgroup per row for dx: two sums, of g and of g * h, then the
-// row again.  dgamma and dbeta are sums over all rows: workgroups take blocks of
-// rows and leave partial sums, a second launch adds the blocks up in order.
+// Forward: the mean, then the mean square of what is left of it (not the
+// difference of two large sums), then y.  Backward: two sums, of g and of g * h,
+// then dx.  dgamma and dbeta are sums over all rows: every workgroup keeps its
+// share while it goes over its rows and leaves it as partial sums, a second
+// launch adds those up in order.  All of it is bound by HBM: the arithmetic is
+// a fifth of the time that the bytes take, as long as the next row is on its way
+// while one is worked on.
+//
+// Rows of up to 16384 elements lie in registers between the sums and the output
+// (norm_rows, norm_grad_rows): one read, one write.  Longer rows, and rows
+// shorter than one access, are read again for every step (norm, norm_dx,
+// norm_columns).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -28,18 +35,17 @@ struct NormArgs {
 template <class TX, class TY>
 __global__ __launch_bounds__(kNormBlock) void norm_kernel(NormArgs a, const TX* x, TY* y) {
   constexpr uint32_t N = kPerAccess<TX, TY>;
-  __shared__ float scratch[2 * kNormWaves];
+  __shared__ float scratch[kNormWaves];
   for (uint32_t row = blockIdx.x; row < a.n; row += gridDim.x) {
     const TX* xr = x + row * a.x_stride;
-    float sum = 0.0f, unused = 0.0f;
+    float sum = 0.0f;
     for (uint32_t at = threadIdx.x * N; at < a.dim; at += kNormBlock * N) {
       float v[N];
       load_row<N>(xr, at, a.dim, 0.0f, v);
 #pragma unroll
       for (uint32_t i = 0; i < N; ++i) sum += v[i];
     }
-    block_sum2<kNormWaves>(sum, unused, scratch);
-    const float mean = sum / (float)a.dim;
+    const float mean = block_sum<kNormWaves>(sum, scratch) / (float)a.dim;
     float sq = 0.0f;
     for (uint32_t at = threadIdx.x * N; at < a.dim; at += kNormBlock * N) {
       float v[N];
@@ -47,8 +53,7 @@ __global__ __launch_bounds__(kNormBlock) void norm_kernel(NormArgs a, const TX* 
 #pragma unroll
       for (uint32_t i = 0; i < N; ++i) sq = fmaf(v[i] - mean, v[i] - mean, sq);
     }
-    block_sum2<kNormWaves>(sq, unused, scratch);
-    const float r = 1.0f / sqrtf(sq / (float)a.dim + a.eps);
+    const float r = 1.0f / sqrtf(block_sum<kNormWaves>(sq, scratch) / (float)a.dim + a.eps);
     if (a.stats && threadIdx.x == 0) {
       a.stats[2 * (uint64_t)row] = mean;
       a.stats[2 * (uint64_t)row + 1] = r;
@@ -122,6 +127,262 @@ __global__ __launch_bounds__(kNormBlock) void norm_columns_kernel(NormArgs a, co
   }
 }
 
+// ----------------------------------------------------------------------------- rows in registers
+// W wavefronts to a row, V accesses per thread, O wavefronts on a SIMD at a time.  Workgroups (of four rows where a row is
+// one wavefront's) stay and go from row to row, so that gamma and beta are read once, and ask for the next row before
+// they work on this one.  The grid is what the device holds at once: with more workgroups than that the last ones run
+// after the others (three of eight wavefronts on a CU that held two: 215 us for 180).
+template <uint32_t W_, uint32_t V_, uint32_t O_, bool LDS_ = false>
+struct RowShape {
+  static constexpr uint32_t W = W_, V = V_, O = O_;
+  static constexpr bool LDS = LDS_;  // the sums over the rows are kept in LDS
+  static constexpr uint32_t kRows = W == 1 ? 4 : 1, kWaves = W * kRows, kThreads = kWaves * kWave;
+  static constexpr uint32_t kPerCu = 4 * O > kWaves ? 4 * O / kWaves : 1;
+};
+
+// A thread's part of a row; what is not its own stays zero bits.
+template <class T, uint32_t N, class S, bool ONCE>
+struct RawRow {
+  Raw<T, N> v[S::V];
+  __device__ __forceinline__ RawRow() {
+#pragma unroll
+    for (uint32_t j = 0; j < S::V; ++j)
+#pragma unroll
+      for (uint32_t i = 0; i < Raw<T, N>::kWords; ++i) v[j].w[i] = 0;
+  }
+  __device__ __forceinline__ void load(const T* row, const Place<N> (&place)[S::V]) {
+#pragma unroll
+    for (uint32_t j = 0; j < S::V; ++j)
+      if (place[j].any()) v[j].template load<ONCE>(row + place[j].at);
+  }
+};
+
+template <class TX, class TY, class S, bool ONCE>
+__global__ __launch_bounds__(S::kThreads, S::O) void norm_rows_kernel(NormArgs a, const TX* x, TY* y) {
+  constexpr uint32_t N = kPerAccess<TX, TY>, L = S::W * kWave, V = S::V;
+  __shared__ float scratch[2 * S::W];
+  const uint32_t lane = threadIdx.x % L, step = gridDim.x * S::kRows;
+  float g[V][N], b[V][N];
+  Place<N> place[V];
+#pragma unroll
+  for (uint32_t j = 0; j < V; ++j) {
+    place[j] = Place<N>((j * L + lane) * N, a.dim);
+#pragma unroll
+    for (uint32_t i = 0; i < N; ++i) {
+      g[j][i] = 1.0f;
+      b[j][i] = 0.0f;
+    }
+    if (a.gamma) load_values<N>(a.gamma + place[j].at, g[j]);
+    if (a.beta) load_values<N>(a.beta + place[j].at, b[j]);
+  }
+  const float dim = (float)a.dim;
+  uint32_t row = blockIdx.x * S::kRows + threadIdx.x / L;
+  RawRow<TX, N, S, ONCE> raw;
+  if (row < a.n) raw.load(x + row * a.x_stride, place);
+  for (; row < a.n; row += step) {
+    float v[V][N], sum = 0.0f, sq = 0.0f;
+#pragma unroll
+    for (uint32_t j = 0; j < V; ++j) {
+      raw.v[j].values(v[j]);
+      place[j].mask(v[j], 0.0f);
+#pragma unroll
+      for (uint32_t i = 0; i < N; ++i) sum += v[j][i];
+    }
+    if (row + step < a.n) raw.load(x + (row + step) * a.x_stride, place);
+    const float mean = block_sum<S::W>(sum, scratch) / dim;
+#pragma unroll
+    for (uint32_t j = 0; j < V; ++j) {
+#pragma unroll
+      for (uint32_t i = 0; i < N; ++i) v[j][i] -= mean;
+      place[j].mask(v[j], 0.0f);
+#pragma unroll
+      for (uint32_t i = 0; i < N; ++i) sq = fmaf(v[j][i], v[j][i], sq);
+    }
+    const float r = 1.0f / sqrtf(block_sum<S::W>(sq, scratch) / dim + a.eps);
+    if (a.stats && lane == 0) {
+      a.stats[2 * (uint64_t)row] = mean;
+      a.stats[2 * (uint64_t)row + 1] = r;
+    }
+#pragma unroll
+    for (uint32_t j = 0; j < V; ++j) {
+#pragma unroll
+      for (uint32_t i = 0; i < N; ++i) v[j][i] = fmaf(v[j][i] * r, g[j][i], b[j][i]);
+      place[j].template store<ONCE>(y + row * a.y_stride, v[j]);
+    }
+  }
+}
+
+// The backward pass of rows, and the thread's share of the sums over the rows.
+template <class TX, class TY, class S, bool ONCE>
+__global__ __launch_bounds__(S::kThreads, S::O) void norm_grad_rows_kernel(NormArgs a, const TX* x, const TY* dy, TX* dx, float* part) {
+  constexpr uint32_t N = kPerAccess<TX, TY>, L = S::W * kWave, V = S::V;
+  __shared__ float scratch[2 * S::W];
+  const uint32_t lane = threadIdx.x % L, step = gridDim.x * S::kRows;
+  // the sums over the rows: in registers, or in LDS where a thread has too many columns for that
+  constexpr uint32_t R = S::LDS ? 1 : V;
+  float g[R][N], dg[R][N], db[R][N];
+  extern __shared__ float4 sums[];  // [2][V * N / 4][L]
+  auto sum_at = [&](uint32_t which, uint32_t j, uint32_t q) -> float4& { return sums[((which * V + j) * (N / 4) + q) * L + lane]; };
+  Place<N> place[V];
+#pragma unroll
+  for (uint32_t j = 0; j < V; ++j) {
+    place[j] = Place<N>((j * L + lane) * N, a.dim);
+    if constexpr (S::LDS) {
+#pragma unroll
+      for (uint32_t q = 0; q < N / 4; ++q) sum_at(0, j, q) = sum_at(1, j, q) = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    } else {
+#pragma unroll
+      for (uint32_t i = 0; i < N; ++i) {
+        g[j][i] = 1.0f;
+        dg[j][i] = db[j][i] = 0.0f;
+      }
+      if (a.gamma) load_values<N>(a.gamma + place[j].at, g[j]);
+    }
+  }
+  const float dim = (float)a.dim;
+  uint32_t row = blockIdx.x * S::kRows + threadIdx.x / L;
+  RawRow<TX, N, S, ONCE> rx;
+  RawRow<TY, N, S, ONCE> ry;
+  float mean = 0.0f, r = 0.0f;
+  auto ask = [&](uint32_t at) {
+    rx.load(x + at * a.x_stride, place);
+    ry.load(dy + at * a.y_stride, place);
+    mean = a.stats[2 * (uint64_t)at];
+    r = a.stats[2 * (uint64_t)at + 1];
+  };
+  if (row < a.n) ask(row);
+  for (; row < a.n; row += step) {
+    float h[V][N], t[V][N], sg = 0.0f, sgh = 0.0f;
+    const float r_now = r;
+#pragma unroll
+    for (uint32_t j = 0; j < V; ++j) {
+      rx.v[j].values(h[j]);
+      ry.v[j].values(t[j]);
+      place[j].mask(h[j], mean);  // what is not the thread's adds nothing
+      place[j].mask(t[j], 0.0f);
+      float gj[N];
+      if constexpr (S::LDS) {
+#pragma unroll
+        for (uint32_t i = 0; i < N; ++i) gj[i] = 1.0f;
+        if (a.gamma) load_values<N>(a.gamma + place[j].at, gj);
+      }
+#pragma unroll
+      for (uint32_t i = 0; i < N; ++i) h[j][i] = (h[j][i] - mean) * r_now;
+      if constexpr (S::LDS) {
+#pragma unroll
+        for (uint32_t q = 0; q < N / 4; ++q) {
+          float4 &sdg = sum_at(0, j, q), &sdb = sum_at(1, j, q);
+          float* tq = t[j] + 4 * q;
+          const float* hq = h[j] + 4 * q;
+          sdg = make_float4(fmaf(tq[0], hq[0], sdg.x), fmaf(tq[1], hq[1], sdg.y), fmaf(tq[2], hq[2], sdg.z), fmaf(tq[3], hq[3], sdg.w));
+          sdb = make_float4(sdb.x + tq[0], sdb.y + tq[1], sdb.z + tq[2], sdb.w + tq[3]);
+        }
+      } else {
+#pragma unroll
+        for (uint32_t i = 0; i < N; ++i) {
+          dg[j][i] = fmaf(t[j][i], h[j][i], dg[j][i]);
+          db[j][i] += t[j][i];
+        }
+      }
+#pragma unroll
+      for (uint32_t i = 0; i < N; ++i) {
+        t[j][i] *= S::LDS ? gj[i] : g[S::LDS ? 0 : j][i];
+        sg += t[j][i];
+        sgh = fmaf(t[j][i], h[j][i], sgh);
+      }
+    }
+    if (row + step < a.n) ask(row + step);
+    if (!dx) continue;
+    block_sum2<S::W>(sg, sgh, scratch);
+    sg /= dim;
+    sgh /= dim;
+#pragma unroll
+    for (uint32_t j = 0; j < V; ++j) {
+#pragma unroll
+      for (uint32_t i = 0; i < N; ++i) t[j][i] = r_now * (t[j][i] - sg - h[j][i] * sgh);
+      place[j].template store<ONCE>(dx + row * a.dx_stride, t[j]);
+    }
+  }
+  if (!part) return;
+  float* to = part + 2 * (uint64_t)blockIdx.x * a.dim;
+  if constexpr (S::kRows > 1) {  // the workgroup's rows in turn
+    for (uint32_t turn = 0; turn < S::kRows; ++turn) {
+      if (threadIdx.x / L == turn)
+#pragma unroll
+        for (uint32_t j = 0; j < V; ++j)
+#pragma unroll
+          for (uint32_t q = 0; q < N / 4; ++q) {
+            float4 &sdg = sum_at(0, j, q), &sdb = sum_at(1, j, q);
+            float *dgq = dg[j] + 4 * q, *dbq = db[j] + 4 * q;
+            if (turn) {
+              dgq[0] += sdg.x, dgq[1] += sdg.y, dgq[2] += sdg.z, dgq[3] += sdg.w;
+              dbq[0] += sdb.x, dbq[1] += sdb.y, dbq[2] += sdb.z, dbq[3] += sdb.w;
+            }
+            sdg = make_float4(dgq[0], dgq[1], dgq[2], dgq[3]);
+            sdb = make_float4(dbq[0], dbq[1], dbq[2], dbq[3]);
+          }
+      __syncthreads();
+    }
+    if (threadIdx.x / L != S::kRows - 1) return;
+  }
+#pragma unroll
+  for (uint32_t j = 0; j < V; ++j) {
+    if constexpr (S::LDS) {
+      float all[2][N];
+#pragma unroll
+      for (uint32_t q = 0; q < N / 4; ++q)
+#pragma unroll
+        for (uint32_t k = 0; k < 2; ++k) {
+          const float4 s = sum_at(k, j, q);
+          float* to_q = all[k] + 4 * q;
+          to_q[0] = s.x, to_q[1] = s.y, to_q[2] = s.z, to_q[3] = s.w;
+        }
+      place[j].template store<false>(to, all[0]);
+      place[j].template store<false>(to + a.dim, all[1]);
+    } else {
+      place[j].template store<false>(to, dg[j]);
+      place[j].template store<false>(to + a.dim, db[j]);
+    }
+  }
+}
+
+// Few wavefronts with many bytes under way each do best: rows of one wavefront need no barrier (65536 x 4096 bf16: a
+// wavefront with eight accesses per thread 183 us, four with two 201, eight with one 220).  With few rows that leaves
+// CUs empty, so up to 8191 rows long ones are spread over more wavefronts (200 x 4096: 4.0 us, 7.0 by one; 4096 x 4096:
+// 14.0 and 17.3; 16384 x 4096 49 by one, 52).
+// Calls f with the shape for rows of `dim` elements, `per` of them an access; false: too long for registers, or shorter than
+// an access.
+template <class F>
+bool by_norm_shape(uint32_t n, uint32_t dim, uint32_t per, F f) {
+  const uint32_t vectors = (dim + per - 1) / per;
+  if (dim < per) return false;
+  const bool many = n >= 8192;
+  if (vectors <= 64) return f(RowShape<1, 1, 8>{});
+  if (vectors <= 128) return f(RowShape<1, 2, 2>{});
+  if (vectors <= 256) return many ? f(RowShape<1, 4, 2>{}) : f(RowShape<2, 2, 4>{});
+  if (vectors <= 512) return many ? f(RowShape<1, 8, 1>{}) : f(RowShape<4, 2, 6>{});
+  if (vectors <= 1024) return f(RowShape<8, 2, 4>{});
+  if (vectors <= 2048) return f(RowShape<8, 4, 2>{});
+  if (vectors <= 4096 && per == 4) return f(RowShape<16, 4, 4>{});
+  return false;
+}
+// Backward a thread holds five values per column (gamma, two sums, h, g), so one access per thread as far as a workgroup
+// goes.  Beyond 8192 fp32 (1024 threads with 16 columns each) the sums over the rows lie in LDS (8192 x 16384 fp32: 280 us,
+// 437 with them in registers that spill).
+template <class F>
+bool by_norm_grad_shape(uint32_t dim, uint32_t per, F f) {
+  const uint32_t vectors = (dim + per - 1) / per;
+  if (dim < per) return false;
+  if (vectors <= 64) return f(RowShape<1, 1, 6>{});
+  if (vectors <= 128) return f(RowShape<2, 1, 4>{});
+  if (vectors <= 256) return f(RowShape<4, 1, 4>{});
+  if (vectors <= 512) return f(RowShape<8, 1, 4>{});
+  if (vectors <= 1024) return f(RowShape<16, 1, 4>{});
+  if (vectors <= 2048) return f(RowShape<16, 2, 4>{});
+  if (vectors <= 4096 && per == 4) return f(RowShape<16, 4, 4, true>{});
+  return false;
+}
+
 // Adds the blocks up: 64 columns a workgroup, a sixteenth of the blocks a wavefront.
 constexpr uint32_t kJoinWaves = 16;
 __global__ __launch_bounds__(kJoinWaves * kWave) void norm_join_kernel(const float* part, uint32_t blocks, uint32_t dim,
@@ -146,9 +407,15 @@ __global__ __launch_bounds__(kJoinWaves * kWave) void norm_join_kernel(const flo
   }
 }
 
-constexpr uint32_t kRowBlocks = 256;  // blocks of rows for the column sums, at most
+constexpr uint32_t kRowBlocks = 2048;  // workgroups that leave partial sums, at most ...
+constexpr uint32_t kRowsEach = 8;      // ... and rows that each goes over, at least, beyond 256 workgroups
+uint32_t partials(uint32_t n) { return std::min(kRowBlocks, std::max(std::min(n, 256u), n / kRowsEach)); }
 
-uint32_t rows_per_block(uint32_t n) { return std::max(1u, (n + kRowBlocks - 1) / kRowBlocks); }
+// Data that the last-level cache (256 MB) does not hold anyway are read and written past the caches' order (65536 x 4096
+// bf16: 198 -> 183 us; 2007 x 1003 fp32, which it does hold, 14.5 -> 16.5).
+bool once(uint32_t n, uint32_t dim, uint32_t bytes) { return (uint64_t)n * dim * bytes > 256ull * 1000000; }
+
+uint32_t rows_per_block(uint32_t n) { return std::max(1u, (n + 255u) / 256u); }
 
 int launched() { return hip_check(hipGetLastError()); }
 
@@ -171,9 +438,18 @@ int cvlc_layer_norm(uint32_t n, uint32_t dim, const void* d_x, uint32_t x_type, 
   if (!buffer_ok(d_x, type_bytes(x_type)) || !buffer_ok(d_y, type_bytes(y_type))) return CVLC_ERR_ARG;
   if (d_x == d_y && (x_type != y_type || x_stride != y_stride)) return CVLC_ERR_ARG;
   const NormArgs a{n, dim, x_stride, y_stride, 0, d_gamma, d_beta, eps, d_stats};
+  const bool past = once(n, dim, type_bytes(x_type) + type_bytes(y_type));
   by_types(x_type, y_type, [&](auto tx, auto ty) {
     using TX = decltype(tx);
     using TY = decltype(ty);
+    if (by_norm_shape(n, dim, kPerAccess<TX, TY>, [&](auto shape) {
+          using S = decltype(shape);
+          hipLaunchKernelGGL((past ? norm_rows_kernel<TX, TY, S, true> : norm_rows_kernel<TX, TY, S, false>),
+                             dim3(std::min((n + S::kRows - 1) / S::kRows, 256u * S::kPerCu)), dim3(S::kThreads), 0,
+                             static_cast<hipStream_t>(hip_stream), a, static_cast<const TX*>(d_x), static_cast<TY*>(d_y));
+          return true;
+        }))
+      return;
     hipLaunchKernelGGL((norm_kernel<TX, TY>), dim3(std::min(n, 1u << 20)), dim3(kNormBlock), 0, static_cast<hipStream_t>(hip_stream),
                        a, static_cast<const TX*>(d_x), static_cast<TY*>(d_y));
   });
@@ -181,7 +457,7 @@ int cvlc_layer_norm(uint32_t n, uint32_t dim, const void* d_x, uint32_t x_type, 
 }
 
 size_t cvlc_layer_norm_grad_workspace_bytes(uint32_t n, uint32_t dim) {
-  const uint64_t blocks = std::min(n, cvlc::kRowBlocks);
+  const uint64_t blocks = cvlc::partials(n);
   return 256u + (size_t)(blocks * 2u * dim * sizeof(float));
 }
 
@@ -210,14 +486,26 @@ int cvlc_layer_norm_grad(uint32_t n, uint32_t dim, const void* d_dy, uint32_t dy
   if (ws_bytes < cvlc_layer_norm_grad_workspace_bytes(n, dim)) return CVLC_ERR_CAPACITY;
   hipStream_t stream = static_cast<hipStream_t>(hip_stream);
   const NormArgs a{n, dim, x_stride, dy_stride, dx_stride, d_gamma, nullptr, 0.0f, const_cast<float*>(d_stats)};
+  const bool past = once(n, dim, (d_dx ? 2u : 1u) * type_bytes(x_type) + type_bytes(dy_type));
   float* part = static_cast<float*>(d_workspace);
-  const uint32_t block_rows = rows_per_block(n), blocks = (n + block_rows - 1) / block_rows;
+  const uint32_t block_rows = rows_per_block(n);
+  uint32_t blocks = (n + block_rows - 1) / block_rows;
   if (n)
     by_types(x_type, dy_type, [&](auto tx, auto ty) {
       using TX = decltype(tx);
       using TY = decltype(ty);
       const TX* x = static_cast<const TX*>(d_x);
       const TY* dy = static_cast<const TY*>(d_dy);
+      if (by_norm_grad_shape(dim, kPerAccess<TX, TY>, [&](auto shape) {
+            using S = decltype(shape);
+            blocks = std::min({(n + S::kRows - 1) / S::kRows, 256u * S::kPerCu, partials(n)});
+            constexpr uint32_t lds = S::LDS || S::kRows > 1 ? 2 * S::V * kPerAccess<TX, TY> * S::W * kWave * sizeof(float) : 0;
+            hipLaunchKernelGGL((past ? norm_grad_rows_kernel<TX, TY, S, true> : norm_grad_rows_kernel<TX, TY, S, false>), dim3(blocks),
+                               dim3(S::kThreads), lds, stream, a, x, dy,
+                               static_cast<TX*>(d_dx), d_dgamma || d_dbeta ? part : nullptr);
+            return true;
+          }))
+        return;
       // the sums over the rows come first: dx may lie where dy or x does
       if (d_dgamma || d_dbeta)
         hipLaunchKernelGGL((norm_columns_kernel<TX, TY>), dim3(std::min((dim + kNormBlock - 1) / kNormBlock, 65536u), blocks),

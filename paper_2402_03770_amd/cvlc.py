@@ -363,6 +363,8 @@ def fit_alpha(updates: Sequence[torch.Tensor], alpha_out: torch.Tensor, workspac
 # ----------------------------------------------------------------------------- the local step of a language-model client
 # Tensors are checked against each other here, since the library sees addresses only; nothing is copied, cast or
 # allocated, so a tensor that does not fit is refused.
+# The handle without a Stream object around it, where torch has that: 2.8 us less a call.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda device: torch.cuda.current_stream(device).cuda_stream)
 _TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 _ID_BYTES = {torch.int32: 4, torch.int64: 8}
 
@@ -402,12 +404,13 @@ def _id_bytes(what: str, name: str, ids: torch.Tensor, dims: int) -> int:
     return size
 
 
-def _on_device(what: str, *tensors: Optional[torch.Tensor]) -> None:
-    """All tensors lie on the current device, the one that the call's stream belongs to."""
+def _stream_of(what: str, *tensors: Optional[torch.Tensor]) -> int:
+    """The current stream, of the device that all tensors have to lie on."""
     here = torch.cuda.current_device() if tensors[0].is_cuda else -1
     for t in tensors:
         if t is not None and (here < 0 or t.get_device() != here):
             _refuse(what, f"a tensor is on {t.device}, not on the current GPU")
+    return _raw_stream(here)
 
 
 def _status(what: str, status: Optional[torch.Tensor]):
@@ -443,8 +446,8 @@ def embed(ids: torch.Tensor, table: torch.Tensor, out: torch.Tensor, scale: floa
     tp, tt, ts = _matrix(what, "table", table, vocab, dim)
     op, ot, os_ = _matrix(what, "out", out, n, dim)
     st = _status(what, status)
-    _on_device(what, ids, table, out, status)
-    _check(lib().cvlc_embed(n, ids.data_ptr(), size, tp, tt, ts, vocab, dim, scale, op, ot, os_, st, _stream_handle()), what)
+    stream = _stream_of(what, ids, table, out, status)
+    _check(lib().cvlc_embed(n, ids.data_ptr(), size, tp, tt, ts, vocab, dim, scale, op, ot, os_, st, stream), what)
 
 
 def embed_grad(ids: torch.Tensor, dout: torch.Tensor, dtable: torch.Tensor, workspace: torch.Tensor, scale: float = 1.0,
@@ -459,10 +462,10 @@ def embed_grad(ids: torch.Tensor, dout: torch.Tensor, dtable: torch.Tensor, work
     vocab, dim = dtable.shape
     dp, dt, ds = _matrix(what, "dout", dout, n, dim)
     tp, _, ts = _matrix(what, "dtable", dtable, vocab, dim)
-    _on_device(what, ids, dout, dtable, workspace)
+    stream = _stream_of(what, ids, dout, dtable, workspace)
     _check(lib().cvlc_embed_grad(n, ids.data_ptr(), size, dp, dt, ds, vocab, dim, scale, tp, ts,
                                  GRAD_ACCUMULATE if accumulate else 0, workspace.data_ptr(), workspace.numel(),
-                                 _stream_handle()), what)
+                                 stream), what)
 
 
 def layer_norm(x: torch.Tensor, gamma: Optional[torch.Tensor], beta: Optional[torch.Tensor], y: torch.Tensor,
@@ -478,8 +481,8 @@ def layer_norm(x: torch.Tensor, gamma: Optional[torch.Tensor], beta: Optional[to
     yp, yt, ys = _matrix(what, "y", y, n, dim)
     gp, bp = _vector(what, "gamma", gamma, (dim,)), _vector(what, "beta", beta, (dim,))
     sp = _vector(what, "stats_out", stats_out, (n, 2))
-    _on_device(what, x, y, gamma, beta, stats_out)
-    _check(lib().cvlc_layer_norm(n, dim, xp, xt, xs, gp, bp, eps, yp, yt, ys, sp, _stream_handle()), what)
+    stream = _stream_of(what, x, y, gamma, beta, stats_out)
+    _check(lib().cvlc_layer_norm(n, dim, xp, xt, xs, gp, bp, eps, yp, yt, ys, sp, stream), what)
 
 
 def layer_norm_grad(dy: torch.Tensor, x: torch.Tensor, stats: torch.Tensor, gamma: Optional[torch.Tensor],
@@ -500,10 +503,10 @@ def layer_norm_grad(dy: torch.Tensor, x: torch.Tensor, stats: torch.Tensor, gamm
             _refuse(what, "dx is not of x's type")
     sp, gp = _vector(what, "stats", stats, (n, 2)), _vector(what, "gamma", gamma, (dim,))
     dgp, dbp = _vector(what, "dgamma", dgamma, (dim,)), _vector(what, "dbeta", dbeta, (dim,))
-    _on_device(what, x, dy, stats, gamma, dx, dgamma, dbeta, workspace)
+    stream = _stream_of(what, x, dy, stats, gamma, dx, dgamma, dbeta, workspace)
     _check(lib().cvlc_layer_norm_grad(n, dim, yp, yt, ys, xp, xt, xs, sp, gp, dp, ds, dgp, dbp,
                                       GRAD_ACCUMULATE if accumulate else 0, workspace.data_ptr(), workspace.numel(),
-                                      _stream_handle()), what)
+                                      stream), what)
 
 
 def _lists(what: str, logits: torch.Tensor, teacher_ids: torch.Tensor, teacher_values: torch.Tensor):
@@ -539,10 +542,10 @@ def distill(logits: torch.Tensor, teacher_ids: torch.Tensor, teacher_values: tor
             _refuse(what, "dlogits are not of the logits' type")
     wp, lp = _vector(what, "weights", weights, (n,)), _vector(what, "loss_out", loss_out, (n,))
     sp, st = _vector(what, "stats_out", stats_out, (n, 2)), _status(what, status)
-    _on_device(what, logits, teacher_ids, teacher_values, loss_out, workspace, weights, dlogits, stats_out, status)
+    stream = _stream_of(what, logits, teacher_ids, teacher_values, loss_out, workspace, weights, dlogits, stats_out, status)
     _check(lib().cvlc_distill(n, vocab, zp, zt, zs, k, teacher_ids.data_ptr(), size, teacher_values.data_ptr(), kind,
                               temperature, DISTILL_LOGPROBS if logprobs else 0, wp, lp, sp, dp, ds,
-                              workspace.data_ptr(), workspace.numel(), st, _stream_handle()), what)
+                              workspace.data_ptr(), workspace.numel(), st, stream), what)
 
 
 def distill_grad(logits: torch.Tensor, teacher_ids: torch.Tensor, teacher_values: torch.Tensor, stats: torch.Tensor,
@@ -556,10 +559,10 @@ def distill_grad(logits: torch.Tensor, teacher_ids: torch.Tensor, teacher_values
     if dt != zt:
         _refuse(what, "dlogits are not of the logits' type")
     wp, sp, st = _vector(what, "weights", weights, (n,)), _vector(what, "stats", stats, (n, 2)), _status(what, status)
-    _on_device(what, logits, teacher_ids, teacher_values, stats, dlogits, weights, status)
+    stream = _stream_of(what, logits, teacher_ids, teacher_values, stats, dlogits, weights, status)
     _check(lib().cvlc_distill_grad(n, vocab, zp, zt, zs, k, teacher_ids.data_ptr(), size, teacher_values.data_ptr(),
                                    kind, temperature, DISTILL_LOGPROBS if logprobs else 0, wp, sp, dp, ds, st,
-                                   _stream_handle()), what)
+                                   stream), what)
 
 
 def device_status(workspace: torch.Tensor) -> int:

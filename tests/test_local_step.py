@@ -267,6 +267,44 @@ def test_layer_norm_grad(types, n, dim):
 
 
 @gpu
+@pytest.mark.parametrize("types", [(F32, F32), (BF16, BF16), (F32, F16)])
+@pytest.mark.parametrize("n,dim", [(8300, 60), (2100, 700), (8200, 1100), (8200, 2050), (1100, 2050), (700, 4101), (300, 9001), (300, 16384)])
+def test_layer_norm_of_more_rows_than_go_at_once(types, n, dim):
+    """Workgroups that go from row to row, forward and backward."""
+    tx, ty = types
+    x = random_matrix(n, dim, tx, 35, scale=2.0, shift=1.0)
+    gamma, beta = (random_matrix(1, dim, F32, s)[0].contiguous() for s in (36, 37))
+    y, stats = torch.empty(n, dim, dtype=ty, device=DEV), torch.empty(n, 2, device=DEV)
+    cv.layer_norm(x, gamma, beta, y, stats)
+    want, tol, s, s_tol = ref.layer_norm(f64(x), f64(gamma), f64(beta), 1e-5)
+    assert_near(stats, s, s_tol)
+    assert_near(y, want, tol, ty)
+    check_norm_grad(n, dim, tx, ty, seed=38)
+
+
+@gpu
+@pytest.mark.parametrize("n,dim,dtype", [(70_000, 1000, BF16), (9000, 4096, F32)])
+def test_layer_norm_of_more_than_the_caches_hold(n, dim, dtype):
+    """Large calls go past the caches' order: sampled rows, and the sums over all of them."""
+    g = torch.Generator(device=DEV).manual_seed(39)
+    x, dy = (torch.randn(n, dim, generator=g, device=DEV).to(dtype) for _ in range(2))
+    y, dx, stats, sums = torch.empty_like(x), torch.empty_like(x), torch.empty(n, 2, device=DEV), torch.empty(2, dim, device=DEV)
+    cv.layer_norm(x, None, None, y, stats)
+    cv.layer_norm_grad(dy, x, stats, None, dx, sums[0], sums[1], cv.new_workspace(cv.layer_norm_grad_workspace_bytes(n, dim), DEV))
+    some = torch.arange(0, n, 331, device=DEV)
+    want, tol, s, s_tol = ref.layer_norm(f64(x[some]), None, None, 1e-5)
+    assert_near(stats[some], s, s_tol)
+    assert_near(y[some], want, tol, dtype)
+    assert_near(dx[some], *ref.layer_norm_grad(f64(dy[some]), f64(x[some]), f64(stats[some]), None)[:2], dtype)
+    total, size = torch.zeros(2, dim, dtype=torch.float64, device=DEV), torch.zeros(2, dim, dtype=torch.float64, device=DEV)
+    for b in range(0, n, 4096):
+        d, h = dy[b:b + 4096].double(), (x[b:b + 4096].double() - stats[b:b + 4096, :1].double()) * stats[b:b + 4096, 1:].double()
+        total += torch.stack([(d * h).sum(0), d.sum(0)])
+        size += torch.stack([(d * h).abs().sum(0), d.abs().sum(0)])
+    assert_near(sums, f64(total), (ref.depth(n) + 6) * ref.U * f64(size))
+
+
+@gpu
 @pytest.mark.parametrize("n,dim", [(0, 40), (40, 200), (2, 20000)])
 def test_layer_norm_grad_parts_and_sums(n, dim):
     for parts in (("dx",), ("dgamma",), ("dbeta",), ("dx", "dbeta"), ("dgamma", "dbeta")):
