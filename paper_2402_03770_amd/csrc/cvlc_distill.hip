@@ -1,16 +1,24 @@
 // cvlc_distill.hip -- distillation from a teacher's top logits: the loss of every
 // row and the gradient of the student's logits.
 //
-// A workgroup per row.  It first turns the teacher's list into probabilities in
-// LDS (the list is short), then passes over the row with a running maximum m and
-// sum S of exp((z - m) / T), and, where the gradient is wanted, passes over it
-// again and writes w T P q everywhere; the few listed places are then written
-// again with their own gradient, every one by the thread of its entry.
+// A row's logits give a maximum m and a sum S of exp((z - m) / T), kept as a
+// running pair: a value above the maximum scales the sum so far.  Its list gives
+// such a pair too.  Then every place of the gradient is w T P q, and the few
+// listed ones are written again with their own gradient.
 //
-// m starts at the type's lowest finite value, so that a row of masked logits
-// (-inf) ends with S = 0, which stands for q = 0, and a row of logits that are all
-// at the lowest value ends like any other.  Differences to m are taken before
-// they are scaled: a scaled logit may overflow, a difference of exactly 0 may not.
+//   rows     a row in the registers of W wavefronts between the sum and the
+//            gradient: one read, one write.  Workgroups go from row to row, and
+//            every access that has been turned into gradient is loaded again
+//            from the next row at once.
+//   long     rows too long for that, and rows of which only the loss or only the
+//            gradient is wanted: in passes of four accesses per thread.
+//   part_sum, part_finish   few rows: parts of a row per workgroup, their pairs
+//            joined by every workgroup that goes on with a part.
+//
+// Differences to m are taken before they are scaled: a scaled logit may overflow,
+// a difference of exactly 0 may not.  m starts at the type's lowest finite value, so
+// that a row of masked logits (-inf) ends with S = 0, which stands for q = 0, and a
+// row of logits that are all at the lowest value ends like any other.
 #include <hip/hip_runtime.h>
 
 #include <cfloat>
@@ -23,7 +31,6 @@
 namespace cvlc {
 namespace {
 
-constexpr uint32_t kDistillBlock = 256, kDistillWaves = kDistillBlock / kWave;
 constexpr uint32_t kMaxK = CVLC_DISTILL_MAX_K;
 
 struct DistillArgs {
@@ -36,6 +43,10 @@ struct DistillArgs {
   const float* weights;
   float *loss, *stats;  // stats: written by the loss, read by the gradient alone
   uint32_t* status;
+  // few rows: the parts' pairs, [n][parts], and the listed logits, [n][k], read before any gradient may take their place
+  uint32_t parts;
+  float2* pairs;
+  float* logits;
 };
 
 // exp((z - m) / T).  The instruction flushes results below 2^-126, which a sum of at least 1 does not notice.
@@ -47,10 +58,28 @@ __device__ __forceinline__ float exp_scaled(float z, float m, float c, float sca
   return scaled * __builtin_amdgcn_exp2f(fmaf(z - m, c, kLift));
 }
 
+// A maximum and the sum of exponentials relative to it.
 struct MaxSum {
   float m, s;
 };
+constexpr MaxSum kNothing{-FLT_MAX, 0.0f};
 
+template <uint32_t N>
+__device__ __forceinline__ void take(MaxSum& t, const float (&v)[N], float c) {
+  float m = t.m;
+#pragma unroll
+  for (uint32_t i = 0; i < N; ++i) m = fmaxf(m, v[i]);
+  t.s *= exp_part(t.m, m, c);
+  t.m = m;
+#pragma unroll
+  for (uint32_t i = 0; i < N; ++i) t.s += exp_part(v[i], m, c);
+}
+__device__ __forceinline__ MaxSum wave_join(MaxSum t, float c) {
+  const float m = wave_max(t.m);
+  return {m, wave_sum(t.s * exp_part(t.m, m, c))};
+}
+
+// ----------------------------------------------------------------------------- the teacher's list
 __device__ __forceinline__ int64_t load_id(const void* ids, uint32_t id_bytes, uint64_t i) {
   return id_bytes == 8 ? static_cast<const int64_t*>(ids)[i] : static_cast<const int32_t*>(ids)[i];
 }
@@ -59,155 +88,425 @@ __device__ __forceinline__ float load_as_float(const void* p, uint32_t type, uin
   return type == CVLC_BF16 ? (float)static_cast<const bf16_t*>(p)[i] : (float)static_cast<const f16_t*>(p)[i];
 }
 
-// The maximum, ignoring NaN, of one value per thread, and the sum of another, in every thread.
-template <uint32_t NW>
-__device__ __forceinline__ float block_max(float v, float* scratch) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
-  __syncthreads();
-  if (lane_id() == 0) scratch[wave_id()] = v;
-  __syncthreads();
-  v = scratch[0];
-#pragma unroll
-  for (uint32_t w = 1; w < NW; ++w) v = fmaxf(v, scratch[w]);
-  return v;
-}
-
-// The teacher's list of a row, in LDS: entries that are not there have id -1 and p = 0.
-struct List {
-  int32_t id[kMaxK];
-  float p[kMaxK], tlogp[kMaxK], z[kMaxK];  // tlogp: T ln p, which stays finite where ln p does not
-  float scratch[2 * kDistillWaves];
+// An entry of a list: its place in the row (-1: it is not there), its value and the student's logit, as it lies in memory.
+template <class T>
+struct Entry {
+  int32_t id;
+  float t;
+  T z;
 };
-
-// Fills the list but for z; returns P (0: the list is empty).
-__device__ float load_list(const DistillArgs& a, uint32_t row, List& l) {
-  const uint64_t at = (uint64_t)row * a.k;
-  float top = -INFINITY;
-  for (uint32_t j = threadIdx.x; j < a.k; j += kDistillBlock) {
-    const int64_t id = load_id(a.ids, a.id_bytes, at + j);
-    const float t = load_as_float(a.values, a.value_type, at + j);
-    const bool there = id >= 0 && id < (int64_t)a.vocab && t != -INFINITY;
-    if (id >= (int64_t)a.vocab && a.status) atomicOr(a.status, CVLC_DEV_INDEX);
-    l.id[j] = there ? (int32_t)id : -1;
-    l.tlogp[j] = t;
-    if (there) top = fmaxf(top, t);
+// As it lies in memory, to be looked at later.
+struct RawEntry {
+  int64_t id;
+  float t;
+  __device__ __forceinline__ void load(const DistillArgs& a, uint32_t row, uint32_t j) {
+    const uint64_t at = (uint64_t)row * a.k + j;
+    id = load_id(a.ids, a.id_bytes, at);
+    t = load_as_float(a.values, a.value_type, at);
   }
-  top = a.logprobs ? 0.0f : block_max<kDistillWaves>(top, l.scratch);
-  const float c = a.logprobs ? (float)M_LOG2E : a.c;
-  float sum = 0.0f, unused = 0.0f;
-  for (uint32_t j = threadIdx.x; j < a.k; j += kDistillBlock) {
-    l.p[j] = l.id[j] >= 0 ? exp2f((l.tlogp[j] - top) * c) : 0.0f;
-    sum += l.p[j];
+};
+template <class T>
+__device__ __forceinline__ Entry<T> entry_of(const DistillArgs& a, RawEntry r, const T* zr, bool with_logit = true) {
+  const bool inside = r.id >= 0 && r.id < (int64_t)a.vocab;
+  if (r.id >= (int64_t)a.vocab && a.status) atomicOr(a.status, CVLC_DEV_INDEX);
+  Entry<T> e{-1, r.t, (T)0.0f};
+  if (inside && r.t != -INFINITY) {
+    e.id = (int32_t)r.id;
+    if (with_logit) e.z = zr[e.id];
   }
-  block_sum2<kDistillWaves>(sum, unused, l.scratch);
-  if (!a.logprobs && sum != 0.0f) {
-    const float inv = 1.0f / sum, tlog_sum = a.T * logf(sum);
-    for (uint32_t j = threadIdx.x; j < a.k; j += kDistillBlock) {
-      l.p[j] *= inv;
-      l.tlogp[j] = (l.tlogp[j] - top) - tlog_sum;
-    }
-    sum = sum == sum ? 1.0f : sum;
-  } else if (a.logprobs) {
-    for (uint32_t j = threadIdx.x; j < a.k; j += kDistillBlock) l.tlogp[j] *= a.T;
-  }
-  __syncthreads();
-  return sum;
+  return e;
 }
 
-// w T^2 times the sum over the list of p (ln p - ln q), q from the row's m and S.
-__device__ float list_loss(const DistillArgs& a, List& l, float m, float S, float wT) {
-  const float tlog_S = a.T * logf(S);
-  float loss = 0.0f, unused = 0.0f;
-  for (uint32_t j = threadIdx.x; j < a.k; j += kDistillBlock) {
-    if (l.id[j] < 0 || l.p[j] == 0.0f) continue;
-    const float tlogq = S == 0.0f ? -INFINITY : (l.z[j] - m) - tlog_S;
-    loss += wT * l.p[j] * (l.tlogp[j] - tlogq);
+// What a list's pair says: the scale that turns exp((t - m) c) into p, T ln p up to t, and P (0: the list is empty).
+// T ln p and T ln q stay finite where ln p and ln q do not.
+struct ListSums {
+  float m, c, inv, tlog, slope, P;
+  __device__ __forceinline__ ListSums(const DistillArgs& a, MaxSum t) {
+    if (a.logprobs) {
+      m = 0.0f;
+      c = (float)M_LOG2E;
+      inv = 1.0f;
+      tlog = 0.0f;
+      slope = a.T;
+      P = t.s == 0.0f ? 0.0f : t.s * exp2f(t.m * c);
+    } else {
+      m = t.m;
+      c = a.c;
+      inv = 1.0f / t.s;
+      tlog = a.T * logf(t.s);
+      slope = 1.0f;
+      P = t.s == 0.0f ? 0.0f : t.s == t.s ? 1.0f : t.s;
+    }
   }
-  block_sum2<kDistillWaves>(loss, unused, l.scratch);
+  __device__ __forceinline__ float p(float t) const { return exp2f((t - m) * c) * inv; }
+  // p (T ln p - T ln q)
+  __device__ __forceinline__ float loss(float t, float tlogq) const {
+    const float pt = p(t);
+    return pt == 0.0f ? 0.0f : pt * ((t - m) * slope - tlog - tlogq);
+  }
+};
+// c of a list's pair while it is made
+__device__ __forceinline__ float list_c(const DistillArgs& a) { return a.logprobs ? (float)M_LOG2E : a.c; }
+__device__ __forceinline__ void take_entry(MaxSum& t, int32_t id, float value, float c) {
+  if (id < 0) return;
+  const float v[1] = {value};
+  take<1>(t, v, c);
+}
+// T ln q of a logit
+__device__ __forceinline__ float tlogq_of(const DistillArgs& a, float z, MaxSum t) {
+  return t.s == 0.0f ? -INFINITY : (z - t.m) - a.T * logf(t.s);
+}
+
+// Lists in LDS, while a row is worked on: ids and p, for entries that share a place.
+struct ListLds {
+  int32_t* id;
+  float *p, *z;
+  __device__ __forceinline__ ListLds(float* base, uint32_t k) : id(reinterpret_cast<int32_t*>(base)), p(base + k), z(base + 2 * k) {}
+};
+constexpr uint32_t kListWords = 3;
+
+// Entry j's place of a row's gradient.
+template <class T>
+__device__ __forceinline__ void write_listed(const DistillArgs& a, const ListLds& l, uint32_t j, T* drow, MaxSum t, float P, float wT) {
+  const int32_t id = l.id[j];
+  if (id < 0) return;
+  float p = 0.0f;
+  for (uint32_t i = 0; i < a.k; ++i) p += l.id[i] == id ? l.p[i] : 0.0f;
+  const float inv = t.s == 0.0f ? 0.0f : 1.0f / t.s;
+  drow[id] = (T)(wT * (exp_scaled(l.z[j], t.m, a.c, P * inv * kUnlift) - p));
+}
+
+template <uint32_t W>
+__device__ __forceinline__ void group_sync() {
+  if constexpr (W == 1)
+    wave_sync();
+  else
+    __syncthreads();
+}
+
+// ----------------------------------------------------------------------------- rows in registers
+// N elements of a row of `width` >= N from `first` on; see Place, whose values are worked out again where they are needed.
+template <bool ONCE, class T, uint32_t N>
+__device__ __forceinline__ void load_place(Raw<T, N>& raw, const T* row, uint32_t first, uint32_t width) {
+  if (first < width) raw.template load<ONCE>(row + min(first, width - N));
+}
+
+// W wavefronts to a row, V accesses per thread; workgroups of at least four wavefronts, which are then rows of their own.
+template <class T, bool LOSS, bool GRAD, bool ONCE, uint32_t W, uint32_t V, uint32_t O>
+__global__ __launch_bounds__((W == 1 ? 4 : W) * kWave, O) void distill_rows_kernel(DistillArgs a, const T* logits, T* dlogits) {
+  constexpr uint32_t N = kPerAccess<T>, L = W * kWave, ROWS = W == 1 ? 4 : 1;
+  extern __shared__ float lists[];  // [ROWS][2][kListWords][k]
+  __shared__ float4 pairs[2][ROWS][W];
+  __shared__ float losses[2][ROWS][W];
+  const uint32_t lane = threadIdx.x % L, mine = threadIdx.x / L, step = gridDim.x * ROWS, wave = lane / kWave;
+  uint32_t row = blockIdx.x * ROWS + mine, turn = 0;
+  Raw<T, N> raw[V];
+  RawEntry entry{-1, 0.0f};
+#pragma unroll
+  for (uint32_t j = 0; j < V; ++j)
+#pragma unroll
+    for (uint32_t i = 0; i < Raw<T, N>::kWords; ++i) raw[j].w[i] = 0;
+  const bool has_entry = lane < a.k;
+  float w = 0.0f;
+  if (row < a.n) {
+    w = a.weights ? a.weights[row] : 1.0f;
+    if (w != 0.0f) {
+#pragma unroll
+      for (uint32_t j = 0; j < V; ++j) load_place<ONCE>(raw[j], logits + row * a.stride, (j * L + lane) * N, a.vocab);
+      if (has_entry) entry.load(a, row, lane);
+    }
+  }
+  for (; row < a.n; row += step) {
+    const T* zr = logits + row * a.stride;
+    const uint32_t next = row + step;
+    const bool more = next < a.n;
+    const float w_next = !more ? 0.0f : a.weights ? a.weights[next] : 1.0f;
+    const bool load_next = w_next != 0.0f;
+    const T* zn = logits + (uint64_t)(more ? next : row) * a.stride;
+    const ListLds l(lists + (2 * mine + turn) * kListWords * a.k, a.k);
+    MaxSum t = kNothing;
+    float P = 0.0f;
+    if (w != 0.0f) {
+      // the list: every thread its entries
+      Entry<T> e{-1, 0.0f, (T)0.0f};
+      MaxSum q = kNothing;
+      const float lc = list_c(a);
+      if (has_entry) e = entry_of(a, entry, zr);
+      for (uint32_t j = lane + L; j < a.k; j += L) {
+        RawEntry r;
+        r.load(a, row, j);
+        const Entry<T> f = entry_of(a, r, zr);
+        take_entry(q, f.id, f.t, lc);
+        l.id[j] = f.id;
+        l.p[j] = f.t;
+        l.z[j] = (float)f.z;
+      }
+      take_entry(q, e.id, e.t, lc);
+      if (LOSS) {
+#pragma unroll
+        for (uint32_t j = 0; j < V; ++j) {
+          const uint32_t first = (j * L + lane) * N;
+          if (first >= a.vocab) break;
+          float v[N];
+          raw[j].values(v);
+          Place<N>(first, a.vocab).mask(v, -INFINITY);
+          take(t, v, a.c);
+          if (!GRAD && load_next) load_place<ONCE>(raw[j], zn, first, a.vocab);
+        }
+        t = wave_join(t, a.c);
+      }
+      q = wave_join(q, lc);
+      if (has_entry) {
+        l.id[lane] = e.id;
+        l.p[lane] = e.t;
+        l.z[lane] = (float)e.z;
+      }
+      if (W > 1) {
+        if (lane_id() == 0) pairs[turn][mine][wave] = make_float4(t.m, t.s, q.m, q.s);
+        __syncthreads();
+        const float4 x = lane_id() < W ? pairs[turn][mine][lane_id()] : make_float4(-FLT_MAX, 0.0f, -FLT_MAX, 0.0f);
+        if (LOSS) t = wave_join({x.x, x.y}, a.c);
+        q = wave_join({x.z, x.w}, lc);
+      } else {
+        wave_sync();
+      }
+      if (!LOSS) t = {a.stats[2 * (uint64_t)row], a.stats[2 * (uint64_t)row + 1]};
+      const ListSums s(a, q);
+      P = s.P;
+      // p of every entry, and the loss
+      float loss = 0.0f;
+      for (uint32_t j = lane; j < a.k; j += L) {
+        if (l.id[j] < 0) continue;
+        const float value = l.p[j];
+        if (LOSS) loss += w * a.T * s.loss(value, tlogq_of(a, l.z[j], t));
+        l.p[j] = s.p(value);
+      }
+      if (LOSS) {
+        loss = wave_sum(loss);
+        if (W > 1 && lane_id() == 0) losses[turn][mine][wave] = loss;
+        if (W == 1 && lane == 0 && a.loss) a.loss[row] = loss;
+        if (lane == 0 && a.stats) {
+          a.stats[2 * (uint64_t)row] = P == 0.0f ? 0.0f : t.m;
+          a.stats[2 * (uint64_t)row + 1] = P == 0.0f ? 0.0f : t.s;
+        }
+      }
+    } else if (LOSS && lane == 0) {
+      if (a.loss) a.loss[row] = 0.0f;
+      if (a.stats) a.stats[2 * (uint64_t)row] = a.stats[2 * (uint64_t)row + 1] = 0.0f;
+    }
+    if (load_next && has_entry) entry.load(a, next, lane);
+    if (GRAD || w == 0.0f) {
+      T* dr = GRAD ? dlogits + row * a.dstride : nullptr;
+      const float scale = P == 0.0f || t.s == 0.0f ? 0.0f : w * a.T * P * (1.0f / t.s) * kUnlift;
+      const bool nothing = P == 0.0f;
+#pragma unroll
+      for (uint32_t j = 0; j < V; ++j) {
+        const uint32_t first = (j * L + lane) * N;
+        if (first >= a.vocab) break;
+        if constexpr (GRAD) {
+          float v[N];
+          raw[j].values(v);
+#pragma unroll
+          for (uint32_t i = 0; i < N; ++i) v[i] = nothing ? 0.0f : exp_scaled(v[i], t.m, a.c, scale);
+          Place<N>(first, a.vocab).template store<ONCE>(dr, v);
+        }
+        if (load_next) load_place<ONCE>(raw[j], zn, first, a.vocab);
+      }
+    }
+    if (w != 0.0f) {
+      group_sync<W>();  // every place is written, every p known
+      if (LOSS && W > 1 && lane == 0 && a.loss) {
+        float sum = 0.0f;
+#pragma unroll
+        for (uint32_t i = 0; i < W; ++i) sum += losses[turn][mine][i];
+        a.loss[row] = sum;
+      }
+      if (GRAD && P != 0.0f)
+        for (uint32_t j = lane; j < a.k; j += L) write_listed(a, l, j, dlogits + row * a.dstride, t, P, w * a.T);
+      turn ^= 1;  // the other half of LDS: this one may still be read
+    }
+    w = w_next;
+  }
+}
+
+// ----------------------------------------------------------------------------- long rows, parts of rows
+constexpr uint32_t kLongBlock = 512, kLongWaves = kLongBlock / kWave;
+constexpr uint32_t kDeep = 4;  // accesses under way per thread
+
+// f(first, values) over elements [from, to) of a row, four accesses per thread at a time.  Elements beyond `to` read -inf.
+template <bool ONCE, class T, class F>
+__device__ __forceinline__ void over_row(const T* zr, uint32_t from, uint32_t to, F f) {
+  constexpr uint32_t N = kPerAccess<T>;
+  for (uint64_t base = from + threadIdx.x * N; base < to; base += kDeep * kLongBlock * N) {
+    Raw<T, N> raw[kDeep];
+#pragma unroll
+    for (uint32_t u = 0; u < kDeep; ++u) {
+      const uint64_t first = base + u * kLongBlock * N;
+      if (first + N <= to) raw[u].template load<ONCE>(zr + first);
+    }
+#pragma unroll
+    for (uint32_t u = 0; u < kDeep; ++u) {
+      const uint64_t first = base + u * kLongBlock * N;
+      float v[N];
+      if (first + N <= to)
+        raw[u].values(v);
+      else if (first < to)
+        load_some<N>(zr + first, (uint32_t)(to - first), -INFINITY, v);
+      else
+        break;
+      f((uint32_t)first, v);
+    }
+  }
+}
+template <bool ONCE, uint32_t N, class T>
+__device__ __forceinline__ void store_part(T* row, uint32_t first, uint32_t to, const float (&v)[N]) {
+  if (first + N <= to)
+    store_whole<ONCE, N>(row + first, v);
+  else
+    store_some<N>(row + first, to - first, v);
+}
+
+// The pair of a workgroup from its threads'.
+__device__ __forceinline__ MaxSum block_join(MaxSum t, float c, float2* scratch) {
+  t = wave_join(t, c);
+  __syncthreads();
+  if (lane_id() == 0) scratch[wave_id()] = make_float2(t.m, t.s);
+  __syncthreads();
+  const float2 x = lane_id() < kLongWaves ? scratch[lane_id()] : make_float2(-FLT_MAX, 0.0f);
+  return wave_join({x.x, x.y}, c);
+}
+
+// A row's list into LDS, with values in the place of p.  Its sums; all threads.  `saved`: the listed logits, or NULL.
+template <class T>
+__device__ __forceinline__ ListSums load_list(const DistillArgs& a, uint32_t row, const T* zr, const float* saved, const ListLds& l,
+                                              float2* scratch) {
+  MaxSum q = kNothing;
+  const float c = list_c(a);
+  for (uint32_t j = threadIdx.x; j < a.k; j += kLongBlock) {
+    RawEntry r;
+    r.load(a, row, j);
+    const Entry<T> e = entry_of(a, r, zr, !saved);
+    take_entry(q, e.id, e.t, c);
+    l.id[j] = e.id;
+    l.p[j] = e.t;
+    l.z[j] = saved ? saved[j] : (float)e.z;
+  }
+  return ListSums(a, block_join(q, c, scratch));
+}
+// Turns the values into p; the loss (a thread's share of it).
+__device__ __forceinline__ float finish_list(const DistillArgs& a, const ListLds& l, const ListSums& s, MaxSum t, float wT) {
+  float loss = 0.0f;
+  for (uint32_t j = threadIdx.x; j < a.k; j += kLongBlock) {
+    if (l.id[j] < 0) continue;
+    const float value = l.p[j];
+    loss += wT * s.loss(value, tlogq_of(a, l.z[j], t));
+    l.p[j] = s.p(value);
+  }
   return loss;
 }
 
-// The listed places of a row's gradient.
-template <class T>
-__device__ void write_listed(const DistillArgs& a, const List& l, T* drow, float m, float inv, float P, float wT) {
-  for (uint32_t j = threadIdx.x; j < a.k; j += kDistillBlock) {
-    const int32_t id = l.id[j];
-    if (id < 0) continue;
-    float p = 0.0f;
-    for (uint32_t i = 0; i < a.k; ++i) p += l.id[i] == id ? l.p[i] : 0.0f;
-    drow[id] = (T)(wT * (exp_scaled(l.z[j], m, a.c, P * inv * kUnlift) - p));
+// Elements [from, to) of a row's gradient.
+template <bool ONCE, class T>
+__device__ __forceinline__ void write_gradient(const DistillArgs& a, const T* zr, T* dr, uint32_t from, uint32_t to, MaxSum t, float P,
+                                               float wT) {
+  constexpr uint32_t N = kPerAccess<T>;
+  if (P == 0.0f) {
+    const float zero[N] = {};
+    for (uint64_t first = from + threadIdx.x * N; first < to; first += kLongBlock * N) store_part<ONCE, N>(dr, (uint32_t)first, to, zero);
+    return;
   }
+  const float scale = t.s == 0.0f ? 0.0f : wT * P * (1.0f / t.s) * kUnlift;
+  over_row<ONCE>(zr, from, to, [&](uint32_t first, float (&v)[N]) {
+#pragma unroll
+    for (uint32_t i = 0; i < N; ++i) v[i] = exp_scaled(v[i], t.m, a.c, scale);
+    store_part<ONCE, N>(dr, first, to, v);
+  });
 }
 
-template <class T, bool LOSS, bool GRAD>
-__global__ __launch_bounds__(kDistillBlock) void distill_kernel(DistillArgs a, const T* logits, T* dlogits) {
+// A workgroup per row (LOSS, PARTS = false) or per part of a row, whose pairs or statistics are known then.
+template <class T, bool LOSS, bool GRAD, bool ONCE, bool PARTS>
+__global__ __launch_bounds__(kLongBlock) void distill_long_kernel(DistillArgs a, const T* logits, T* dlogits) {
   constexpr uint32_t N = kPerAccess<T>;
-  __shared__ List l;
+  extern __shared__ float lists[];
+  __shared__ float2 scratch[kLongWaves];
+  __shared__ float sums[kLongWaves];
+  const ListLds l(lists, a.k);
+  const uint32_t part = PARTS ? blockIdx.y : 0u;
+  const uint32_t each = PARTS ? ((a.vocab + a.parts - 1) / a.parts + N - 1) / N * N : a.vocab;
+  const uint32_t from = min((uint64_t)part * each, (uint64_t)a.vocab), to = min((uint64_t)from + each, (uint64_t)a.vocab);
   for (uint32_t row = blockIdx.x; row < a.n; row += gridDim.x) {
     const T* zr = logits + row * a.stride;
     T* dr = GRAD ? dlogits + row * a.dstride : nullptr;
-    const float w = a.weights ? a.weights[row] : 1.0f;
+    const float w = a.weights ? a.weights[row] : 1.0f, wT = w * a.T;
+    MaxSum t = kNothing;
+    float P = 0.0f;
     __syncthreads();
-    const float P = w == 0.0f ? 0.0f : load_list(a, row, l);
-    if (P == 0.0f) {  // nothing to learn here
-      if (LOSS && threadIdx.x == 0) {
-        if (a.loss) a.loss[row] = 0.0f;
-        if (a.stats) a.stats[2 * (uint64_t)row] = a.stats[2 * (uint64_t)row + 1] = 0.0f;
-      }
-      if (GRAD)
-        for (uint32_t at = threadIdx.x * N; at < a.vocab; at += kDistillBlock * N) {
-          const float zero[N] = {};
-          store_row<N>(dr, at, a.vocab, zero);
+    if (w != 0.0f) {
+      const ListSums s = load_list(a, row, zr, PARTS && LOSS ? a.logits + (uint64_t)row * a.k : nullptr, l, scratch);
+      P = s.P;
+      if (P != 0.0f) {
+        if (!LOSS) {
+          t = {a.stats[2 * (uint64_t)row], a.stats[2 * (uint64_t)row + 1]};
+        } else if (PARTS) {
+          for (uint32_t i = lane_id(); i < a.parts; i += kWave) {
+            const float2 x = a.pairs[(uint64_t)row * a.parts + i];
+            const float m = fmaxf(t.m, x.x);
+            t = {m, t.s * exp_part(t.m, m, a.c) + x.y * exp_part(x.x, m, a.c)};
+          }
+          t = wave_join(t, a.c);
+        } else {
+          over_row<false>(zr, from, to, [&](uint32_t, float (&v)[N]) { take(t, v, a.c); });
+          t = block_join(t, a.c, scratch);
         }
-      continue;
+        const float loss = finish_list(a, l, s, t, wT);
+        if (LOSS && part == 0) {
+          const float sum = block_sum<kLongWaves>(loss, sums);
+          if (threadIdx.x == 0) {
+            if (a.loss) a.loss[row] = sum;
+            if (a.stats) {
+              a.stats[2 * (uint64_t)row] = t.m;
+              a.stats[2 * (uint64_t)row + 1] = t.s;
+            }
+          }
+        }
+      }
     }
-    for (uint32_t j = threadIdx.x; j < a.k; j += kDistillBlock) l.z[j] = l.id[j] >= 0 ? (float)zr[l.id[j]] : 0.0f;
-    MaxSum t{-FLT_MAX, 0.0f};
-    if (LOSS) {
-      for (uint32_t at = threadIdx.x * N; at < a.vocab; at += kDistillBlock * N) {
-        float v[N];
-        load_row<N>(zr, at, a.vocab, -INFINITY, v);
-        float m = t.m;
-#pragma unroll
-        for (uint32_t i = 0; i < N; ++i) m = fmaxf(m, v[i]);
-        t.s *= exp_part(t.m, m, a.c);
-        t.m = m;
-#pragma unroll
-        for (uint32_t i = 0; i < N; ++i) t.s += exp_part(v[i], m, a.c);
-      }
-      const float m = block_max<kDistillWaves>(t.m, l.scratch);
-      float unused = 0.0f;
-      t.s *= exp_part(t.m, m, a.c);
-      t.m = m;
-      block_sum2<kDistillWaves>(t.s, unused, l.scratch);
-      const float loss = a.loss ? list_loss(a, l, t.m, t.s, w * a.T) : 0.0f;
-      if (threadIdx.x == 0) {
-        if (a.loss) a.loss[row] = loss;
-        if (a.stats) {
-          a.stats[2 * (uint64_t)row] = t.m;
-          a.stats[2 * (uint64_t)row + 1] = t.s;
-        }
-      }
-    } else {
-      t = {a.stats[2 * (uint64_t)row], a.stats[2 * (uint64_t)row + 1]};
+    if (LOSS && P == 0.0f && part == 0 && threadIdx.x == 0) {
+      if (a.loss) a.loss[row] = 0.0f;
+      if (a.stats) a.stats[2 * (uint64_t)row] = a.stats[2 * (uint64_t)row + 1] = 0.0f;
     }
     if (GRAD) {
-      const float inv = t.s == 0.0f ? 0.0f : 1.0f / t.s, wT = w * a.T, scale = wT * P * inv * kUnlift;
       __syncthreads();  // every listed logit has been read: the gradient may take the logits' place
-      for (uint32_t at = threadIdx.x * N; at < a.vocab; at += kDistillBlock * N) {
-        float v[N];
-        load_row<N>(zr, at, a.vocab, 0.0f, v);
-#pragma unroll
-        for (uint32_t i = 0; i < N; ++i) v[i] = exp_scaled(v[i], t.m, a.c, scale);
-        store_row<N>(dr, at, a.vocab, v);
-      }
+      write_gradient<ONCE>(a, zr, dr, from, to, t, P, wT);
       __syncthreads();
-      write_listed(a, l, dr, t.m, inv, P, wT);
+      if (P != 0.0f)
+        for (uint32_t j = threadIdx.x; j < a.k; j += kLongBlock)
+          if (l.id[j] >= (int32_t)from && l.id[j] < (int32_t)to) write_listed(a, l, j, dr, t, P, wT);
     }
   }
 }
 
+// The pair of a part of a row.
+template <class T>
+__global__ __launch_bounds__(kLongBlock) void part_sum_kernel(DistillArgs a, const T* logits) {
+  constexpr uint32_t N = kPerAccess<T>;
+  __shared__ float2 scratch[kLongWaves];
+  const uint32_t row = blockIdx.x, part = blockIdx.y, each = ((a.vocab + a.parts - 1) / a.parts + N - 1) / N * N;
+  const uint32_t from = min((uint64_t)part * each, (uint64_t)a.vocab), to = min((uint64_t)from + each, (uint64_t)a.vocab);
+  if (a.weights && a.weights[row] == 0.0f) return;
+  if (part == 0)
+    for (uint32_t j = threadIdx.x; j < a.k; j += kLongBlock) {
+      RawEntry r;
+      r.load(a, row, j);
+      if (r.id >= 0 && r.id < (int64_t)a.vocab) a.logits[(uint64_t)row * a.k + j] = (float)logits[row * a.stride + r.id];
+    }
+  MaxSum t = kNothing;
+  over_row<false>(logits + row * a.stride, from, to, [&](uint32_t, float (&v)[N]) { take(t, v, a.c); });
+  t = block_join(t, a.c, scratch);
+  if (threadIdx.x == 0) a.pairs[(uint64_t)row * a.parts + part] = make_float2(t.m, t.s);
+}
+
+// ----------------------------------------------------------------------------- host
 int check(uint32_t n, uint32_t vocab, const void* logits, uint32_t type, uint64_t stride, uint32_t k, const void* ids,
           uint32_t id_bytes, const void* values, uint32_t value_type, float T, uint32_t flags, const float* weights,
           const float* stats, const void* dlogits, uint64_t dstride, const uint32_t* status) {
@@ -226,12 +525,86 @@ int check(uint32_t n, uint32_t vocab, const void* logits, uint32_t type, uint64_
   return CVLC_OK;
 }
 
+template <uint32_t W_, uint32_t V_, uint32_t O_>
+struct RowShape {
+  static constexpr uint32_t W = W_, V = V_, O = O_, kRows = W == 1 ? 4 : 1, kWaves = W * kRows;
+  static constexpr uint32_t kPerCu = 4 * O > kWaves ? 4 * O / kWaves : 1;
+};
+#ifndef S1
+#define S1 1, 1, 8
+#define S2 1, 2, 6
+#define S4 1, 4, 4
+#define F2 4, 2, 6
+#define F4 4, 4, 4
+#define F8 8, 4, 4
+#define F16 8, 8, 4
+#define F32 16, 8, 4
+#define F64 16, 16, 4
+#endif
+// Calls f with the shape that holds a row of `accesses`; false: none does, or there is none for rows that are only read or
+// only written.
+template <bool BOTH, class F>
+bool by_row_shape(uint32_t accesses, F f) {
+  if (accesses <= 64) return f(RowShape<S1>{});
+  if (accesses <= 128) return f(RowShape<S2>{});
+  if (accesses <= 256) return f(RowShape<S4>{});
+  if constexpr (BOTH) {
+    if (accesses <= 512) return f(RowShape<F2>{});
+    if (accesses <= 1024) return f(RowShape<F4>{});
+    if (accesses <= 2048) return f(RowShape<F8>{});
+    if (accesses <= 4096) return f(RowShape<F16>{});
+    if (accesses <= 8192) return f(RowShape<F32>{});
+    if (accesses <= 16384) return f(RowShape<F64>{});
+  }
+  return false;
+}
+
+// Parts that few rows are cut into, by elements alone, so that the workspace does not depend on their type: 1 = none.
+#ifndef PARTELEMS
+#define PARTELEMS 8192u
+#define PARTROWS 512u
+#endif
+constexpr uint32_t kPartRows = PARTROWS, kPartElements = PARTELEMS;
+uint32_t parts_for(uint32_t n, uint32_t vocab) {
+  if (n == 0 || n >= kPartRows) return 1;
+  return std::max(1u, std::min(vocab / kPartElements, (2 * kPartRows + n - 1) / n));
+}
+
+bool once(uint32_t n, uint32_t vocab, uint32_t bytes) { return (uint64_t)n * vocab * bytes > 256ull * 1000000; }
+
 template <bool LOSS, bool GRAD>
-int launch(const DistillArgs& a, uint32_t type, const void* logits, void* dlogits, void* hip_stream) {
+int launch(DistillArgs a, uint32_t type, const void* logits, void* dlogits, hipStream_t stream) {
   by_type(type, [&](auto t) {
     using T = decltype(t);
-    hipLaunchKernelGGL((distill_kernel<T, LOSS, GRAD>), dim3(std::min(a.n, 1u << 20)), dim3(kDistillBlock), 0,
-                       static_cast<hipStream_t>(hip_stream), a, static_cast<const T*>(logits), static_cast<T*>(dlogits));
+    constexpr uint32_t N = kPerAccess<T>;
+    const T* z = static_cast<const T*>(logits);
+    T* d = static_cast<T*>(dlogits);
+    const bool past = once(a.n, a.vocab, (GRAD ? 2 : 1) * sizeof(T));
+    if (a.parts > 1) {
+      const uint32_t lds = kListWords * a.k * sizeof(float);
+      if (LOSS) hipLaunchKernelGGL(part_sum_kernel<T>, dim3(a.n, a.parts), dim3(kLongBlock), 0, stream, a, z);
+      hipLaunchKernelGGL((distill_long_kernel<T, LOSS, GRAD, false, true>), dim3(a.n, GRAD ? a.parts : 1), dim3(kLongBlock), lds, stream,
+                         a, z, d);
+      return;
+    }
+    if (a.vocab >= N && by_row_shape<LOSS && GRAD>((a.vocab + N - 1) / N, [&](auto shape) {
+          using S = decltype(shape);
+          const uint32_t lds = S::kRows * 2 * kListWords * a.k * sizeof(float);
+          const uint32_t grid = std::min((a.n + S::kRows - 1) / S::kRows, 256u * S::kPerCu);
+          auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(grid), dim3(S::kWaves * kWave), lds, stream, a, z, d); };
+          if (past)
+            go(distill_rows_kernel<T, LOSS, GRAD, true, S::W, S::V, S::O>);
+          else
+            go(distill_rows_kernel<T, LOSS, GRAD, false, S::W, S::V, S::O>);
+          return true;
+        }))
+      return;
+    const uint32_t lds = kListWords * a.k * sizeof(float);
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(std::min(a.n, 1u << 20)), dim3(kLongBlock), lds, stream, a, z, d); };
+    if (past)
+      go(distill_long_kernel<T, LOSS, GRAD, true, false>);
+    else
+      go(distill_long_kernel<T, LOSS, GRAD, false, false>);
   });
   return hip_check(hipGetLastError());
 }
@@ -242,9 +615,11 @@ int launch(const DistillArgs& a, uint32_t type, const void* logits, void* dlogit
 extern "C" {
 
 size_t cvlc_distill_workspace_bytes(uint32_t n, uint32_t vocab) {
-  (void)n;
+  using namespace cvlc;
   (void)vocab;
-  return 256u;
+  // the most that fewer rows need, and rows that are not cut need nothing: never less for more rows or longer ones
+  const uint64_t rows = std::min(n, kPartRows);
+  return 256u + (size_t)((rows * kMaxK * sizeof(float)) + (2 * kPartRows + 2 * rows) * sizeof(float2));
 }
 
 int cvlc_distill(uint32_t n, uint32_t vocab, const void* d_logits, uint32_t type, uint64_t stride, uint32_t k, const void* d_ids,
@@ -260,10 +635,13 @@ int cvlc_distill(uint32_t n, uint32_t vocab, const void* d_logits, uint32_t type
   if (!buffer_ok(d_workspace, 256)) return CVLC_ERR_ARG;
   if (ws_bytes < cvlc_distill_workspace_bytes(n, vocab)) return CVLC_ERR_CAPACITY;
   if (n == 0) return CVLC_OK;
+  const uint32_t parts = parts_for(n, vocab);
+  float2* pairs = static_cast<float2*>(d_workspace);
   const DistillArgs a{n, vocab, k, stride, dlogits_stride, d_ids, d_values, id_bytes, value_type, temperature,
-                      (float)(M_LOG2E / temperature), flags & CVLC_DISTILL_LOGPROBS, d_weights, d_loss, d_stats, d_status};
-  return d_dlogits ? launch<true, true>(a, type, d_logits, d_dlogits, hip_stream)
-                   : launch<true, false>(a, type, d_logits, nullptr, hip_stream);
+                      (float)(M_LOG2E / temperature), flags & CVLC_DISTILL_LOGPROBS, d_weights, d_loss, d_stats, d_status,
+                      parts, pairs, reinterpret_cast<float*>(pairs + (uint64_t)n * parts)};
+  hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+  return d_dlogits ? launch<true, true>(a, type, d_logits, d_dlogits, stream) : launch<true, false>(a, type, d_logits, nullptr, stream);
 }
 
 int cvlc_distill_grad(uint32_t n, uint32_t vocab, const void* d_logits, uint32_t type, uint64_t stride, uint32_t k,
@@ -276,10 +654,12 @@ int cvlc_distill_grad(uint32_t n, uint32_t vocab, const void* d_logits, uint32_t
   if (rc) return rc;
   if (n == 0) return CVLC_OK;
   if (!d_stats || !d_dlogits) return CVLC_ERR_ARG;
+  // in place a part's gradient might take a listed logit's place before another part's workgroup has read it
+  const uint32_t parts = d_dlogits == d_logits ? 1u : parts_for(n, vocab);
   const DistillArgs a{n, vocab, k, stride, dlogits_stride, d_ids, d_values, id_bytes, value_type, temperature,
                       (float)(M_LOG2E / temperature), flags & CVLC_DISTILL_LOGPROBS, d_weights, nullptr,
-                      const_cast<float*>(d_stats), d_status};
-  return launch<false, true>(a, type, d_logits, d_dlogits, hip_stream);
+                      const_cast<float*>(d_stats), d_status, parts, nullptr, nullptr};
+  return launch<false, true>(a, type, d_logits, d_dlogits, static_cast<hipStream_t>(hip_stream));
 }
 
 }  // extern "C"

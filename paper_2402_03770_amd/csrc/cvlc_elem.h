@@ -201,6 +201,21 @@ __device__ __forceinline__ float wave_sum(float v) {
   return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
 }
 
+__device__ __forceinline__ float wave_max(float v) {
+  auto other = [&](auto ctrl, auto rows) {
+    const int w = __float_as_int(v);
+    return __int_as_float(__builtin_amdgcn_update_dpp(w, w, ctrl.value, rows.value, 0xF, false));
+  };
+  using std::integral_constant;
+  v = fmaxf(v, other(integral_constant<int, 0x128>{}, integral_constant<int, 0xF>{}));
+  v = fmaxf(v, other(integral_constant<int, 0x124>{}, integral_constant<int, 0xF>{}));
+  v = fmaxf(v, other(integral_constant<int, 0x122>{}, integral_constant<int, 0xF>{}));
+  v = fmaxf(v, other(integral_constant<int, 0x121>{}, integral_constant<int, 0xF>{}));
+  v = fmaxf(v, other(integral_constant<int, 0x142>{}, integral_constant<int, 0xA>{}));
+  v = fmaxf(v, other(integral_constant<int, 0x143>{}, integral_constant<int, 0xC>{}));
+  return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
+}
+
 // The sum of a value over a workgroup of NW wavefronts, the same in every thread.  `scratch` holds NW floats.
 template <uint32_t NW>
 __device__ __forceinline__ float block_sum(float a, float* scratch) {
