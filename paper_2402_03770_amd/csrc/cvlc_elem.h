@@ -24,13 +24,9 @@ inline bool buffer_ok(const void* p, uint32_t bytes) { return p && reinterpret_c
 template <class A, class B = A>
 constexpr uint32_t kPerAccess = 16u / (sizeof(A) > sizeof(B) ? sizeof(A) : sizeof(B));
 
-// N consecutive elements.  Rows start wherever the caller's stride puts them, so the address is a multiple of the
-// element's size only; global memory takes 16 bytes at any such address in one access.
-template <class T, uint32_t N>
-struct __attribute__((packed, aligned(sizeof(T)))) Packed {
-  T v[N];
-};
-
+// Rows start wherever the caller's stride puts them, so an access's address is a multiple of the element's size only;
+// global memory takes 16 bytes at any such address in one access.  Said with vectors of words: of a struct of elements the
+// compiler makes accesses of 2, 4 and 8 bytes.
 typedef uint32_t Quad __attribute__((ext_vector_type(4)));
 typedef uint32_t Pair __attribute__((ext_vector_type(2)));
 typedef Quad UnalignedQuad __attribute__((aligned(2)));
@@ -71,6 +67,28 @@ struct Raw {
     }
   }
 };
+
+// Elements [at, at + N) of a row of `width`, as far as it goes; zero bits beyond.
+template <bool ONCE = false, class T, uint32_t N>
+__device__ __forceinline__ void load_raw(Raw<T, N>& raw, const T* row, uint32_t at, uint32_t width) {
+  if (at + N <= width) {
+    raw.template load<ONCE>(row + at);
+  } else {
+    constexpr uint32_t kEach = 4 / sizeof(T);
+#pragma unroll
+    for (uint32_t i = 0; i < Raw<T, N>::kWords; ++i) {
+      raw.w[i] = 0;
+#pragma unroll
+      for (uint32_t k = 0; k < kEach; ++k)
+        if (at + i * kEach + k < width) {
+          if constexpr (sizeof(T) == 4)
+            raw.w[i] = __float_as_uint(row[at + i]);
+          else
+            raw.w[i] |= (uint32_t)__builtin_bit_cast(uint16_t, row[at + i * kEach + k]) << (16 * k);
+        }
+    }
+  }
+}
 
 // Rounds N values to the type, once, and writes them in accesses of 16 bytes (or one of 8).
 template <bool ONCE, uint32_t N, class T>
@@ -137,23 +155,22 @@ struct Place {
 
 template <uint32_t N, class T>
 __device__ __forceinline__ void load_values(const T* p, float (&x)[N]) {
-  const Packed<T, N> raw = *reinterpret_cast<const Packed<T, N>*>(p);
+  constexpr uint32_t kEach = N * sizeof(T) > 16 ? 16 / sizeof(T) : N;
 #pragma unroll
-  for (uint32_t i = 0; i < N; ++i) x[i] = (float)raw.v[i];
+  for (uint32_t k = 0; k < N; k += kEach) {
+    Raw<T, kEach> raw;
+    float part[kEach];
+    raw.template load<false>(p + k);
+    raw.values(part);
+#pragma unroll
+    for (uint32_t i = 0; i < kEach; ++i) x[k + i] = part[i];
+  }
 }
 // The first `count` of them, `fill` in the place of the others.
 template <uint32_t N, class T>
 __device__ __forceinline__ void load_some(const T* p, uint32_t count, float fill, float (&x)[N]) {
 #pragma unroll
   for (uint32_t i = 0; i < N; ++i) x[i] = i < count ? (float)p[i] : fill;
-}
-// Rounded to the nearest value of the type, once: the only rounding an output sees.
-template <uint32_t N, class T>
-__device__ __forceinline__ void store_values(T* p, const float (&x)[N]) {
-  Packed<T, N> raw;
-#pragma unroll
-  for (uint32_t i = 0; i < N; ++i) raw.v[i] = (T)x[i];
-  *reinterpret_cast<Packed<T, N>*>(p) = raw;
 }
 template <uint32_t N, class T>
 __device__ __forceinline__ void store_some(T* p, uint32_t count, const float (&x)[N]) {
@@ -169,10 +186,10 @@ __device__ __forceinline__ void load_row(const T* row, uint32_t at, uint32_t wid
   else
     load_some<N>(row + at, at < width ? width - at : 0u, fill, x);
 }
-template <uint32_t N, class T>
+template <uint32_t N, bool ONCE = false, class T>
 __device__ __forceinline__ void store_row(T* row, uint32_t at, uint32_t width, const float (&x)[N]) {
   if (at + N <= width)
-    store_values<N>(row + at, x);
+    store_whole<ONCE, N>(row + at, x);
   else if (at < width)
     store_some<N>(row + at, width - at, x);
 }

@@ -685,3 +685,58 @@ def test_workspaces_never_shrink():
         assert cv.layer_norm_grad_workspace_bytes(n, dim) <= cv.layer_norm_grad_workspace_bytes(n + 1, dim)
         assert cv.layer_norm_grad_workspace_bytes(n, dim) <= cv.layer_norm_grad_workspace_bytes(n, dim + 1)
         assert cv.distill_workspace_bytes(n, vocab) <= cv.distill_workspace_bytes(n + 1, vocab)
+
+
+# ----------------------------------------------------------------------------- more tokens than a workgroup lists
+@gpu
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("n,dim,vocab", [(16384, 40, 100), (16385, 41, 5000), (40000, 300, 7), (70001, 33, 300), (50000, 17, 40000)])
+def test_embed_grad_of_many_tokens(dtype, n, dim, vocab):
+    """One side and the other of the largest call that lists its places, and the sort of one, two and three digits."""
+    dout = random_matrix(n, dim, dtype, 100, extra=2, offset=1)
+    _, status = check_embed_grad(tokens(n, vocab, 101), dout, vocab, scale=0.3, extra=1, offset=3)
+    assert status == 0
+
+
+@gpu
+@pytest.mark.parametrize("kind", ["one", "padding", "one beyond", "ends", "runs", "descending"])
+def test_embed_grad_of_many_tokens_in_odd_order(kind):
+    n, vocab, dim = 36000, 5000, 20
+    i = torch.arange(n)
+    ids = {"one": torch.full((n,), 77), "padding": torch.full((n,), -1), "one beyond": torch.where(i == 35999, 5000, i % 4000),
+           "ends": torch.where(i % 3 == 0, 0, 4999), "runs": (i // 64) % vocab, "descending": (n - i) // 37 % vocab}[kind]
+    dout = random_matrix(n, dim, F32, 102)
+    _, status = check_embed_grad(ids.long(), dout, vocab)
+    assert status == (cv.DEV_INDEX if kind == "one beyond" else 0)
+    start = random_matrix(vocab, dim, F32, 103)
+    a, _ = check_embed_grad(ids.int(), dout, vocab, start=start)
+    b, _ = check_embed_grad(ids.int(), dout, vocab, start=start)
+    assert torch.equal(a, b)
+
+
+@gpu
+@pytest.mark.parametrize("n,dim,vocab", [(500, 4099, 600), (2000, 700, 300), (10, 3, 70_000), (0, 5, 70_000), (3000, 8, 1)])
+@pytest.mark.parametrize("dtype", [F32, F16])
+def test_embed_grad_in_one_launch(dtype, n, dim, vocab):
+    """Several blocks of columns, the last one narrow; more rows to a workgroup than it has groups of threads; one row."""
+    dout = random_matrix(n, dim, dtype, 104, extra=1)
+    ids = tokens(n, vocab, 105)
+    a, _ = check_embed_grad(ids, dout, vocab, scale=2.0, offset=1)
+    b, _ = check_embed_grad(ids, dout, vocab, scale=2.0, offset=1)
+    assert torch.equal(a, b)
+
+
+@gpu
+@pytest.mark.parametrize("n,dim", [(8191, 2050), (8195, 2050), (70_001, 24)])
+def test_embed_of_many_rows(n, dim):
+    """Threads that take four rows each, the last one fewer."""
+    vocab = 300
+    table = random_matrix(vocab, dim, BF16, 106)
+    ids = tokens(n, vocab, 107)
+    ids[n - 1] = vocab
+    out, flat = matrix(n, dim, BF16, fill=3.0)
+    status = torch.zeros(1, dtype=torch.int32, device=DEV)
+    cv.embed(ids.to(DEV), table, out, scale=0.7, status=status)
+    want, tol = ref.embed(ids.numpy(), f64(table), 0.7)
+    assert_near(out, want, tol, BF16)
+    assert status.item() == cv.DEV_INDEX and untouched(flat, out, 3.0)
