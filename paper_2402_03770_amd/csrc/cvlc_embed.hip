@@ -386,7 +386,7 @@ __global__ __launch_bounds__(kEmbedBlock) void clear_kernel(uint32_t* status, ui
 }
 
 // ----------------------------------------------------------------------------- few tokens
-constexpr uint32_t kDirectBlock = 512, kDirectWaves = kDirectBlock / kWave;
+constexpr uint32_t kDirectBlock = 1024, kDirectWaves = kDirectBlock / kWave;
 constexpr uint32_t kDirectTokens = 16384;  // places are kept in 16 bits of LDS each
 constexpr uint32_t kSliceRows = 256;       // rows of the table that a workgroup owns, at most
 constexpr uint32_t kScanDeep = 8;          // tokens under way per thread
@@ -544,11 +544,11 @@ __global__ __launch_bounds__(kDirectBlock) void direct_kernel(DirectArgs a, cons
 }
 
 // Slices (a power of two) that the table is cut into, if that is the way for so many tokens.  Every workgroup reads all the
-// tokens, twice, so there are two workgroups a CU and not more (16384 tokens, 32000 rows of 768 bf16: 88 us with four, 81
-// with two), except for a table of more rows than they keep counts of.  Against the sort and its sums, at the time each was
-// measured: 640 tokens of 96 fp32 6.7 us (47 sorted), 16384 of 768 bf16 81 (101), 30000 of 512 119 (99); 1000 of 8192, a
-// table of 1 GB that has to be written, 224 (267).
-constexpr uint32_t kDirectBlocks = 512;
+// tokens, twice, so there is one, as large as they go, to a CU (12000 tokens, 2000 rows of 200 bf16: 16.6 us; two of 512
+// threads each 20.7), except for a table of more rows than it keeps counts of.  Against the sort and its sums, with inputs
+// that are not in the caches: 640 tokens of 96 fp32 6.7 us (35 sorted), 12000 of 200 bf16 16.6 (59), 16384 of 768 bf16 70
+// (73), 1000 of 8192 bf16 into a table of 1 GB 217 (228); 30000 of 512 bf16 119 (99), before both became faster.
+constexpr uint32_t kDirectBlocks = 256;
 constexpr uint64_t kDirectReads = 1u << 25;  // tokens read by all workgroups
 bool direct_slices(uint32_t n, uint32_t vocab, uint32_t column_blocks, uint32_t* slices_log) {
   if (n > kDirectTokens) return false;
