@@ -740,3 +740,41 @@ def test_embed_of_many_rows(n, dim):
     want, tol = ref.embed(ids.numpy(), f64(table), 0.7)
     assert_near(out, want, tol, BF16)
     assert status.item() == cv.DEV_INDEX and untouched(flat, out, 3.0)
+
+
+# ----------------------------------------------------------------------------- together
+@gpu
+def test_local_step_example():
+    """The example's step against automatic differentiation of its loss in 64 bits; then rounds of it, whose loss falls."""
+    import math
+
+    from examples import local_step as ex
+
+    g = torch.Generator().manual_seed(3)
+    n, vocab, dim, k, T = 60, 150, 24, 5, 2.0
+    model = ex.Model(vocab, dim, DEV)
+    flat = torch.randn(model.flat.numel(), generator=g)
+    model.flat.copy_(flat)
+    ids = torch.randint(vocab, (n,), generator=g)
+    ids[-6:] = -1
+    tids, tvals = torch.stack([torch.randperm(vocab, generator=g)[:k] for _ in range(n)]), torch.randn(n, k, generator=g)
+    client = ex.Client(model, ids.to(DEV), tids.to(DEV), tvals.to(DEV), T)
+    loss = client.step(1.0)
+
+    f = flat.double().requires_grad_()
+    table, gamma, beta = f[:vocab * dim].view(vocab, dim), f[vocab * dim:-dim], f[-dim:]
+    x = table[ids.clamp(min=0)] * math.sqrt(dim) * (ids >= 0).double()[:, None]
+    c = x - x.mean(1, keepdim=True)
+    y = c / torch.sqrt((c * c).mean(1, keepdim=True) + 1e-5) * gamma + beta
+    logq = torch.log_softmax(y @ table.t() / T, 1)
+    logp = torch.log_softmax(tvals.double() / T, 1)
+    want = T * T * (logp.exp() * (logp - logq.gather(1, tids))).sum(1)[ids >= 0].mean()
+    want.backward()
+    # four sums in a row, of 150 terms at most, each off by no more than its length times a rounding of its terms, which
+    # cancel to a tenth of their size at worst
+    slack = 4 * 150 * ref.U * 10
+    assert loss.item() == pytest.approx(want.item(), rel=slack)
+    assert torch.linalg.norm(client.update.cpu().double() + f.grad) <= slack * torch.linalg.norm(f.grad)
+
+    losses = ex.run(rounds=6, clients=3, n=200, vocab=300, dim=32, k=8, say=lambda text: None)
+    assert losses[-1] < losses[0]
