@@ -65,7 +65,7 @@ class Client:
         return self.loss.sum()
 
 
-def run(rounds: int = 20, clients: int = 4, n: int = 512, vocab: int = 2000, dim: int = 64, k: int = 16, rate: float = 50.0,
+def run(rounds: int = 20, clients: int = 4, n: int = 512, vocab: int = 2000, dim: int = 64, k: int = 16, rate: float = 4.0,
         temperature: float = 2.0, seed: int = 1, device: str = "cuda:0", say=print):
     """Returns the rounds' mean losses."""
     g = torch.Generator(device=device).manual_seed(seed)

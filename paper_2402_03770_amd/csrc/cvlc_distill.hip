@@ -157,21 +157,38 @@ __device__ __forceinline__ float tlogq_of(const DistillArgs& a, float z, MaxSum 
   return t.s == 0.0f ? -INFINITY : (z - t.m) - a.T * logf(t.s);
 }
 
-// Lists in LDS, while a row is worked on: ids and p, for entries that share a place.
+// Lists in LDS, while a row is worked on: ids, p and logits, each of k entries and up to three without an id, so that four
+// at a time can be read.
+__host__ __device__ constexpr uint32_t list_room(uint32_t k) { return (k + 3u) & ~3u; }
 struct ListLds {
   int32_t* id;
   float *p, *z;
-  __device__ __forceinline__ ListLds(float* base, uint32_t k) : id(reinterpret_cast<int32_t*>(base)), p(base + k), z(base + 2 * k) {}
+  __device__ __forceinline__ ListLds(float* base, uint32_t k)
+      : id(reinterpret_cast<int32_t*>(base)), p(base + list_room(k)), z(base + 2 * list_room(k)) {}
+  // by any four threads
+  __device__ __forceinline__ void end(uint32_t thread, uint32_t k) const {
+    if (k + thread < list_room(k)) id[k + thread] = -1;
+  }
 };
 constexpr uint32_t kListWords = 3;
 
-// Entry j's place of a row's gradient.
-template <class T>
+// Entry j's place of a row's gradient.  Entries of one id share it, and each writes the whole sum: k^2 comparisons, four to
+// a read of LDS and DEEP reads under way (one entry to a read, 3000 rows of 8000 bf16 with lists of 200: 65 us, now 41).
+// DEEP is 1 where the next row fills the registers meanwhile (4096 rows of 131072: 498 us, 583 with four).
+template <uint32_t DEEP, class T>
 __device__ __forceinline__ void write_listed(const DistillArgs& a, const ListLds& l, uint32_t j, T* drow, MaxSum t, float P, float wT) {
   const int32_t id = l.id[j];
   if (id < 0) return;
   float p = 0.0f;
-  for (uint32_t i = 0; i < a.k; ++i) p += l.id[i] == id ? l.p[i] : 0.0f;
+#pragma unroll DEEP
+  for (uint32_t i = 0; i < a.k; i += 4) {
+    const int4 ids = *reinterpret_cast<const int4*>(l.id + i);
+    const float4 ps = *reinterpret_cast<const float4*>(l.p + i);
+    p += ids.x == id ? ps.x : 0.0f;
+    p += ids.y == id ? ps.y : 0.0f;
+    p += ids.z == id ? ps.z : 0.0f;
+    p += ids.w == id ? ps.w : 0.0f;
+  }
   const float inv = t.s == 0.0f ? 0.0f : 1.0f / t.s;
   drow[id] = (T)(wT * (exp_scaled(l.z[j], t.m, a.c, P * inv * kUnlift) - p));
 }
@@ -191,14 +208,25 @@ __device__ __forceinline__ void load_place(Raw<T, N>& raw, const T* row, uint32_
   if (first < width) raw.template load<ONCE>(row + min(first, width - N));
 }
 
+// A place that is worked out where the row ends and nowhere else: known before the loop over the rows, the masks of 16 of
+// them would be held all along, and there are not that many registers.
+template <uint32_t N>
+__device__ __forceinline__ Place<N> place_here(uint32_t first, uint32_t width) {
+  asm volatile("" : "+v"(first));
+  return Place<N>(first, width);
+}
+
 // W wavefronts to a row, V accesses per thread; workgroups of at least four wavefronts, which are then rows of their own.
 template <class T, bool LOSS, bool GRAD, bool ONCE, uint32_t W, uint32_t V, uint32_t O>
 __global__ __launch_bounds__((W == 1 ? 4 : W) * kWave, O) void distill_rows_kernel(DistillArgs a, const T* logits, T* dlogits) {
   constexpr uint32_t N = kPerAccess<T>, L = W * kWave, ROWS = W == 1 ? 4 : 1;
-  extern __shared__ float lists[];  // [ROWS][2][kListWords][k]
+  extern __shared__ float4 list_space[];  // [ROWS][2][kListWords][list_room(k)]
+  float* lists = reinterpret_cast<float*>(list_space);
   __shared__ float4 pairs[2][ROWS][W];
   __shared__ float losses[2][ROWS][W];
-  const uint32_t lane = threadIdx.x % L, mine = threadIdx.x / L, step = gridDim.x * ROWS, wave = lane / kWave;
+  // a row is the same in all of a wavefront's lanes: said so, its addresses are in scalar registers
+  const uint32_t mine = ROWS == 1 ? 0u : __builtin_amdgcn_readfirstlane(threadIdx.x / L), step = gridDim.x * ROWS;
+  const uint32_t lane = threadIdx.x % L, wave = __builtin_amdgcn_readfirstlane(lane / kWave);
   uint32_t row = blockIdx.x * ROWS + mine, turn = 0;
   Raw<T, N> raw[V];
   RawEntry entry{-1, 0.0f};
@@ -223,7 +251,7 @@ __global__ __launch_bounds__((W == 1 ? 4 : W) * kWave, O) void distill_rows_kern
     const float w_next = !more ? 0.0f : a.weights ? a.weights[next] : 1.0f;
     const bool load_next = w_next != 0.0f;
     const T* zn = logits + (uint64_t)(more ? next : row) * a.stride;
-    const ListLds l(lists + (2 * mine + turn) * kListWords * a.k, a.k);
+    const ListLds l(lists + (2 * mine + turn) * kListWords * list_room(a.k), a.k);
     MaxSum t = kNothing;
     float P = 0.0f;
     if (w != 0.0f) {
@@ -249,13 +277,14 @@ __global__ __launch_bounds__((W == 1 ? 4 : W) * kWave, O) void distill_rows_kern
           if (first >= a.vocab) break;
           float v[N];
           raw[j].values(v);
-          Place<N>(first, a.vocab).mask(v, -INFINITY);
+          if (first + N > a.vocab) place_here<N>(first, a.vocab).mask(v, -INFINITY);
           take(t, v, a.c);
           if (!GRAD && load_next) load_place<ONCE>(raw[j], zn, first, a.vocab);
         }
         t = wave_join(t, a.c);
       }
       q = wave_join(q, lc);
+      l.end(lane, a.k);
       if (has_entry) {
         l.id[lane] = e.id;
         l.p[lane] = e.t;
@@ -308,7 +337,10 @@ __global__ __launch_bounds__((W == 1 ? 4 : W) * kWave, O) void distill_rows_kern
           raw[j].values(v);
 #pragma unroll
           for (uint32_t i = 0; i < N; ++i) v[i] = nothing ? 0.0f : exp_scaled(v[i], t.m, a.c, scale);
-          Place<N>(first, a.vocab).template store<ONCE>(dr, v);
+          if (first + N <= a.vocab)
+            store_whole<ONCE, N>(dr + first, v);
+          else
+            place_here<N>(first, a.vocab).template store<ONCE>(dr, v);
         }
         if (load_next) load_place<ONCE>(raw[j], zn, first, a.vocab);
       }
@@ -322,7 +354,7 @@ __global__ __launch_bounds__((W == 1 ? 4 : W) * kWave, O) void distill_rows_kern
         a.loss[row] = sum;
       }
       if (GRAD && P != 0.0f)
-        for (uint32_t j = lane; j < a.k; j += L) write_listed(a, l, j, dlogits + row * a.dstride, t, P, w * a.T);
+        for (uint32_t j = lane; j < a.k; j += L) write_listed<(V < 16 ? 4 : 1)>(a, l, j, dlogits + row * a.dstride, t, P, w * a.T);
       turn ^= 1;  // the other half of LDS: this one may still be read
     }
     w = w_next;
@@ -382,6 +414,7 @@ __device__ __forceinline__ ListSums load_list(const DistillArgs& a, uint32_t row
                                               float2* scratch) {
   MaxSum q = kNothing;
   const float c = list_c(a);
+  l.end(threadIdx.x, a.k);
   for (uint32_t j = threadIdx.x; j < a.k; j += kLongBlock) {
     RawEntry r;
     r.load(a, row, j);
@@ -427,10 +460,10 @@ __device__ __forceinline__ void write_gradient(const DistillArgs& a, const T* zr
 template <class T, bool LOSS, bool GRAD, bool ONCE, bool PARTS>
 __global__ __launch_bounds__(kLongBlock) void distill_long_kernel(DistillArgs a, const T* logits, T* dlogits) {
   constexpr uint32_t N = kPerAccess<T>;
-  extern __shared__ float lists[];
+  extern __shared__ float4 list_space[];
   __shared__ float2 scratch[kLongWaves];
   __shared__ float sums[kLongWaves];
-  const ListLds l(lists, a.k);
+  const ListLds l(reinterpret_cast<float*>(list_space), a.k);
   const uint32_t part = PARTS ? blockIdx.y : 0u;
   const uint32_t each = PARTS ? ((a.vocab + a.parts - 1) / a.parts + N - 1) / N * N : a.vocab;
   const uint32_t from = min((uint64_t)part * each, (uint64_t)a.vocab), to = min((uint64_t)from + each, (uint64_t)a.vocab);
@@ -481,7 +514,7 @@ __global__ __launch_bounds__(kLongBlock) void distill_long_kernel(DistillArgs a,
       __syncthreads();
       if (P != 0.0f)
         for (uint32_t j = threadIdx.x; j < a.k; j += kLongBlock)
-          if (l.id[j] >= (int32_t)from && l.id[j] < (int32_t)to) write_listed(a, l, j, dr, t, P, wT);
+          if (l.id[j] >= (int32_t)from && l.id[j] < (int32_t)to) write_listed<4>(a, l, j, dr, t, P, wT);
     }
   }
 }
@@ -530,10 +563,9 @@ struct RowShape {
   static constexpr uint32_t W = W_, V = V_, O = O_, kRows = W == 1 ? 4 : 1, kWaves = W * kRows;
   static constexpr uint32_t kPerCu = 4 * O > kWaves ? 4 * O / kWaves : 1;
 };
-// Registers hold the row (16 bytes an access) and the threads' 128 hold up to 16 of them at four wavefronts a SIMD, so a CU
-// has one row of 131072 bf16 at a time: 4096 of them 490 us, 4.2 TB/s (two passes over each row, from HBM and then from the
-// caches, 692).  Conditions that are the same in a wavefront told to the compiler as such, and places worked out again at each
-// use instead of held in masks: 622 us, since the branches keep an access's exponentials from another's.
+// Registers hold the row (16 bytes an access), and a thread's 128 hold up to 16 of them at four wavefronts a SIMD, so a CU has
+// one row of 131072 bf16 at a time: 4096 of them 490 us, 4.1 TB/s (two passes over each row, from HBM and then from the
+// caches, 692).  8192 rows of 32000 bf16 215 us, 4.9 TB/s.
 // Calls f with the shape that holds a row of `accesses`; false: none does, or there is none for rows that are only read or
 // only written.
 template <bool BOTH, class F>
@@ -571,7 +603,7 @@ int launch(DistillArgs a, uint32_t type, const void* logits, void* dlogits, hipS
     T* d = static_cast<T*>(dlogits);
     const bool past = once(a.n, a.vocab, (GRAD ? 2 : 1) * sizeof(T));
     if (a.parts > 1) {
-      const uint32_t lds = kListWords * a.k * sizeof(float);
+      const uint32_t lds = kListWords * list_room(a.k) * sizeof(float);
       if (LOSS) hipLaunchKernelGGL(part_sum_kernel<T>, dim3(a.n, a.parts), dim3(kLongBlock), 0, stream, a, z);
       hipLaunchKernelGGL((distill_long_kernel<T, LOSS, GRAD, false, true>), dim3(a.n, GRAD ? a.parts : 1), dim3(kLongBlock), lds, stream,
                          a, z, d);
@@ -579,7 +611,7 @@ int launch(DistillArgs a, uint32_t type, const void* logits, void* dlogits, hipS
     }
     if (a.vocab >= N && by_row_shape<LOSS && GRAD>((a.vocab + N - 1) / N, [&](auto shape) {
           using S = decltype(shape);
-          const uint32_t lds = S::kRows * 2 * kListWords * a.k * sizeof(float);
+          const uint32_t lds = S::kRows * 2 * kListWords * list_room(a.k) * sizeof(float);
           const uint32_t grid = std::min((a.n + S::kRows - 1) / S::kRows, 256u * S::kPerCu);
           auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(grid), dim3(S::kWaves * kWave), lds, stream, a, z, d); };
           if (past)
@@ -589,7 +621,7 @@ int launch(DistillArgs a, uint32_t type, const void* logits, void* dlogits, hipS
           return true;
         }))
       return;
-    const uint32_t lds = kListWords * a.k * sizeof(float);
+    const uint32_t lds = kListWords * list_room(a.k) * sizeof(float);
     auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(std::min(a.n, 1u << 20)), dim3(kLongBlock), lds, stream, a, z, d); };
     if (past)
       go(distill_long_kernel<T, LOSS, GRAD, true, false>);

@@ -778,3 +778,21 @@ def test_local_step_example():
 
     losses = ex.run(rounds=6, clients=3, n=200, vocab=300, dim=32, k=8, say=lambda text: None)
     assert losses[-1] < losses[0]
+
+
+@gpu
+@pytest.mark.parametrize("n,vocab", [(300, 1000), (1100, 9001), (600, 66000), (520, 131071)])
+@pytest.mark.parametrize("k", [1, 6, 63, 130])
+def test_distill_of_lists_with_repeated_entries(n, vocab, k):
+    """Lists of lengths that are no multiple of four, most of whose entries share their ids; sampled rows."""
+    g = torch.Generator(device=DEV).manual_seed(108)
+    logits = torch.randn(n, vocab, generator=g, device=DEV).bfloat16()
+    ids = torch.randint(max(1, k // 3), (n, k), generator=g, device=DEV, dtype=torch.int32) * (vocab // k)
+    ids[:, 0] = vocab - 1
+    values = torch.randn(n, k, generator=g, device=DEV)
+    d, loss = torch.empty_like(logits), torch.empty(n, device=DEV)
+    cv.distill(logits, ids, values, loss, cv.new_workspace(cv.distill_workspace_bytes(n, vocab), DEV), temperature=1.5, dlogits=d)
+    some = torch.tensor([0, 1, n // 2, n - 1], device=DEV)
+    want = ref.distill(f64(logits[some]), ids[some].cpu().numpy(), f64(values[some]), T=1.5)
+    assert_near(loss[some], want[0], want[1])
+    assert_near(d[some], want[4], want[5], BF16)
