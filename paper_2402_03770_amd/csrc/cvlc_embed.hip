@@ -278,8 +278,8 @@ struct SumArgs {
   float* part;  // [chunks][2][dim]: a token from the chunk before, and one that goes on in the chunk after
 };
 
-// Bound by HBM: 131072 tokens, as many rows of 2048 bf16, 230 us for 0.8 GB; with chunks of 64 and writes through the caches
-// 245, and 40000 tokens of 1000 fp32 346 us in all, now 295.
+// Bound by HBM: 131072 tokens, as many rows of 2048 bf16, 186 us for 0.77 GB, 4.1 TB/s; with chunks of 64 and accesses in the
+// caches' order 246, and 40000 tokens of 1000 fp32 346 us in all, now 295.
 template <class T, bool ONCE>
 __global__ __launch_bounds__(kEmbedBlock) void sum_kernel(SumArgs a, const T* dout) {
   constexpr uint32_t N = kPerAccess<T>;
@@ -334,48 +334,51 @@ constexpr uint32_t kJoinWaves = kEmbedBlock / kWave;
 __global__ __launch_bounds__(kEmbedBlock) void join_kernel(SumArgs a) {
   constexpr uint32_t N = kPerAccess<float>;
   __shared__ float sums[kJoinWaves][N][kWave];
-  const uint32_t chunk = blockIdx.x, from = chunk * kChunk, to = from + kChunk, dim = a.table.dim;
-  if (to >= a.n) return;
-  const uint32_t token = a.sorted[to - 1].x;
-  if (token >= a.table.vocab || a.sorted[to].x != token) return;
-  if (a.sorted[from].x == token && from && a.sorted[from - 1].x == token) return;  // began earlier
-  uint32_t more = 0;  // chunks it goes on in
-  for (uint32_t base = chunk + 1; base < a.chunks; base += kWave) {
-    const uint32_t c = base + lane_id();
-    const uint64_t stays = __ballot(c < a.chunks && a.sorted[(uint64_t)min(c, a.chunks - 1) * kChunk].x == token);
-    more += (uint32_t)__popcll(stays);
-    if (stays != ~0ull) break;
-  }
-  const uint32_t first = (uint32_t)((uint64_t)more * wave_id() / kJoinWaves), last = (uint32_t)((uint64_t)more * (wave_id() + 1) / kJoinWaves);
-  for (uint32_t base = blockIdx.y * kWave * N; base < dim; base += gridDim.y * kWave * N) {
-    const uint32_t at = base + lane_id() * N;
-    float s[N] = {};
-    if (wave_id() == 0) load_row<N>(a.part + ((uint64_t)chunk * 2 + 1) * dim, at, dim, 0.0f, s);
-    for (uint32_t c = first; c < last; c += kDeep) {
-      Raw<float, N> raw[kDeep];
+  const uint32_t dim = a.table.dim;
+  for (uint32_t chunk = blockIdx.x; chunk < a.chunks; chunk += gridDim.x) {
+    const uint32_t from = chunk * kChunk, to = from + kChunk;
+    if (to >= a.n) return;
+    const uint32_t token = a.sorted[to - 1].x;
+    if (token >= a.table.vocab || a.sorted[to].x != token) continue;
+    if (a.sorted[from].x == token && from && a.sorted[from - 1].x == token) continue;  // began earlier
+    uint32_t more = 0;  // chunks it goes on in
+    for (uint32_t base = chunk + 1; base < a.chunks; base += kWave) {
+      const uint32_t c = base + lane_id();
+      const uint64_t stays = __ballot(c < a.chunks && a.sorted[(uint64_t)min(c, a.chunks - 1) * kChunk].x == token);
+      more += (uint32_t)__popcll(stays);
+      if (stays != ~0ull) break;
+    }
+    const uint32_t first = (uint32_t)((uint64_t)more * wave_id() / kJoinWaves), last = (uint32_t)((uint64_t)more * (wave_id() + 1) / kJoinWaves);
+    for (uint32_t base = blockIdx.y * kWave * N; base < dim; base += gridDim.y * kWave * N) {
+      const uint32_t at = base + lane_id() * N;
+      float s[N] = {};
+      if (wave_id() == 0) load_row<N>(a.part + ((uint64_t)chunk * 2 + 1) * dim, at, dim, 0.0f, s);
+      for (uint32_t c = first; c < last; c += kDeep) {
+        Raw<float, N> raw[kDeep];
 #pragma unroll
-      for (uint32_t u = 0; u < kDeep; ++u)
-        if (c + u < last) load_raw(raw[u], a.part + (uint64_t)(chunk + 1 + c + u) * 2 * dim, at, dim);
+        for (uint32_t u = 0; u < kDeep; ++u)
+          if (c + u < last) load_raw(raw[u], a.part + (uint64_t)(chunk + 1 + c + u) * 2 * dim, at, dim);
 #pragma unroll
-      for (uint32_t u = 0; u < kDeep; ++u) {
-        if (c + u >= last) break;
-        float v[N];
-        raw[u].values(v);
+        for (uint32_t u = 0; u < kDeep; ++u) {
+          if (c + u >= last) break;
+          float v[N];
+          raw[u].values(v);
 #pragma unroll
-        for (uint32_t i = 0; i < N; ++i) s[i] += v[i];
+          for (uint32_t i = 0; i < N; ++i) s[i] += v[i];
+        }
       }
+#pragma unroll
+      for (uint32_t i = 0; i < N; ++i) sums[wave_id()][i][lane_id()] = s[i];
+      __syncthreads();
+      if (wave_id() == 0) {
+#pragma unroll
+        for (uint32_t w = 1; w < kJoinWaves; ++w)
+#pragma unroll
+          for (uint32_t i = 0; i < N; ++i) s[i] += sums[w][i][lane_id()];
+        if (at < dim) write_sum<N>(a.table, token, at, s);
+      }
+      __syncthreads();
     }
-#pragma unroll
-    for (uint32_t i = 0; i < N; ++i) sums[wave_id()][i][lane_id()] = s[i];
-    __syncthreads();
-    if (wave_id() == 0) {
-#pragma unroll
-      for (uint32_t w = 1; w < kJoinWaves; ++w)
-#pragma unroll
-        for (uint32_t i = 0; i < N; ++i) s[i] += sums[w][i][lane_id()];
-      if (at < dim) write_sum<N>(a.table, token, at, s);
-    }
-    __syncthreads();
   }
 }
 
@@ -555,7 +558,8 @@ bool direct_slices(uint32_t n, uint32_t vocab, uint32_t column_blocks, uint32_t*
   uint32_t log = 0;
   while (log < 31 && (2ull << log) <= vocab && ((2ull << log) * column_blocks <= kDirectBlocks || ((uint64_t)kSliceRows << log) < vocab)) ++log;
   *slices_log = log;
-  return ((uint64_t)kSliceRows << log) >= vocab && (1ull << log) * column_blocks * n <= kDirectReads;
+  // (a launch of 2^32 threads and more would start only the rest of that division)
+  return log <= 21 && ((uint64_t)kSliceRows << log) >= vocab && (1ull << log) * column_blocks * n <= kDirectReads;
 }
 
 size_t align256(size_t v) { return (v + 255u) & ~(size_t)255u; }
@@ -709,7 +713,7 @@ int cvlc_embed_grad(uint32_t n, const void* d_ids, uint32_t id_bytes, const void
                        dim3(kEmbedBlock), 0, stream, sa, static_cast<const T*>(d_dout));
   });
   const uint32_t join_columns = kWave * kPerAccess<float>;
-  hipLaunchKernelGGL(join_kernel, dim3(chunks, std::min(dim / join_columns + (dim % join_columns != 0), 65535u)), dim3(kEmbedBlock), 0,
+  hipLaunchKernelGGL(join_kernel, dim3(std::min(chunks, 1u << 20), std::min(dim / join_columns + (dim % join_columns != 0), 65535u)), dim3(kEmbedBlock), 0,
                      stream, sa);
   return hip_check(hipGetLastError());
 }

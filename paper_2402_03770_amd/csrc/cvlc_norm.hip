@@ -390,20 +390,23 @@ __global__ __launch_bounds__(kJoinWaves * kWave) void norm_join_kernel(const flo
   __shared__ float sums[kJoinWaves][kWave];
   float* out = blockIdx.y ? dbeta : dgamma;
   if (!out) return;
-  const uint32_t c = blockIdx.x * kWave + lane_id();
   const uint32_t each = (blocks + kJoinWaves - 1) / kJoinWaves;
-  const uint32_t from = wave_id() * each, to = min(from + each, blocks);
-  float s = 0.0f;
-  if (c < dim)
+  const uint32_t from = min(wave_id() * each, blocks), to = min(from + each, blocks);
+  for (uint32_t first = blockIdx.x * kWave; first < dim; first += gridDim.x * kWave) {
+    const uint32_t c = first + lane_id();
+    float s = 0.0f;
+    if (c < dim)
 #pragma unroll 8
-    for (uint32_t b = from; b < to; ++b) s += part[(2 * (uint64_t)b + blockIdx.y) * dim + c];
-  sums[wave_id()][lane_id()] = s;
-  __syncthreads();
-  if (wave_id() == 0 && c < dim) {
-    s = add ? out[c] : 0.0f;
+      for (uint32_t b = from; b < to; ++b) s += part[(2 * (uint64_t)b + blockIdx.y) * dim + c];
+    sums[wave_id()][lane_id()] = s;
+    __syncthreads();
+    if (wave_id() == 0 && c < dim) {
+      s = add ? out[c] : 0.0f;
 #pragma unroll
-    for (uint32_t w = 0; w < kJoinWaves; ++w) s += sums[w][lane_id()];
-    out[c] = s;
+      for (uint32_t w = 0; w < kJoinWaves; ++w) s += sums[w][lane_id()];
+      out[c] = s;
+    }
+    __syncthreads();
   }
 }
 
@@ -515,7 +518,7 @@ int cvlc_layer_norm_grad(uint32_t n, uint32_t dim, const void* d_dy, uint32_t dy
                            static_cast<TX*>(d_dx));
     });
   if (d_dgamma || d_dbeta)
-    hipLaunchKernelGGL(norm_join_kernel, dim3((dim + kWave - 1) / kWave, 2), dim3(kJoinWaves * kWave), 0, stream, part, blocks, dim,
+    hipLaunchKernelGGL(norm_join_kernel, dim3(std::min((dim + kWave - 1) / kWave, 1u << 20), 2), dim3(kJoinWaves * kWave), 0, stream, part, blocks, dim,
                        flags & CVLC_GRAD_ACCUMULATE, d_dgamma, d_dbeta);
   return launched();
 }

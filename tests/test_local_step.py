@@ -796,3 +796,17 @@ def test_distill_of_lists_with_repeated_entries(n, vocab, k):
     want = ref.distill(f64(logits[some]), ids[some].cpu().numpy(), f64(values[some]), T=1.5)
     assert_near(loss[some], want[0], want[1])
     assert_near(d[some], want[4], want[5], BF16)
+
+
+@gpu
+@pytest.mark.parametrize("vocab", [536_870_912, 600_000_001])
+def test_embed_grad_into_a_very_long_table(vocab):
+    """One side and the other of the most rows that a launch has threads for."""
+    ids = torch.tensor([vocab - 1, 3, vocab, 3, -1])
+    dout = torch.tensor([[1.0], [2.0], [4.0], [8.0], [16.0]], device=DEV)
+    dtable = torch.full((vocab, 1), 5.0, device=DEV)
+    ws = cv.new_workspace(cv.embed_grad_workspace_bytes(5, vocab, 1), DEV)
+    cv.embed_grad(ids.to(DEV), dout, dtable, ws)
+    assert cv.device_status(ws) == cv.DEV_INDEX
+    assert dtable[3].item() == 10.0 and dtable[vocab - 1].item() == 1.0
+    assert int(torch.count_nonzero(dtable)) == 2
