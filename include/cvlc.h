@@ -351,8 +351,8 @@ int cvlc_embed(uint32_t n, const void* d_ids, uint32_t id_bytes, const void* d_t
 
 /* GPU.  Its gradient: dtable[v,:] = scale * sum of dout[i,:] over the i with
  * id_i = v, taken in ascending order of i (in pieces that are added up in order).
- * Tokens are sorted first, so that a frequent token is no bottleneck.  Every row
- * is written, untouched ones with zeros.
+ * Work is cut by places in the order of tokens, so that a frequent token is no
+ * bottleneck.  Every row is written, untouched ones with zeros.
  *   d_dout     n rows of dim elements of any type
  *   d_dtable   vocab rows of dim fp32
  *   flags      CVLC_GRAD_ACCUMULATE: add to d_dtable instead (its untouched rows
