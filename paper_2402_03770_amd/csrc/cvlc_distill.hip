@@ -51,11 +51,38 @@ struct DistillArgs {
 
 // exp((z - m) / T).  The instruction flushes results below 2^-126, which a sum of at least 1 does not notice.
 __device__ __forceinline__ float exp_part(float z, float m, float c) { return __builtin_amdgcn_exp2f((z - m) * c); }
-// exp((z - m) / T) * scale, where `scaled` is scale * 2^-kLift: lifted into the normal range until the one product that
-// may leave it, so that the smallest gradients are rounded once.
-constexpr float kLift = 32.0f, kUnlift = 0x1p-32f;
-__device__ __forceinline__ float exp_scaled(float z, float m, float c, float scaled) {
-  return scaled * __builtin_amdgcn_exp2f(fmaf(z - m, c, kLift));
+// What a row's exponentials are multiplied by.  Far below the maximum an exponential is lifted by 2^kLift into the
+// normal range until the one product that may leave it, so that the smallest gradients are rounded once.  Next to the
+// maximum that would cost bits (an exponent of 32 and more has a step of 2^-19, 11 roundings of fp32 in the result), so
+// fp32 lifts beyond kFar alone, where the exponent's own step is no finer; 16-bit results do not notice and are spared the
+// choice.
+constexpr float kLift = 32.0f, kUnlift = 0x1p-32f, kFar = -64.0f;
+struct GradScale {
+  float plain, lifted;
+  __device__ __forceinline__ explicit GradScale(float scale) : plain(scale), lifted(scale * kUnlift) {}
+};
+// v becomes exp((v - m) / T) * scale, for results of type T
+template <class T, uint32_t N>
+__device__ __forceinline__ void exp_scaled(float (&v)[N], float m, float c, GradScale s) {
+  if constexpr (sizeof(T) == 4) {
+    float least = INFINITY;
+#pragma unroll
+    for (uint32_t i = 0; i < N; ++i) {
+      v[i] = (v[i] - m) * c;
+      least = fminf(least, v[i]);
+    }
+    if (least < kFar) {  // asked once for all of them: a choice for each took 2 % of the call
+#pragma unroll
+      for (uint32_t i = 0; i < N; ++i)
+        v[i] = (v[i] < kFar ? s.lifted : s.plain) * __builtin_amdgcn_exp2f(v[i] < kFar ? v[i] + kLift : v[i]);
+    } else {
+#pragma unroll
+      for (uint32_t i = 0; i < N; ++i) v[i] = s.plain * __builtin_amdgcn_exp2f(v[i]);
+    }
+  } else {
+#pragma unroll
+    for (uint32_t i = 0; i < N; ++i) v[i] = s.lifted * __builtin_amdgcn_exp2f(fmaf(v[i] - m, c, kLift));
+  }
 }
 
 // A maximum and the sum of exponentials relative to it.
@@ -190,7 +217,9 @@ __device__ __forceinline__ void write_listed(const DistillArgs& a, const ListLds
     p += ids.w == id ? ps.w : 0.0f;
   }
   const float inv = t.s == 0.0f ? 0.0f : 1.0f / t.s;
-  drow[id] = (T)(wT * (exp_scaled(l.z[j], t.m, a.c, P * inv * kUnlift) - p));
+  float q[1] = {l.z[j]};
+  exp_scaled<T>(q, t.m, a.c, GradScale(P * inv));
+  drow[id] = (T)(wT * (q[0] - p));
 }
 
 template <uint32_t W>
@@ -326,7 +355,7 @@ __global__ __launch_bounds__((W == 1 ? 4 : W) * kWave, O) void distill_rows_kern
     if (load_next && has_entry) entry.load(a, next, lane);
     if (GRAD || w == 0.0f) {
       T* dr = GRAD ? dlogits + row * a.dstride : nullptr;
-      const float scale = P == 0.0f || t.s == 0.0f ? 0.0f : w * a.T * P * (1.0f / t.s) * kUnlift;
+      const GradScale scale(P == 0.0f || t.s == 0.0f ? 0.0f : w * a.T * P * (1.0f / t.s));
       const bool nothing = P == 0.0f;
 #pragma unroll
       for (uint32_t j = 0; j < V; ++j) {
@@ -335,8 +364,9 @@ __global__ __launch_bounds__((W == 1 ? 4 : W) * kWave, O) void distill_rows_kern
         if constexpr (GRAD) {
           float v[N];
           raw[j].values(v);
+          exp_scaled<T>(v, t.m, a.c, scale);
 #pragma unroll
-          for (uint32_t i = 0; i < N; ++i) v[i] = nothing ? 0.0f : exp_scaled(v[i], t.m, a.c, scale);
+          for (uint32_t i = 0; i < N; ++i) v[i] = nothing ? 0.0f : v[i];
           if (first + N <= a.vocab)
             store_whole<ONCE, N>(dr + first, v);
           else
@@ -448,10 +478,9 @@ __device__ __forceinline__ void write_gradient(const DistillArgs& a, const T* zr
     for (uint64_t first = from + threadIdx.x * N; first < to; first += kLongBlock * N) store_part<ONCE, N>(dr, (uint32_t)first, to, zero);
     return;
   }
-  const float scale = t.s == 0.0f ? 0.0f : wT * P * (1.0f / t.s) * kUnlift;
+  const GradScale scale(t.s == 0.0f ? 0.0f : wT * P * (1.0f / t.s));
   over_row<ONCE>(zr, from, to, [&](uint32_t first, float (&v)[N]) {
-#pragma unroll
-    for (uint32_t i = 0; i < N; ++i) v[i] = exp_scaled(v[i], t.m, a.c, scale);
+    exp_scaled<T>(v, t.m, a.c, scale);
     store_part<ONCE, N>(dr, first, to, v);
   });
 }

@@ -1,0 +1,60 @@
+"""The local step's operators where one kernel takes over from another: bits of the smallest results, the largest calls,
+places of one call in another's buffers.  Against the same formulas in 64 bits, as tests/test_local_step.py.
+"""
+import numpy as np
+import pytest
+import torch
+
+import paper_2402_03770_amd.cvlc as cv
+from oracle import local_step as ref
+
+DEV = "cuda:0"
+F32, BF16, F16 = torch.float32, torch.bfloat16, torch.float16
+gpu = pytest.mark.gpu
+
+
+def f64(t):
+    return t.detach().cpu().to(torch.float64).numpy()
+
+
+def uniform(rows, width, low, high, seed, dtype=F32):
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    return (low + (high - low) * torch.rand(rows, width, generator=g, device=DEV)).to(dtype)
+
+
+def workspace(n, vocab):
+    return cv.new_workspace(cv.distill_workspace_bytes(n, vocab), DEV)
+
+
+# a wavefront per row, several, a row that the registers do not hold, one of few that is cut into parts
+ROWS = [(300, 100), (40, 3001), (600, 20001), (520, 70001), (3, 100000)]
+
+
+def both_gradients(logits, ids, values, T, weights=None, **more):
+    """The gradient in the loss's pass, and alone from the kept statistics."""
+    n, vocab = logits.shape
+    fused, alone, stats, loss = torch.empty_like(logits), torch.empty_like(logits), torch.empty(n, 2, device=DEV), torch.empty(n, device=DEV)
+    cv.distill(logits, ids, values, loss, workspace(n, vocab), temperature=T, weights=weights, dlogits=fused, stats_out=stats, **more)
+    cv.distill_grad(logits, ids, values, stats, alone, temperature=T, weights=weights, **more)
+    return fused, alone
+
+
+@gpu
+@pytest.mark.parametrize("n,vocab", ROWS)
+@pytest.mark.parametrize("T,spread", [(1.0, 0.25), (2.0, 0.25), (0.5, 110.0)])
+def test_distill_gradient_keeps_the_bits_of_fp32(n, vocab, T, spread):
+    """Two unlisted places of a row differ by exp((z - z') / T) alone, whatever the row's sum: next to the maximum, and down
+    to the smallest results."""
+    logits = uniform(n, vocab, 0.0, spread * T, 1)
+    logits[:, 0] = spread * T                                # the row's maximum
+    ids, values = torch.full((n, 1), vocab - 1, dtype=torch.int32, device=DEV), torch.zeros(n, 1, device=DEV)
+    some = [0, n // 2, n - 1]
+    z = f64(logits[some])
+    arg = (z - z[:, :1]) / T
+    for got in both_gradients(logits, ids, values, T):
+        g = f64(got[some])
+        want = g[:, :1] * np.exp(arg)
+        # (z - m), 1 / T and their product rounded, 1 ulp of the exponential, the product with the row's scale; the maximum's
+        # own entry has the last two; a result below the normal ones is rounded to half the smallest
+        tol = (3 * np.abs(arg) + 7) * ref.U * want + 2.0 ** -150
+        assert np.all(np.abs(g - want)[:, :-1] <= tol[:, :-1]), float(((np.abs(g - want) - 2.0 ** -150) / want / ref.U)[:, :-1].max())
