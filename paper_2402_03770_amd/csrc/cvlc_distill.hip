@@ -55,15 +55,22 @@ __device__ __forceinline__ float exp_part(float z, float m, float c) { return __
 // normal range until the one product that may leave it, so that the smallest gradients are rounded once.  Next to the
 // maximum that would cost bits (an exponent of 32 and more has a step of 2^-19, 11 roundings of fp32 in the result), so
 // fp32 lifts beyond kFar alone, where the exponent's own step is no finer; 16-bit results do not notice and are spared the
-// choice.
-constexpr float kLift = 32.0f, kUnlift = 0x1p-32f, kFar = -64.0f;
+// choice.  They do not lift a scale below kTiny: it would become subnormal and lose its bits, and what it makes of an
+// exponential that needs a lift is 0.
+constexpr float kLift = 32.0f, kUnlift = 0x1p-32f, kFar = -64.0f, kTiny = 0x1p-24f;
+template <class T>
 struct GradScale {
-  float plain, lifted;
-  __device__ __forceinline__ explicit GradScale(float scale) : plain(scale), lifted(scale * kUnlift) {}
+  float plain, lift, lifted;
+  __device__ __forceinline__ explicit GradScale(float scale) : plain(scale), lift(kLift), lifted(scale * kUnlift) {
+    if (sizeof(T) < 4 && fabsf(scale) < kTiny) {
+      lift = 0.0f;
+      lifted = scale;
+    }
+  }
 };
 // v becomes exp((v - m) / T) * scale, for results of type T
 template <class T, uint32_t N>
-__device__ __forceinline__ void exp_scaled(float (&v)[N], float m, float c, GradScale s) {
+__device__ __forceinline__ void exp_scaled(float (&v)[N], float m, float c, GradScale<T> s) {
   if constexpr (sizeof(T) == 4) {
     float least = INFINITY;
 #pragma unroll
@@ -74,14 +81,14 @@ __device__ __forceinline__ void exp_scaled(float (&v)[N], float m, float c, Grad
     if (least < kFar) {  // asked once for all of them: a choice for each took 2 % of the call
 #pragma unroll
       for (uint32_t i = 0; i < N; ++i)
-        v[i] = (v[i] < kFar ? s.lifted : s.plain) * __builtin_amdgcn_exp2f(v[i] < kFar ? v[i] + kLift : v[i]);
+        v[i] = (v[i] < kFar ? s.lifted : s.plain) * __builtin_amdgcn_exp2f(v[i] < kFar ? v[i] + s.lift : v[i]);
     } else {
 #pragma unroll
       for (uint32_t i = 0; i < N; ++i) v[i] = s.plain * __builtin_amdgcn_exp2f(v[i]);
     }
   } else {
 #pragma unroll
-    for (uint32_t i = 0; i < N; ++i) v[i] = s.lifted * __builtin_amdgcn_exp2f(fmaf(v[i] - m, c, kLift));
+    for (uint32_t i = 0; i < N; ++i) v[i] = s.lifted * __builtin_amdgcn_exp2f(fmaf(v[i] - m, c, s.lift));
   }
 }
 
@@ -218,7 +225,7 @@ __device__ __forceinline__ void write_listed(const DistillArgs& a, const ListLds
   }
   const float inv = t.s == 0.0f ? 0.0f : 1.0f / t.s;
   float q[1] = {l.z[j]};
-  exp_scaled<T>(q, t.m, a.c, GradScale(P * inv));
+  exp_scaled<T>(q, t.m, a.c, GradScale<T>(P * inv));
   drow[id] = (T)(wT * (q[0] - p));
 }
 
@@ -355,7 +362,7 @@ __global__ __launch_bounds__((W == 1 ? 4 : W) * kWave, O) void distill_rows_kern
     if (load_next && has_entry) entry.load(a, next, lane);
     if (GRAD || w == 0.0f) {
       T* dr = GRAD ? dlogits + row * a.dstride : nullptr;
-      const GradScale scale(P == 0.0f || t.s == 0.0f ? 0.0f : w * a.T * P * (1.0f / t.s));
+      const GradScale<T> scale(P == 0.0f || t.s == 0.0f ? 0.0f : w * a.T * P * (1.0f / t.s));
       const bool nothing = P == 0.0f;
 #pragma unroll
       for (uint32_t j = 0; j < V; ++j) {
@@ -478,7 +485,7 @@ __device__ __forceinline__ void write_gradient(const DistillArgs& a, const T* zr
     for (uint64_t first = from + threadIdx.x * N; first < to; first += kLongBlock * N) store_part<ONCE, N>(dr, (uint32_t)first, to, zero);
     return;
   }
-  const GradScale scale(t.s == 0.0f ? 0.0f : wT * P * (1.0f / t.s));
+  const GradScale<T> scale(t.s == 0.0f ? 0.0f : wT * P * (1.0f / t.s));
   over_row<ONCE>(zr, from, to, [&](uint32_t first, float (&v)[N]) {
     exp_scaled<T>(v, t.m, a.c, scale);
     store_part<ONCE, N>(dr, first, to, v);

@@ -58,3 +58,39 @@ def test_distill_gradient_keeps_the_bits_of_fp32(n, vocab, T, spread):
         # own entry has the last two; a result below the normal ones is rounded to half the smallest
         tol = (3 * np.abs(arg) + 7) * ref.U * want + 2.0 ** -150
         assert np.all(np.abs(g - want)[:, :-1] <= tol[:, :-1]), float(((np.abs(g - want) - 2.0 ** -150) / want / ref.U)[:, :-1].max())
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n,vocab", ROWS)
+@pytest.mark.parametrize("weight", [1e-28, -1e-33, 3e-37])
+def test_distill_gradient_of_tiny_weights(n, vocab, dtype, weight):
+    """A weight scales the gradient and costs none of its bits, as long as the results are normal numbers."""
+    logits = uniform(n, vocab, -2.0, 2.0, 2, dtype)
+    ids = torch.tensor([[1, vocab - 1, 1]], dtype=torch.int64, device=DEV).expand(n, 3).contiguous()
+    values = uniform(n, 3, 0.0, 2.0, 3)
+    some = [0, n - 1]
+    w = np.full(2, float(np.float32(weight)))
+    want, tol = ref.distill(f64(logits[some]), ids[some].cpu().numpy(), f64(values[some]), T=1.0, weights=w)[4:]
+    tol = tol + ref.half_step(np.abs(want) + tol, torch.finfo(dtype).eps, 2.0 ** -149 if dtype == F32 else 2.0 ** -133) + 2.0 ** -149
+    # (a row's scale may lie below the normal numbers itself, and so may its product)
+    for got in both_gradients(logits, ids, values, 1.0, weights=torch.full((n,), weight, device=DEV)):
+        err = np.abs(f64(got[some]) - want)
+        assert np.all(err <= tol), float((err / np.abs(want)).max())
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n,vocab", ROWS)
+def test_distill_gradient_of_a_tiny_share(n, vocab, dtype):
+    """Log-probabilities whose sum P is tiny: P q keeps its bits at listed places and at the others."""
+    logits = uniform(n, vocab, -2.0, 2.0, 4, dtype)
+    ids = torch.tensor([[1, vocab - 1]], dtype=torch.int32, device=DEV).expand(n, 2).contiguous()
+    values = torch.full((n, 2), -70.0, device=DEV)
+    values[:, 1] = -80.0                                      # P is 4e-31: 1 / S and 2^-32 more would leave the normal range
+    some = [0, n - 1]
+    want, tol = ref.distill(f64(logits[some]), ids[some].cpu().numpy(), f64(values[some]), T=1.0, logprobs=True)[4:]
+    tol = tol + ref.half_step(np.abs(want) + tol, torch.finfo(dtype).eps, 2.0 ** -149 if dtype == F32 else 2.0 ** -133)
+    for got in both_gradients(logits, ids, values, 1.0, logprobs=True):
+        err = np.abs(f64(got[some]) - want)
+        assert np.all(err <= tol), float((err / np.abs(want)).max())
