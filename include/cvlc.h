@@ -435,7 +435,8 @@ int cvlc_distill(uint32_t n, uint32_t vocab, const void* d_logits, uint32_t type
 
 /* GPU.  The gradient alone, from the statistics of an earlier cvlc_distill on the
  * same logits, lists, temperature and flags; the weights may be others (a mean
- * over a count known only then), but a row that had none has no statistics. */
+ * over a count known only then), but a row that had none has no statistics.
+ * d_dlogits may be d_logits (same stride).  Arguments otherwise as there. */
 int cvlc_distill_grad(uint32_t n, uint32_t vocab, const void* d_logits, uint32_t type, uint64_t stride,
                       uint32_t k, const void* d_ids, uint32_t id_bytes, const void* d_values,
                       uint32_t value_type, float temperature, uint32_t flags, const float* d_weights,

@@ -551,7 +551,8 @@ def distill(logits: torch.Tensor, teacher_ids: torch.Tensor, teacher_values: tor
 def distill_grad(logits: torch.Tensor, teacher_ids: torch.Tensor, teacher_values: torch.Tensor, stats: torch.Tensor,
                  dlogits: torch.Tensor, temperature: float = 1.0, weights: Optional[torch.Tensor] = None,
                  logprobs: bool = False, status: Optional[torch.Tensor] = None) -> None:
-    """cvlc_distill_grad on the current stream: the gradient from the statistics that distill kept."""
+    """cvlc_distill_grad on the current stream: the gradient (`dlogits`, the logits' type; may be `logits` itself) from the
+    statistics that distill kept."""
     what = "cvlc_distill_grad"
     n, vocab, k, size, kind = _lists(what, logits, teacher_ids, teacher_values)
     zp, zt, zs = _matrix(what, "logits", logits, n, vocab)

@@ -94,3 +94,27 @@ def test_distill_gradient_of_a_tiny_share(n, vocab, dtype):
     for got in both_gradients(logits, ids, values, 1.0, logprobs=True):
         err = np.abs(f64(got[some]) - want)
         assert np.all(err <= tol), float((err / np.abs(want)).max())
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [F32, F16])
+@pytest.mark.parametrize("n,vocab", ROWS)
+def test_distill_grad_in_place(n, vocab, dtype):
+    """The gradient alone may take the logits' place: the same bits as beside them; rows without weight are zeros."""
+    logits = uniform(n, vocab, -3.0, 3.0, 5, dtype)
+    g = torch.Generator(device=DEV).manual_seed(6)
+    # every part of a row has listed places, some of them listed twice
+    ids = torch.randint(vocab, (n, 33), generator=g, device=DEV)
+    ids[:, 20:] = ids[:, :13]
+    values, weights = uniform(n, 33, 0.0, 3.0, 7), uniform(n, 1, 0.5, 1.0, 8)[:, 0].contiguous()
+    weights[1] = 0.0
+    stats, loss, beside = torch.empty(n, 2, device=DEV), torch.empty(n, device=DEV), torch.empty_like(logits)
+    cv.distill(logits, ids, values, loss, workspace(n, vocab), temperature=1.5, weights=weights, stats_out=stats)
+    cv.distill_grad(logits, ids, values, stats, beside, temperature=1.5, weights=weights)
+    some = [0, 1, n - 1]
+    want, tol = ref.distill(f64(logits[some]), ids[some].cpu().numpy(), f64(values[some]), T=1.5, weights=f64(weights[some]))[4:]
+    cv.distill_grad(logits, ids, values, stats, logits, temperature=1.5, weights=weights)
+    assert torch.equal(logits, beside)
+    tol = tol + ref.half_step(np.abs(want) + tol, torch.finfo(dtype).eps, 2.0 ** -149 if dtype == F32 else 2.0 ** -24)
+    assert np.all(np.abs(f64(logits[some]) - want) <= tol)
+    assert not bool(logits[1].any())
