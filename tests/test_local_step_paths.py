@@ -118,3 +118,103 @@ def test_distill_grad_in_place(n, vocab, dtype):
     tol = tol + ref.half_step(np.abs(want) + tol, torch.finfo(dtype).eps, 2.0 ** -149 if dtype == F32 else 2.0 ** -24)
     assert np.all(np.abs(f64(logits[some]) - want) <= tol)
     assert not bool(logits[1].any())
+
+
+def near(got, want, tol, dtype=F32):
+    """Within `tol` and half a step of the type; equal where the value is infinite."""
+    got = f64(got)
+    fine = np.isfinite(want)
+    assert got.shape == want.shape and np.array_equal(got[~fine], want[~fine], equal_nan=True)
+    smallest = {F32: 2.0 ** -149, BF16: 2.0 ** -133, F16: 2.0 ** -24}[dtype]
+    tol = tol[fine] + ref.half_step(np.abs(want[fine]) + tol[fine], torch.finfo(dtype).eps, smallest)
+    assert np.all(np.abs(got[fine] - want[fine]) <= tol), float((np.abs(got[fine] - want[fine]) - tol).max())
+
+
+def spread_lists(n, vocab, k, seed):
+    """Lists over the whole vocabulary, an eighth of whose entries repeat others."""
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    ids = torch.randint(vocab, (n, k), generator=g, device=DEV, dtype=torch.int32)
+    if k >= 8:
+        ids[:, -(k // 8):] = ids[:, :k // 8]
+    return ids, 3.0 * torch.randn(n, k, generator=g, device=DEV)
+
+
+def check_all(logits, ids, values, T, some, weights=None):
+    """Loss alone, gradient alone, both together, and both in place, at sampled rows."""
+    n, vocab = logits.shape
+    w = None if weights is None else f64(weights[some])
+    loss, loss_tol, stats, stats_tol, grad, grad_tol = ref.distill(f64(logits[some]), ids[some].cpu().numpy(), f64(values[some]), T=T, weights=w)
+    ws, got_loss, got_stats = workspace(n, vocab), torch.full((n,), 11.0, device=DEV), torch.full((n, 2), 11.0, device=DEV)
+    ws.fill_(0xA5)
+    cv.distill(logits, ids, values, got_loss, ws, temperature=T, weights=weights, stats_out=got_stats)
+    near(got_loss[some], loss, loss_tol)
+    near(got_stats[some], stats, stats_tol)
+    d = torch.full_like(logits, 13.0)
+    cv.distill_grad(logits, ids, values, got_stats, d, temperature=T, weights=weights)
+    near(d[some], grad, grad_tol, logits.dtype)
+    d.fill_(13.0)
+    got_loss.fill_(11.0)
+    cv.distill(logits, ids, values, got_loss, ws, temperature=T, weights=weights, dlogits=d)
+    near(got_loss[some], loss, loss_tol)
+    near(d[some], grad, grad_tol, logits.dtype)
+    again = torch.empty_like(got_loss)
+    cv.distill(logits, ids, values, again, ws, temperature=T, weights=weights, dlogits=logits)
+    assert torch.equal(again, got_loss) and torch.equal(logits, d)
+
+
+@gpu
+@pytest.mark.parametrize("n,vocab,dtype", [(520, 70001, F32), (513, 262144, BF16), (1100, 140001, F16)])
+def test_distill_of_many_rows_beyond_the_registers(n, vocab, dtype):
+    """Rows that one workgroup goes over in passes; the larger two of them past the caches' order."""
+    logits = uniform(n, vocab, -4.0, 4.0, 10, dtype)
+    logits[:, vocab // 3] = float("-inf")
+    ids, values = spread_lists(n, vocab, 70, 11)
+    check_all(logits, ids, values, 1.5, [0, 1, n // 2, n - 1])
+
+
+@gpu
+@pytest.mark.parametrize("n,vocab,dtype", [(9000, 15003, BF16), (700_000, 100, F32), (70_000, 1000, F32), (1000, 66001, F32)])
+def test_distill_of_more_than_the_caches_hold(n, vocab, dtype):
+    """Short rows and long ones, read and written past the caches' order."""
+    logits = uniform(n, vocab, -4.0, 4.0, 12, dtype)
+    ids, values = spread_lists(n, vocab, 9, 13)
+    check_all(logits, ids, values, 2.0, [0, 1, 4095, n // 2, n - 2, n - 1] if n > 4095 else [0, 1, n - 1])
+
+
+@gpu
+@pytest.mark.parametrize("k", [681, 682, 683, 1000, 1024])
+@pytest.mark.parametrize("n,vocab", [(700, 62), (300, 900), (2000, 1030), (30, 5000)])
+def test_distill_of_long_lists_on_short_rows(n, vocab, k):
+    """Four rows' lists to a workgroup, in up to 96 KB of LDS."""
+    logits = uniform(n, vocab, -4.0, 4.0, 14, BF16)
+    ids, values = spread_lists(n, vocab, k, 15)
+    check_all(logits, ids, values, 2.0, [0, 1, 2, 3, n - 2, n - 1])
+
+
+@gpu
+@pytest.mark.parametrize("n,vocab", ROWS)
+def test_distill_reads_nothing_of_rows_without_weight(n, vocab):
+    """Logits, lists and statistics of such rows hold NaN and numbers beyond the vocabulary: zeros, and no bit of the status."""
+    logits = uniform(n, vocab, -4.0, 4.0, 16, BF16)
+    ids, values = spread_lists(n, vocab, 12, 17)
+    weights = torch.ones(n, device=DEV)
+    weights[::3] = 0.0
+    lost = weights == 0.0
+    logits[lost], values[lost], ids[lost] = float("nan"), float("nan"), 1 << 30
+    status, ws = torch.zeros(1, dtype=torch.int32, device=DEV), workspace(n, vocab)
+    loss, stats = torch.full((n,), 11.0, device=DEV), torch.full((n, 2), 11.0, device=DEV)
+    cv.distill(logits, ids, values, loss, ws, weights=weights, stats_out=stats, status=status)
+    stats_lost = stats[lost].clone()
+    stats[lost] = float("nan")
+    alone, fused, loss2 = torch.full_like(logits, 13.0), torch.full_like(logits, 13.0), torch.full((n,), 11.0, device=DEV)
+    cv.distill_grad(logits, ids, values, stats, alone, weights=weights, status=status)
+    cv.distill(logits, ids, values, loss2, ws, weights=weights, dlogits=fused, status=status)
+    for zeros in (loss[lost], loss2[lost], stats_lost, alone[lost], fused[lost]):
+        assert not bool(zeros.any())
+    assert status.item() == 0
+    some = [1, 2] + ([n - 2] if (n - 2) % 3 else [])
+    want = ref.distill(f64(logits[some]), ids[some].cpu().numpy(), f64(values[some]))
+    near(loss[some], want[0], want[1])
+    near(loss2[some], want[0], want[1])
+    near(alone[some], want[4], want[5], BF16)
+    near(fused[some], want[4], want[5], BF16)
