@@ -218,3 +218,109 @@ def test_distill_reads_nothing_of_rows_without_weight(n, vocab):
     near(loss2[some], want[0], want[1])
     near(alone[some], want[4], want[5], BF16)
     near(fused[some], want[4], want[5], BF16)
+
+
+# ----------------------------------------------------------------------------- embedding
+def text(n, vocab, seed, beyond=0):
+    """Tokens of which the low ones are frequent, a tenth padding, `beyond` of them beyond the vocabulary."""
+    rng = np.random.default_rng(seed)
+    ids = np.minimum((np.exp(rng.random(n) * np.log(vocab + 1.0)) - 1).astype(np.int64), vocab - 1)
+    ids[rng.random(n) < 0.1] = -1
+    ids[rng.choice(n, beyond, replace=False)] = vocab
+    ids[0] = ids[n // 2] = ids[n - 1] = vocab - 1             # the last digit's largest value, from several tiles
+    return torch.from_numpy(ids).to(DEV)
+
+
+def check_embed_grad(ids, dout, vocab, scale, status, start=None):
+    """Against sums in 64 bits on the GPU; twice, bit for bit."""
+    n, dim = dout.shape
+    ws = cv.new_workspace(cv.embed_grad_workspace_bytes(n, vocab, dim), DEV)
+    got = []
+    for _ in range(2):
+        ws.fill_(0xA5)
+        dtable = torch.full((vocab, dim), 5.0, device=DEV) if start is None else start.clone()
+        cv.embed_grad(ids, dout, dtable, ws, scale=scale, accumulate=start is not None)
+        assert cv.device_status(ws) == status
+        got.append(dtable)
+    assert torch.equal(*got)
+    del got
+    there = (ids >= 0) & (ids < vocab)
+    rows, where = torch.unique(ids[there], return_inverse=True)
+    want, size = torch.zeros(2, rows.numel(), dim, dtype=torch.float64, device=DEV)
+    part = max(1, (1 << 26) // dim)                           # rows at a time
+    places = torch.nonzero(there)[:, 0]
+    for b in range(0, places.numel(), part):
+        d = dout[places[b:b + part]].double()
+        want.index_add_(0, where[b:b + part], d)
+        size.index_add_(0, where[b:b + part], d.abs())
+    count = torch.bincount(where, minlength=rows.numel())[:, None]
+    want, tol = want * scale, (count + 3) * ref.U * size * abs(scale)
+    if start is not None:
+        want += start[rows].double()
+        tol += want.abs() * ref.U
+    assert bool(((dtable[rows].double() - want).abs() <= tol + 2.0 ** -149).all())
+    rest = torch.ones(vocab, dtype=torch.bool, device=DEV)
+    rest[rows] = False
+    untouched = dtable[rest]
+    assert torch.equal(untouched, start[rest]) if start is not None else not bool(untouched.any())
+
+
+@gpu
+@pytest.mark.parametrize("add", [False, True])
+@pytest.mark.parametrize("n,dim,vocab", [(20_000, 3, 5_000_000), (40_000, 9, 4_194_303), (40_000, 9, 4_194_304), (300_000, 7, 50_000),
+                                         (270_000, 2, 6_000_000), (17_000, 40, 2_000)])
+def test_embed_grad_by_every_number_of_digits(n, dim, vocab, add):
+    """One, two and three passes of the sort over several tiles; tiles counted by every workgroup for itself and, more than
+    64 of them, by a scan between the passes."""
+    g = torch.Generator(device=DEV).manual_seed(20)
+    dout = torch.randn(n, dim, generator=g, device=DEV).to(BF16)
+    start = torch.randn(vocab, dim, generator=g, device=DEV) if add else None
+    check_embed_grad(text(n, vocab, 21, beyond=5), dout, vocab, 0.5, cv.DEV_INDEX, start)
+
+
+@gpu
+@pytest.mark.parametrize("add", [False, True])
+@pytest.mark.parametrize("n,dim,dtype", [(70_000, 1000, F32), (100_001, 1300, BF16), (33_000, 4099, F16)])
+def test_embed_grad_of_more_than_the_caches_hold(n, dim, dtype, add):
+    """Rows read past the caches' order."""
+    g = torch.Generator(device=DEV).manual_seed(22)
+    dout = torch.randn(n, dim, generator=g, device=DEV).to(dtype)
+    vocab = 9000
+    start = torch.randn(vocab, dim, generator=g, device=DEV) if add else None
+    check_embed_grad(text(n, vocab, 23), dout, vocab, 2.0, 0, start)
+
+
+@gpu
+@pytest.mark.parametrize("n", [4096, 16384, 16385])
+@pytest.mark.parametrize("share", [0.5, 1.0])
+@pytest.mark.parametrize("add", [False, True])
+def test_embed_grad_of_one_token_above_all(n, share, add):
+    """A padding or separator token that is a row like any other, for half of the places and for all of them."""
+    g = torch.Generator(device=DEV).manual_seed(24)
+    vocab, dim = 3000, 256
+    dout = torch.randn(n, dim, generator=g, device=DEV).to(BF16)
+    ids = text(n, vocab, 25)
+    ids[torch.rand(n, generator=g, device=DEV) < share] = 11
+    start = torch.randn(vocab, dim, generator=g, device=DEV) if add else None
+    check_embed_grad(ids, dout, vocab, 1.0, 0, start)
+
+
+@gpu
+@pytest.mark.parametrize("types", [(F32, F32), (BF16, BF16), (F16, F16), (F32, BF16), (F32, F16)])
+@pytest.mark.parametrize("n,dim", [(300_001, 100), (70_001, 240), (2_200_003, 5)])
+def test_embed_of_four_rows_to_a_thread(types, n, dim):
+    """More than 8192 workgroups of several rows each; the last ones have fewer."""
+    tt, to = types
+    vocab, scale = 500, 1.5
+    g = torch.Generator(device=DEV).manual_seed(26)
+    table = torch.randn(vocab, dim, generator=g, device=DEV).to(tt)
+    ids = text(n, vocab, 27, beyond=3)
+    flat = torch.full((n * (dim + 1) + 8,), 3.0, dtype=to, device=DEV)
+    out = flat[:n * (dim + 1)].view(n, dim + 1)[:, :dim]
+    status = torch.zeros(1, dtype=torch.int32, device=DEV)
+    cv.embed(ids.int(), table, out, scale=scale, status=status)
+    there = (ids >= 0) & (ids < vocab)
+    want = torch.where(there[:, None], table[ids.clamp(0, vocab - 1)].float() * scale, 0.0).to(to)
+    assert torch.equal(out, want) and status.item() == cv.DEV_INDEX
+    out.fill_(3.0)
+    assert bool((flat == 3.0).all())
