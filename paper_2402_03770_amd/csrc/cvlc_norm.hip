@@ -352,8 +352,8 @@ __global__ __launch_bounds__(S::kThreads, S::O) void norm_grad_rows_kernel(NormA
 // 14.0 and 17.3; 16384 x 4096 49 by one, 52).
 // Calls f with the shape for rows of `dim` elements, `per` of them an access; false: too long for registers, or shorter than
 // an access.
-template <class F>
-bool by_norm_shape(uint32_t n, uint32_t dim, uint32_t per, F f) {
+template <uint32_t per, class F>
+bool by_norm_shape(uint32_t n, uint32_t dim, F f) {
   const uint32_t vectors = (dim + per - 1) / per;
   if (dim < per) return false;
   const bool many = n >= 8192;
@@ -363,14 +363,15 @@ bool by_norm_shape(uint32_t n, uint32_t dim, uint32_t per, F f) {
   if (vectors <= 512) return many ? f(RowShape<1, 8, 1>{}) : f(RowShape<4, 2, 6>{});
   if (vectors <= 1024) return f(RowShape<8, 2, 4>{});
   if (vectors <= 2048) return f(RowShape<8, 4, 2>{});
-  if (vectors <= 4096 && per == 4) return f(RowShape<16, 4, 4>{});
+  if constexpr (per == 4)
+    if (vectors <= 4096) return f(RowShape<16, 4, 4>{});
   return false;
 }
 // Backward a thread holds five values per column (gamma, two sums, h, g), so one access per thread as far as a workgroup
 // goes.  Beyond 8192 fp32 (1024 threads with 16 columns each) the sums over the rows lie in LDS (8192 x 16384 fp32: 280 us,
 // 437 with them in registers that spill).
-template <class F>
-bool by_norm_grad_shape(uint32_t dim, uint32_t per, F f) {
+template <uint32_t per, class F>
+bool by_norm_grad_shape(uint32_t dim, F f) {
   const uint32_t vectors = (dim + per - 1) / per;
   if (dim < per) return false;
   if (vectors <= 64) return f(RowShape<1, 1, 6>{});
@@ -379,7 +380,8 @@ bool by_norm_grad_shape(uint32_t dim, uint32_t per, F f) {
   if (vectors <= 512) return f(RowShape<8, 1, 4>{});
   if (vectors <= 1024) return f(RowShape<16, 1, 4>{});
   if (vectors <= 2048) return f(RowShape<16, 2, 4>{});
-  if (vectors <= 4096 && per == 4) return f(RowShape<16, 4, 4, true>{});
+  if constexpr (per == 4)
+    if (vectors <= 4096) return f(RowShape<16, 4, 4, true>{});
   return false;
 }
 
@@ -445,7 +447,7 @@ int cvlc_layer_norm(uint32_t n, uint32_t dim, const void* d_x, uint32_t x_type, 
   by_types(x_type, y_type, [&](auto tx, auto ty) {
     using TX = decltype(tx);
     using TY = decltype(ty);
-    if (by_norm_shape(n, dim, kPerAccess<TX, TY>, [&](auto shape) {
+    if (by_norm_shape<kPerAccess<TX, TY>>(n, dim, [&](auto shape) {
           using S = decltype(shape);
           hipLaunchKernelGGL((past ? norm_rows_kernel<TX, TY, S, true> : norm_rows_kernel<TX, TY, S, false>),
                              dim3(std::min((n + S::kRows - 1) / S::kRows, 256u * S::kPerCu)), dim3(S::kThreads), 0,
@@ -499,7 +501,7 @@ int cvlc_layer_norm_grad(uint32_t n, uint32_t dim, const void* d_dy, uint32_t dy
       using TY = decltype(ty);
       const TX* x = static_cast<const TX*>(d_x);
       const TY* dy = static_cast<const TY*>(d_dy);
-      if (by_norm_grad_shape(dim, kPerAccess<TX, TY>, [&](auto shape) {
+      if (by_norm_grad_shape<kPerAccess<TX, TY>>(dim, [&](auto shape) {
             using S = decltype(shape);
             blocks = std::min({(n + S::kRows - 1) / S::kRows, 256u * S::kPerCu, partials(n)});
             constexpr uint32_t lds = S::LDS || S::kRows > 1 ? 2 * S::V * kPerAccess<TX, TY> * S::W * kWave * sizeof(float) : 0;

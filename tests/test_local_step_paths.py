@@ -1,6 +1,8 @@
 """The local step's operators where one kernel takes over from another: bits of the smallest results, the largest calls,
 places of one call in another's buffers.  Against the same formulas in 64 bits, as tests/test_local_step.py.
 """
+import re
+
 import numpy as np
 import pytest
 import torch
@@ -324,3 +326,13 @@ def test_embed_of_four_rows_to_a_thread(types, n, dim):
     assert torch.equal(out, want) and status.item() == cv.DEV_INDEX
     out.fill_(3.0)
     assert bool((flat == 3.0).all())
+
+
+# ----------------------------------------------------------------------------- layer norm
+def test_norm_shapes_are_those_that_calls_reach():
+    """Rows of 16384 values are the longest in registers: 4 accesses for each of 1024 threads where an access holds four
+    values.  Where it holds eight (both types of 16 bits) no call takes that shape, so the library holds no kernel of it."""
+    with open(cv.LIB_PATH, "rb") as f:
+        names = set(re.findall(rb"norm_(?:grad_)?rows_kernelI\w+?RowShapeILj16ELj4E", f.read()))
+    assert any(b"kernelIff" in n for n in names)
+    assert not [n for n in names if not n.split(b"kernelI")[1].startswith(b"f")], names
