@@ -336,3 +336,25 @@ def test_norm_shapes_are_those_that_calls_reach():
         names = set(re.findall(rb"norm_(?:grad_)?rows_kernelI\w+?RowShapeILj16ELj4E", f.read()))
     assert any(b"kernelIff" in n for n in names)
     assert not [n for n in names if not n.split(b"kernelI")[1].startswith(b"f")], names
+
+
+@gpu
+@pytest.mark.parametrize("types", [(F32, F32), (BF16, BF16), (F16, F16), (F32, BF16)])
+@pytest.mark.parametrize("n", [8191, 8192, 16383, 16384])
+def test_layer_norm_by_one_wavefront_and_by_more(types, n):
+    """One side and the other of the numbers of rows from which a wavefront has a row to itself; sampled rows, all of y."""
+    tx, ty = types
+    dim = 1301 if tx == F32 else 2603                        # 326 accesses; half of it has 163
+    for width in (dim, dim // 2):
+        x = 3.0 + 2.0 * uniform(n, width, -1.0, 1.0, 30).to(tx)
+        gamma, beta = uniform(2, width, 0.5, 1.5, 31)
+        y, stats = torch.full((n, width), 7.0, dtype=ty, device=DEV), torch.empty(n, 2, device=DEV)
+        cv.layer_norm(x, gamma, beta, y, stats)
+        some = [0, 1, 2, 3, n // 2, n - 2, n - 1]
+        want, tol, s, s_tol = ref.layer_norm(f64(x[some]), f64(gamma), f64(beta), 1e-5)
+        near(stats[some], s, s_tol)
+        near(y[some], want, tol, ty)
+        h = (x.double() - stats[:, :1].double()) * stats[:, 1:].double() * gamma.double() + beta.double()
+        # from the statistics as they are: the difference, two products and a sum rounded, then the type
+        tol = 4 * ref.U * (h.abs() + beta.abs().double()) + h.abs() * (torch.finfo(ty).eps / 2) * 1.001 + 2.0 ** -149
+        assert bool(((y.double() - h).abs() <= tol).all())
