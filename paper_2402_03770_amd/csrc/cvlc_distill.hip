@@ -10,8 +10,9 @@
 //            gradient: one read, one write.  Workgroups go from row to row, and
 //            every access that has been turned into gradient is loaded again
 //            from the next row at once.
-//   long     rows too long for that, and rows of which only the loss or only the
-//            gradient is wanted: in passes of four accesses per thread.
+//            Rows of which only the loss or only the gradient is wanted too, as
+//            long as they are one wavefront's.
+//   long     longer rows: in passes of four accesses per thread.
 //   part_sum, part_finish   few rows: parts of a row per workgroup, their pairs
 //            joined by every workgroup that goes on with a part.
 //

@@ -2,7 +2,9 @@
 //
 // Gradient: dtable[v] = scale * sum of the dout rows whose token is v.  Texts'
 // tokens are far from even (the commonest is a twentieth of all), so no token is
-// one thread's, and every order of summation is fixed by places alone.
+// one thread's, and every order of summation is fixed by places alone.  Few
+// tokens: a row of the table is one workgroup's per block of columns, so a token
+// that most places hold is what the call waits for.  Many: work is cut by places.
 //
 // Few tokens, in one launch:
 //   direct       a workgroup owns every slices-th row of the table and a block of
@@ -31,7 +33,10 @@ namespace cvlc {
 namespace {
 
 constexpr uint32_t kEmbedBlock = 256;
-constexpr uint32_t kManyBlocks = 8192;  // workgroups of one row per thread from which a thread takes four
+// Workgroups of one row per thread from which a thread takes four, past the caches' order.  Rows of 2048 bf16, one and four:
+// 4096 of them 6.8 and 6.9 us, 8192 10.7 and 10.1, 16384 25.4 and 17.0; with a layer norm of the output behind them, which then finds
+// less of it in the caches, 8192 26.9 and 27.9, 16384 50.7 and 49.1, 32768 83.1 and 78.5.
+constexpr uint32_t kManyBlocks = 8192;
 constexpr uint32_t kSortBlock = 256, kSortWaves = kSortBlock / kWave;
 constexpr uint32_t kTile = 4096;                           // pairs a workgroup sorts per pass
 constexpr uint32_t kTileRounds = kTile / kSortBlock;       // of 64 consecutive pairs per wavefront
@@ -46,7 +51,7 @@ __device__ __forceinline__ int64_t load_token(const void* ids, uint32_t id_bytes
 
 // ----------------------------------------------------------------------------- lookup
 // `lanes` threads (a power of two) to a row, U rows under way per thread.  Many rows are written past the caches' order, which
-// then hold the frequent tokens' rows of the table (65536 x 2048 bf16: 55 us, 5.9 TB/s of what has to move; 77 without).
+// then hold the frequent tokens' rows of the table (65536 x 2048 bf16: 59 us; four rows in the caches' order 79, one 97).
 template <class TT, class TO, uint32_t U>
 __global__ __launch_bounds__(kEmbedBlock) void embed_kernel(uint32_t n, const void* ids, uint32_t id_bytes, const TT* table,
                                                             uint64_t table_stride, uint32_t vocab, uint32_t dim, float scale,
@@ -549,8 +554,11 @@ __global__ __launch_bounds__(kDirectBlock) void direct_kernel(DirectArgs a, cons
 // Slices (a power of two) that the table is cut into, if that is the way for so many tokens.  Every workgroup reads all the
 // tokens, twice, so there is one, as large as they go, to a CU (12000 tokens, 2000 rows of 200 bf16: 16.6 us; two of 512
 // threads each 20.7), except for a table of more rows than it keeps counts of.  Against the sort and its sums, with inputs
-// that are not in the caches: 640 tokens of 96 fp32 6.7 us (35 sorted), 12000 of 200 bf16 16.6 (59), 16384 of 768 bf16 70
-// (73), 1000 of 8192 bf16 into a table of 1 GB 217 (228); 30000 of 512 bf16 119 (99), before both became faster.
+// that are not in the caches: 640 tokens of 96 fp32 6.7 us (35 sorted), 4096 of 768 bf16 into 32000 rows 40 (70), 12288 63 (72),
+// 16384 70 (73), 24576 85 (76); 16384 of 512 fp32 58 (68), 24576 74 (71); 16384 of 512 bf16 into 8000 rows 29 (65), 24576 40
+// (67); 1000 of 8192 bf16 into a table of 1 GB 217 (228).  The worst texts are those of one token: where it holds half of
+// 16384 places and all of them, 256 bf16 65 (75) and 113 (77), 768 bf16 194 (81) and 322 (86); 4096 places of 2048 109 (88) and
+// 140 (86).  More places than 16384 are sorted, also where the table is small, so that it stays at that.
 constexpr uint32_t kDirectBlocks = 256;
 constexpr uint64_t kDirectReads = 1u << 25;  // tokens read by all workgroups
 bool direct_slices(uint32_t n, uint32_t vocab, uint32_t column_blocks, uint32_t* slices_log) {

@@ -370,8 +370,9 @@ bool by_norm_shape(uint32_t n, uint32_t dim, F f) {
   return false;
 }
 // Backward a thread holds five values per column (gamma, two sums, h, g), so one access per thread as far as a workgroup
-// goes.  Beyond 8192 fp32 (1024 threads with 16 columns each) the sums over the rows lie in LDS (8192 x 16384 fp32: 280 us,
-// 437 with them in registers that spill).
+// goes.  Beyond 8192 fp32 (1024 threads with 16 columns each) the sums over the rows lie in LDS (8192 x 16384 fp32: 281 us,
+// 437 with them in registers that spill).  Two accesses of eight values, 16 columns as well, fit for bf16 (8192 x 16384: 148 us)
+// and nearly for fp16, which spills 4 registers (185).
 template <uint32_t per, class F>
 bool by_norm_grad_shape(uint32_t dim, F f) {
   const uint32_t vectors = (dim + per - 1) / per;
