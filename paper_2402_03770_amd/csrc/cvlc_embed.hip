@@ -283,7 +283,7 @@ struct SumArgs {
   float* part;  // [chunks][2][dim]: a token from the chunk before, and one that goes on in the chunk after
 };
 
-// Bound by HBM: 131072 tokens, as many rows of 2048 bf16, 186 us for 0.77 GB, 4.1 TB/s; with chunks of 64 and accesses in the
+// Bound by memory: 131072 tokens, as many rows of 2048 bf16, 186 us for 0.82 GB, 4.4 TB/s; with chunks of 64 and accesses in the
 // caches' order 246, and 40000 tokens of 1000 fp32 346 us in all, now 295.
 template <class T, bool ONCE>
 __global__ __launch_bounds__(kEmbedBlock) void sum_kernel(SumArgs a, const T* dout) {

@@ -349,10 +349,10 @@ __global__ __launch_bounds__(S::kThreads, S::O) void norm_grad_rows_kernel(NormA
 // Few wavefronts with many bytes under way each do best: rows of one wavefront need no barrier (65536 x 4096 bf16: a
 // wavefront with eight accesses per thread 183 us, four with two 201, eight with one 220).  With few rows that leaves
 // CUs empty, so rows of more than 128 accesses are spread over two wavefronts below 8192 rows, rows of more than 256 over
-// four below 16384.  By one wavefront and by the more, bf16: 8192 x 2048 12.6 and 12.8 us (4096 8.2 and 8.3, 200 rows 4.0 and
-// 7.0 on the device); of 4096 values, 4096 rows 15.3 and 13.0, 8192 27.9 and 26.7, 16384 48.4 and 47.9, 32768 92.4 and 95.6; of
-// 2500, which leave three of eight accesses idle, 8192 24.6 and 20.1, 16384 43.7 and 36.9.  fp32: 8192 x 1300 19.1 and 18.0, 16384
-// 32.8 and 34.8.
+// four below 16384.  By one wavefront and by the more, bf16: rows of 2048, 200 of them 4.3 and 3.2 us on the device, 2048 6.1
+// and 5.7, 4096 8.9 both, 8192 12.6 and 12.8 a call; of 4096, 200 6.4 and 3.5 on the device, 4096 15.3 and 13.0 a call, 8192 27.9
+// and 26.7, 16384 48.4 and 47.9, 32768 92.4 and 95.6; of 2500, which leave three of eight accesses idle, 8192 24.6 and 20.1,
+// 16384 43.7 and 36.9.  fp32: 8192 x 1300 19.1 and 18.0, 16384 32.8 and 34.8.
 // Calls f with the shape for rows of `dim` elements, `per` of them an access; false: too long for registers, or shorter than
 // an access.
 template <uint32_t per, class F>
