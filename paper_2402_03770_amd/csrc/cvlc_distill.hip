@@ -57,7 +57,8 @@ __device__ __forceinline__ float exp_part(float z, float m, float c) { return __
 // maximum that would cost bits (an exponent of 32 and more has a step of 2^-19, 11 roundings of fp32 in the result), so
 // fp32 lifts beyond kFar alone, where the exponent's own step is no finer; 16-bit results do not notice and are spared the
 // choice.  They do not lift a scale below kTiny: it would become subnormal and lose its bits, and what it makes of an
-// exponential that needs a lift is 0.
+// exponential that needs a lift is 0.  Exponentials below 2^-158 become 0: no result of a scale up to 2^8 notices, and of a
+// larger one what is that far below the row's largest.
 constexpr float kLift = 32.0f, kUnlift = 0x1p-32f, kFar = -64.0f, kTiny = 0x1p-24f;
 template <class T>
 struct GradScale {
