@@ -445,6 +445,68 @@ int cvlc_distill_grad(uint32_t n, uint32_t vocab, const void* d_logits, uint32_t
                       const float* d_stats, void* d_dlogits, uint64_t dlogits_stride, uint32_t* d_status,
                       void* hip_stream);
 
+/* One AdamW step over all tensors of a model.  With g the gradient times
+ * grad_scale and t the step's number, element by element,
+ *   m <- beta1 m + (1 - beta1) g,   v <- beta2 v + (1 - beta2) g^2,
+ *   p <- p (1 - lr weight_decay) - lr / (1 - beta1^t) * m / (sqrt(v) / sqrt(1 - beta2^t) + eps).
+ * An element whose g^2 is not finite in fp32 keeps its weight and averages and
+ * sets CVLC_DEV_NONFINITE.
+ *
+ * Averages of 8 bits are codes of e4m3 (bias 7, largest value 448, no infinity),
+ * of m and of sqrt(v), times a scale for each per CVLC_ADAMW_BLOCK values of the
+ * tensor: {largest |m| / 448, largest sqrt(v) / 448}, zeros where the largest is
+ * below 2^-100.  The weights move by the averages before they are held.  m is
+ * rounded to nearest.  sqrt(v) goes to one of the two codes around it, up with
+ * the probability of its distance from the lower one in steps of 2^-16 (a step
+ * changes it by less than a code, so to nearest it would never move), and to
+ * zero only from zero.  Its 16 random bits are those of Philox4x32-10 with key
+ * seed and counter (i / 8, 0, t, tensor) for element i: halves of the four words
+ * in ascending order, low ones first.  All zeros is where training starts. */
+#define CVLC_ADAMW_BLOCK 256u
+typedef struct cvlc_adamw_tensor_t {
+  uint64_t n;           /* elements, 0 allowed, at most 2^35                          */
+  float* d_param;       /* n fp32, as a slice of the model's flat vector is           */
+  const void* d_grad;   /* n of grad_type                                             */
+  void *d_m, *d_v;      /* n fp32 each, or n codes of a byte each                     */
+  float* d_scales;      /* 8 bits: ceil(n / CVLC_ADAMW_BLOCK) pairs, 8-byte aligned   */
+  void* d_copy;         /* NULL, or n of copy_type: the new weights, rounded          */
+  uint32_t grad_type;   /* CVLC_F32, CVLC_BF16, CVLC_F16                              */
+  uint32_t copy_type;   /* CVLC_BF16, CVLC_F16                                        */
+  uint32_t state_bits;  /* 32 or 8                                                    */
+  float weight_decay;
+} cvlc_adamw_tensor_t;
+
+/* What cvlc_adamw_plan leaves for the steps; the caller keeps it with its workspace. */
+typedef struct cvlc_adamw_plan_t {
+  void* d_workspace;
+  uint32_t count, chunks;
+  uint64_t moved;       /* bytes of a step, about */
+} cvlc_adamw_plan_t;
+
+typedef struct cvlc_adamw_rates_t {
+  double lr, beta1, beta2, eps, grad_scale; /* 0 <= beta < 1, eps > 0  */
+  uint32_t step;                            /* t, from 1 on             */
+} cvlc_adamw_rates_t;
+
+/* GPU.  Lays the tensors' table out in the workspace, once for all steps: the
+ * steps read addresses, types and decays from there, so buffers must stay where
+ * they are.  Buffers that share elements of which a step writes some are refused.
+ *   d_workspace  device, 256-byte aligned, ws_bytes >=
+ *                cvlc_adamw_workspace_bytes(count, tensors); holds no status
+ *                word; not to be written to while the plan is in use */
+size_t cvlc_adamw_workspace_bytes(uint32_t count, const cvlc_adamw_tensor_t* tensors);
+int cvlc_adamw_plan(uint32_t count, const cvlc_adamw_tensor_t* tensors, void* d_workspace, size_t ws_bytes,
+                    cvlc_adamw_plan_t* plan_out, void* hip_stream);
+
+/* GPU.  The step, one launch.
+ *   d_now     NULL, or device, three fp32 {t, lr, grad_scale} that stand in for
+ *             those of `rates`: what a captured step reads anew at every replay
+ *   seed      of the rounding of 8-bit averages
+ *   d_status  device or NULL: status bits are OR-ed into this word, which the
+ *             caller clears */
+int cvlc_adamw(const cvlc_adamw_plan_t* plan, const cvlc_adamw_rates_t* rates, const float* d_now, uint64_t seed,
+               uint32_t* d_status, void* hip_stream);
+
 /* Profiling aid (not part of the hot path).  Between cvlc_profile_start and
  * cvlc_profile_stop every cvlc_encode_batch / cvlc_decode_aggregate / cvlc_fit_alpha call of this
  * process brackets the stages selected in stage_mask (bit i = stage i) with a

@@ -1,0 +1,87 @@
+"""What a client trains with, in 64 bits, from the definitions (numpy, test infrastructure).
+
+Every function returns, beside its results, how far fp32 arithmetic may take them; `U` is fp32's unit roundoff.
+"""
+from __future__ import annotations
+
+import numpy as np
+
+from .local_step import U
+
+# ----------------------------------------------------------------------------- AdamW
+BLOCK, TOP, TINY = 256, 448.0, 2.0 ** -100
+# the codes 0 ... 126 of e4m3: four bits of exponent (bias 7), three of fraction
+CODES = np.array([(c % 8) * 2.0 ** -9 if c < 8 else (1 + (c % 8) / 8) * 2.0 ** (c // 8 - 7) for c in range(127)])
+
+
+def values(codes):
+    """What codes, as bytes, stand for."""
+    codes = np.asarray(codes).astype(np.int64)
+    return np.where(codes >= 128, -1.0, 1.0) * CODES[codes & 127]
+
+
+def spread(scales, n):
+    return np.repeat(np.asarray(scales, np.float64), BLOCK, 0)[:n]
+
+
+def chances(n, seed, step, tensor):
+    """Element i's 16 bits: Philox4x32-10 of (i / 8, 0, step, tensor), the halves of its words, low ones first."""
+    low = np.uint64(0xFFFFFFFF)
+    c = [np.arange((n + 7) // 8, dtype=np.uint64)] + [np.full((n + 7) // 8, x, np.uint64) for x in (0, step, tensor)]
+    k = [seed & 0xFFFFFFFF, seed >> 32]
+    for _ in range(10):
+        p, q = c[0] * np.uint64(0xD2511F53), c[2] * np.uint64(0xCD9E8D57)
+        c = [(q >> np.uint64(32)) ^ c[1] ^ np.uint64(k[0]), q & low, (p >> np.uint64(32)) ^ c[3] ^ np.uint64(k[1]), p & low]
+        k = [(k[0] + 0x9E3779B9) & 0xFFFFFFFF, (k[1] + 0xBB67AE85) & 0xFFFFFFFF]
+    halves = [h for w in c for h in (w & np.uint64(0xFFFF), w >> np.uint64(16))]
+    return np.stack(halves, 1).reshape(-1)[:n].astype(np.float64)
+
+
+def nearest(y):
+    """The codes nearest to y, 0 <= y <= 448, even ones where two are as near."""
+    at = np.clip(np.searchsorted(CODES, y), 1, 126)
+    below, above = y - CODES[at - 1], CODES[at] - y
+    return np.where((below < above) | ((below == above) & ((at - 1) % 2 == 0)), at - 1, at)
+
+
+def by_chance(y, chance):
+    """The codes below y >= 0 or above it, above where the chance carries over; none but zeros become zeros."""
+    at = np.clip(np.searchsorted(CODES, y, side="right") - 1, 0, 126)
+    step = np.where(at < 126, CODES[np.minimum(at + 1, 126)] - CODES[at], 1.0)
+    up = (y - CODES[at]) / step + chance * 2.0 ** -16 >= 1.0
+    return np.where(y > 0, np.clip(at + up, 1, 126), 0)
+
+
+def adamw(param, grad, m, v, step, lr, betas, eps, decay, grad_scale=1.0, held=False):
+    """param, m, v, sqrt v after the step and how far off each may be.  `held`: m and v come out of 8 bits, with a rounding
+    (of v three) more.  An element whose gradient squared is beyond fp32 keeps what it has."""
+    p, g, m, v = (np.asarray(x, np.float64) for x in (param, grad, m, v))
+    (b1, b2), lr, scale = betas, float(lr), float(np.float32(grad_scale))
+    with np.errstate(over="ignore", invalid="ignore"):
+        gs = g * scale
+        new_m, new_v = b1 * m + (1 - b1) * gs, b2 * v + (1 - b2) * gs * gs
+        # a factor has a rounding, its product another, the sum a third
+        off_m = (4 + held) * U * (np.abs(b1 * m) + np.abs((1 - b1) * gs)) + 2.0 ** -148
+        off_v = (6 + 3 * held) * U * new_v + 2.0 ** -148
+        fine = np.isfinite(gs) & (np.abs(gs) * np.abs(gs) < np.finfo(np.float32).max)
+        new_m, new_v = np.where(fine, new_m, m), np.where(fine, new_v, v)
+        root = np.sqrt(new_v)
+        off_root = np.where(root > 0, off_v / np.maximum(2 * root, 1e-300), 0.0) + U * root
+        rate = lr / (1 - b1 ** step)
+        under = root / np.sqrt(1 - b2 ** step) + eps
+        off_under = off_root / np.sqrt(1 - b2 ** step) + 3 * U * under
+        move = new_m / under
+        off_move = off_m / under + np.abs(move) * (off_under / under + U)
+        to = p * (1 - lr * decay) - rate * move
+        off = np.abs(p) * (3 * U * abs(lr * decay) + 2 * U) + abs(rate) * (off_move + 3 * U * np.abs(move)) + U * np.abs(to)
+    return (np.where(fine, to, p), np.where(fine, off, 0.0), new_m, np.where(fine, off_m, 2 * U * np.abs(m)),
+            new_v, np.where(fine, off_v, 4 * U * np.abs(v)), root, np.where(fine, off_root, 4 * U * root), fine)
+
+
+def scales_of(x, off):
+    """The blocks' scales of |x| and how far off; what lies about the border to zeros may go either way."""
+    n = x.size
+    blocks = -(-n // BLOCK)
+    top, far = (np.pad(a, (0, blocks * BLOCK - n)).reshape(blocks, BLOCK) for a in (np.abs(x), off))
+    top, far = top.max(1), far.max(1)
+    return np.where(top >= TINY, top, 0.0) / TOP, far / TOP + 2 * U * top / TOP

@@ -22,6 +22,7 @@ FIT_RANKS_MAX = 32
 GRAD_ACCUMULATE = 1
 DISTILL_LOGPROBS = 1
 DISTILL_MAX_K = 1024
+ADAMW_BLOCK = 256
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libcvlc.so")
@@ -54,6 +55,24 @@ class SegStats(C.Structure):
     """cvlc_seg_stats_t"""
     _fields_ = [("min", C.c_float), ("max", C.c_float), ("sumsq", C.c_double),
                 ("count", C.c_uint32), ("reserved", C.c_uint32), ("errsq", C.c_double)]
+
+
+class AdamwTensor(C.Structure):
+    """cvlc_adamw_tensor_t"""
+    _fields_ = [("n", C.c_uint64), ("param", C.c_void_p), ("grad", C.c_void_p), ("m", C.c_void_p), ("v", C.c_void_p),
+                ("scales", C.c_void_p), ("copy", C.c_void_p), ("grad_type", C.c_uint32), ("copy_type", C.c_uint32),
+                ("state_bits", C.c_uint32), ("weight_decay", C.c_float)]
+
+
+class AdamwPlanData(C.Structure):
+    """cvlc_adamw_plan_t"""
+    _fields_ = [("workspace", C.c_void_p), ("count", C.c_uint32), ("chunks", C.c_uint32), ("moved", C.c_uint64)]
+
+
+class AdamwRates(C.Structure):
+    """cvlc_adamw_rates_t"""
+    _fields_ = [("lr", C.c_double), ("beta1", C.c_double), ("beta2", C.c_double), ("eps", C.c_double),
+                ("grad_scale", C.c_double), ("step", C.c_uint32)]
 
 
 class CvlcError(RuntimeError):
@@ -138,6 +157,10 @@ def lib() -> C.CDLL:
         L.cvlc_distill.argtypes = [u32, u32, vp, u32, u64, u32, vp, u32, vp, u32, f32, u32, vp, vp, vp, vp, u64, vp,
                                    C.c_size_t, vp, vp]
         L.cvlc_distill_grad.argtypes = [u32, u32, vp, u32, u64, u32, vp, u32, vp, u32, f32, u32, vp, vp, vp, u64, vp, vp]
+        L.cvlc_adamw_workspace_bytes.argtypes = [u32, C.POINTER(AdamwTensor)]
+        L.cvlc_adamw_workspace_bytes.restype = C.c_size_t
+        L.cvlc_adamw_plan.argtypes = [u32, C.POINTER(AdamwTensor), vp, C.c_size_t, C.POINTER(AdamwPlanData), vp]
+        L.cvlc_adamw.argtypes = [C.POINTER(AdamwPlanData), C.POINTER(AdamwRates), vp, u64, vp, vp]
         L.cvlc_profile_start.argtypes = [C.c_uint32]
         L.cvlc_profile_stop.argtypes = [C.POINTER(C.c_float), u32p]
         L.cvlc_status_string.argtypes = [C.c_int]
@@ -564,6 +587,72 @@ def distill_grad(logits: torch.Tensor, teacher_ids: torch.Tensor, teacher_values
     _check(lib().cvlc_distill_grad(n, vocab, zp, zt, zs, k, teacher_ids.data_ptr(), size, teacher_values.data_ptr(),
                                    kind, temperature, DISTILL_LOGPROBS if logprobs else 0, wp, sp, dp, ds, st,
                                    stream), what)
+
+
+class AdamwPlan:
+    """cvlc_adamw_plan: what adamw() steps over.  Lists of one entry per tensor, contiguous, of equal numbers of elements:
+    `params` float32, `grads` of any type, `m` and `v` both float32 or, for averages in 8 bits, both float8_e4m3fn or
+    uint8, with `scales` float32 (ceil(n / ADAMW_BLOCK), 2).  `copies`: None, or per tensor None or bfloat16 or float16.
+    Keeps the tensors, which must stay where they are, and a workspace of its own; waits until it is laid out."""
+
+    def __init__(self, params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], m: Sequence[torch.Tensor],
+                 v: Sequence[torch.Tensor], scales: Optional[Sequence[Optional[torch.Tensor]]] = None,
+                 copies: Optional[Sequence[Optional[torch.Tensor]]] = None,
+                 weight_decays: Optional[Sequence[float]] = None):
+        what, count = "cvlc_adamw_plan", len(params)
+        scales = scales if scales is not None else [None] * count
+        copies = copies if copies is not None else [None] * count
+        decays = weight_decays if weight_decays is not None else [0.0] * count
+        lists = (grads, m, v, scales, copies, decays)
+        if any(len(x) != count for x in lists):
+            _refuse(what, "the lists are not of one length")
+        if count == 0:
+            _refuse(what, "there is no tensor")
+        table = (AdamwTensor * count)()
+        for i, (p, g, a, b, s, c, decay) in enumerate(zip(params, *lists)):
+            n, bits = p.numel(), _STATE_BITS.get(a.dtype)
+            if p.dtype != torch.float32 or g.dtype not in _TYPES:
+                _refuse(what, f"tensor {i}: {p.dtype} weights or {g.dtype} gradients")
+            if bits is None or b.dtype != a.dtype:
+                _refuse(what, f"tensor {i}: averages of {a.dtype} and {b.dtype}")
+            if c is not None and c.dtype not in (torch.bfloat16, torch.float16):
+                _refuse(what, f"tensor {i}: a copy of {c.dtype}")
+            if any(x is not None and (x.numel() != n or not x.is_contiguous()) for x in (p, g, a, b, c)):
+                _refuse(what, f"tensor {i}: not contiguous, or not of {n} elements")
+            if (bits == 8) != (s is not None):
+                _refuse(what, f"tensor {i}: scales go with averages of 8 bits")
+            table[i] = AdamwTensor(n, p.data_ptr(), g.data_ptr(), a.data_ptr(), b.data_ptr(),
+                                   _vector(what, "scales", s, (-(-n // ADAMW_BLOCK), 2)), c.data_ptr() if c is not None else None,
+                                   _TYPES[g.dtype], _TYPES[c.dtype] if c is not None else 0, bits, decay)
+        self.tensors = (list(params), *(list(x) for x in lists[:-1]))
+        every = [t for x in self.tensors for t in x if t is not None]
+        stream = _stream_of(what, *every)
+        if torch.cuda.is_current_stream_capturing():
+            _refuse(what, "a plan is made before a graph is captured")
+        self.device, self.data = params[0].get_device(), AdamwPlanData()
+        self.workspace = new_workspace(lib().cvlc_adamw_workspace_bytes(count, table), params[0].device)
+        _check(lib().cvlc_adamw_plan(count, table, self.workspace.data_ptr(), self.workspace.numel(), C.byref(self.data), stream), what)
+        torch.cuda.current_stream().synchronize()      # a step may go on any stream
+
+
+_STATE_BITS = {torch.float32: 32, torch.uint8: 8, torch.float8_e4m3fn: 8}
+
+
+def adamw(plan: AdamwPlan, step: int, lr: float, betas=(0.9, 0.999), eps: float = 1e-8, grad_scale: float = 1.0, seed: int = 0,
+          now: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None) -> None:
+    """cvlc_adamw on the current stream: one AdamW step, the `step`-th (from 1 on), over all tensors of the plan.  `now` is
+    an optional float32 tensor {step, lr, grad_scale} on the device that stands in for the arguments, which a captured step
+    reads at every replay; `status` an optional int32 tensor of one entry that receives DEV_NONFINITE."""
+    what = "cvlc_adamw"
+    if torch.cuda.current_device() != plan.device:
+        _refuse(what, f"the plan is on cuda:{plan.device}, not on the current GPU")
+    if now is not None or status is not None:
+        _stream_of(what, *(t for t in (now, status) if t is not None))
+    np_, st = _vector(what, "now", now, (3,)), _status(what, status)
+    if not 0 <= step < 1 << 32:
+        _refuse(what, f"step {step}")
+    rates = AdamwRates(lr, betas[0], betas[1], eps, grad_scale, step)
+    _check(lib().cvlc_adamw(C.byref(plan.data), C.byref(rates), np_, seed & (1 << 64) - 1, st, _raw_stream(plan.device)), what)
 
 
 def device_status(workspace: torch.Tensor) -> int:
