@@ -445,6 +445,58 @@ int cvlc_distill_grad(uint32_t n, uint32_t vocab, const void* d_logits, uint32_t
                       const float* d_stats, void* d_dlogits, uint64_t dlogits_stride, uint32_t* d_status,
                       void* hip_stream);
 
+/* A gated linear recurrence, channel by channel, over sequences of rows: with
+ * f = 1 / (1 + exp(-gate)),
+ *   h_t = f_t h_(t-1) + (1 - f_t) x_t.
+ * All matrices are n rows of dim elements of one type; states are n_seq rows of
+ * dim fp32 without gaps.  A row may go to any of n_seq sequences that lie one
+ * after the other:
+ *   d_starts   device, n_seq + 1 offsets of start_bytes = 4 or 8 bytes, signed,
+ *              ascending, between 0 and n: sequence j has the rows from
+ *              d_starts[j] up to before d_starts[j + 1], or none.  Rows before
+ *              the first and behind the last offset are neither read nor
+ *              written.  Offsets that are not so set CVLC_DEV_INDEX; results are
+ *              then unspecified.  NULL: n_seq sequences of n / n_seq rows each
+ *              (n a multiple of n_seq).
+ *   d_status   as for cvlc_embed */
+
+/* GPU.  Forward.
+ *   d_h0       the states before the first rows, or NULL (zeros)
+ *   d_last     NULL, or receives the states after the last rows (of a sequence
+ *              without rows, the one before)
+ *   d_workspace  device, 256-byte aligned, ws_bytes >=
+ *              cvlc_gated_scan_workspace_bytes(n, dim, n_seq); holds no status word */
+size_t cvlc_gated_scan_workspace_bytes(uint32_t n, uint32_t dim, uint32_t n_seq);
+int cvlc_gated_scan(uint32_t n, uint32_t dim, const void* d_x, uint64_t x_stride, const void* d_gate,
+                    uint64_t gate_stride, uint32_t type, uint32_t n_seq, const void* d_starts, uint32_t start_bytes,
+                    const float* d_h0, void* d_h, uint64_t h_stride, float* d_last, void* d_workspace,
+                    size_t ws_bytes, uint32_t* d_status, void* hip_stream);
+
+/* GPU.  Its backward pass, from the forward pass's h as it was written.  With D_t
+ * the whole gradient of h_t, D_t = dy_t + f_(t+1) D_(t+1):
+ *   dx_t = (1 - f_t) D_t,   dgate_t = D_t (h_(t-1) - x_t) f_t (1 - f_t),   dh0 = f_1 D_1.
+ *   d_dlast    the gradients of the states after the last rows, or NULL (zeros)
+ *   d_dh0      NULL, or receives the gradients of the states before the first rows
+ * The workspace is as large as the forward pass's. */
+int cvlc_gated_scan_grad(uint32_t n, uint32_t dim, const void* d_dy, uint64_t dy_stride, const void* d_x,
+                         uint64_t x_stride, const void* d_gate, uint64_t gate_stride, const void* d_h,
+                         uint64_t h_stride, uint32_t type, uint32_t n_seq, const void* d_starts, uint32_t start_bytes,
+                         const float* d_h0, const float* d_dlast, void* d_dx, uint64_t dx_stride, void* d_dgate,
+                         uint64_t dgate_stride, float* d_dh0, void* d_workspace, size_t ws_bytes, uint32_t* d_status,
+                         void* hip_stream);
+
+/* GPU.  One token of each of n sequences: row i takes the state of its slot one
+ * step on and receives it as h.
+ *   d_slots    device, n numbers of slot_bytes = 4 or 8 bytes, signed, or NULL
+ *              (row i's is i).  A negative one is padding: its row of h is zeros.
+ *              So is that of one at or beyond n_slots, or that a row before has
+ *              named already; those set CVLC_DEV_INDEX.
+ *   d_states   n_slots rows of dim fp32 without gaps */
+int cvlc_gated_scan_step(uint32_t n, uint32_t dim, const void* d_x, uint64_t x_stride, const void* d_gate,
+                         uint64_t gate_stride, uint32_t type, const void* d_slots, uint32_t slot_bytes,
+                         uint32_t n_slots, float* d_states, void* d_h, uint64_t h_stride, uint32_t* d_status,
+                         void* hip_stream);
+
 /* One AdamW step over all tensors of a model.  With g the gradient times
  * grad_scale and t the step's number, element by element,
  *   m <- beta1 m + (1 - beta1) g,   v <- beta2 v + (1 - beta2) g^2,

@@ -85,3 +85,51 @@ def scales_of(x, off):
     top, far = (np.pad(a, (0, blocks * BLOCK - n)).reshape(blocks, BLOCK) for a in (np.abs(x), off))
     top, far = top.max(1), far.max(1)
     return np.where(top >= TINY, top, 0.0) / TOP, far / TOP + 2 * U * top / TOP
+
+
+# ----------------------------------------------------------------------------- the gated scan
+def sigmoid(z):
+    e = np.exp(-np.abs(z))
+    return np.where(z >= 0, 1.0, e) / (1 + e), np.where(z >= 0, e, 1.0) / (1 + e)
+
+
+def gated_scan(x, gate, bounds, h0=None):
+    """h, the last states, and how far off each.  `bounds`: (first row, one behind the last) of every sequence.  A gate and
+    its rest are off by at most 8 U of themselves; joined in any order a step adds no more than 16 U of what its terms'
+    magnitudes would add up to."""
+    f, rest = sigmoid(x * 0 + gate)
+    h, off = np.full(x.shape, np.nan), np.zeros(x.shape)
+    last, off_last = np.zeros((len(bounds), x.shape[1])), np.zeros((len(bounds), x.shape[1]))
+    for s, (low, high) in enumerate(bounds):
+        u = np.zeros(x.shape[1]) if h0 is None else h0[s].astype(np.float64)
+        size, far = np.abs(u), np.zeros(x.shape[1])
+        for t in range(low, high):
+            u = f[t] * u + rest[t] * x[t]
+            size = f[t] * size + rest[t] * np.abs(x[t])
+            far = f[t] * far + 16 * U * size + 2.0 ** -126
+            h[t], off[t] = u, far
+        last[s], off_last[s] = u, far
+    return h, off, last, off_last
+
+
+def gated_scan_grad(dy, x, gate, h, bounds, h0=None, dlast=None):
+    """dx, dgate, dh0, and how far off each."""
+    f, rest = sigmoid(x * 0 + gate)
+    dim = x.shape[1]
+    dx, dgate, off_x, off_g = (np.full(x.shape, np.nan) for _ in range(4))
+    dh0, off_0 = np.zeros((len(bounds), dim)), np.zeros((len(bounds), dim))
+    for s, (low, high) in enumerate(bounds):
+        c = np.zeros(dim) if dlast is None else dlast[s].astype(np.float64)
+        size, far = np.abs(c), np.zeros(dim)
+        for t in reversed(range(low, high)):
+            before = h[t - 1] if t > low else (np.zeros(dim) if h0 is None else h0[s].astype(np.float64))
+            d, whole = dy[t] + c, np.abs(dy[t]) + size
+            off_d = far + U * whole
+            dx[t], off_x[t] = rest[t] * d, rest[t] * (off_d + 10 * U * np.abs(d)) + 2.0 ** -126
+            dgate[t] = d * (before - x[t]) * f[t] * rest[t]
+            off_g[t] = f[t] * rest[t] * (np.abs(before - x[t]) * off_d + 24 * U * np.abs(d) * (np.abs(before) + np.abs(x[t]))) + 2.0 ** -126
+            c = f[t] * d
+            size = f[t] * whole
+            far = f[t] * far + 16 * U * size + 2.0 ** -126
+        dh0[s], off_0[s] = c, far
+    return dx, off_x, dgate, off_g, dh0, off_0

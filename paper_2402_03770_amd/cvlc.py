@@ -157,6 +157,12 @@ def lib() -> C.CDLL:
         L.cvlc_distill.argtypes = [u32, u32, vp, u32, u64, u32, vp, u32, vp, u32, f32, u32, vp, vp, vp, vp, u64, vp,
                                    C.c_size_t, vp, vp]
         L.cvlc_distill_grad.argtypes = [u32, u32, vp, u32, u64, u32, vp, u32, vp, u32, f32, u32, vp, vp, vp, u64, vp, vp]
+        L.cvlc_gated_scan_workspace_bytes.argtypes = [u32, u32, u32]
+        L.cvlc_gated_scan_workspace_bytes.restype = C.c_size_t
+        L.cvlc_gated_scan.argtypes = [u32, u32, vp, u64, vp, u64, u32, u32, vp, u32, vp, vp, u64, vp, vp, C.c_size_t, vp, vp]
+        L.cvlc_gated_scan_grad.argtypes = [u32, u32, vp, u64, vp, u64, vp, u64, vp, u64, u32, u32, vp, u32, vp, vp, vp, u64, vp, u64,
+                                           vp, vp, C.c_size_t, vp, vp]
+        L.cvlc_gated_scan_step.argtypes = [u32, u32, vp, u64, vp, u64, u32, vp, u32, u32, vp, vp, u64, vp, vp]
         L.cvlc_adamw_workspace_bytes.argtypes = [u32, C.POINTER(AdamwTensor)]
         L.cvlc_adamw_workspace_bytes.restype = C.c_size_t
         L.cvlc_adamw_plan.argtypes = [u32, C.POINTER(AdamwTensor), vp, C.c_size_t, C.POINTER(AdamwPlanData), vp]
@@ -587,6 +593,97 @@ def distill_grad(logits: torch.Tensor, teacher_ids: torch.Tensor, teacher_values
     _check(lib().cvlc_distill_grad(n, vocab, zp, zt, zs, k, teacher_ids.data_ptr(), size, teacher_values.data_ptr(),
                                    kind, temperature, DISTILL_LOGPROBS if logprobs else 0, wp, sp, dp, ds, st,
                                    stream), what)
+
+
+def gated_scan_workspace_bytes(n: int, dim: int, sequences: int) -> int:
+    return int(lib().cvlc_gated_scan_workspace_bytes(n, dim, sequences))
+
+
+def _sequences(what: str, n: int, starts: Optional[torch.Tensor], sequences: Optional[int]):
+    """(number of sequences, offsets' address, their size)"""
+    if (starts is None) == (sequences is None):
+        _refuse(what, "either starts or sequences says how the rows are cut")
+    if starts is None:
+        if not 0 <= sequences < 1 << 31 or (n % sequences if sequences else n):
+            _refuse(what, f"{n} rows do not make {sequences} sequences of one length")
+        return sequences, None, 0
+    size = _id_bytes(what, "starts", starts, 1)
+    if starts.numel() < 1:
+        _refuse(what, "starts has no entry")
+    return starts.numel() - 1, starts.data_ptr(), size
+
+
+def _alike(what: str, n: int, dim: int, **matrices: torch.Tensor):
+    """Addresses and strides of matrices that are all of one type, and the type."""
+    out, kinds = [], set()
+    for name, t in matrices.items():
+        address, kind, stride = _matrix(what, name, t, n, dim)
+        out += [address, stride]
+        kinds.add(kind)
+    if len(kinds) > 1:
+        _refuse(what, "the matrices are not all of one type")
+    return out, kinds.pop()
+
+
+def gated_scan(x: torch.Tensor, gate: torch.Tensor, h: torch.Tensor, workspace: torch.Tensor, starts: Optional[torch.Tensor] = None,
+               sequences: Optional[int] = None, h0: Optional[torch.Tensor] = None, last_out: Optional[torch.Tensor] = None,
+               status: Optional[torch.Tensor] = None) -> None:
+    """cvlc_gated_scan on the current stream: h_t = f_t h_(t-1) + (1 - f_t) x_t with f = sigmoid(gate), channel by channel.
+    `x`, `gate` and `h` are (n, dim) of one type.  Sequences lie one after the other, cut by `starts` (an int32 or int64 tensor
+    of their number and one more offsets, ascending) or into `sequences` of one length.  `h0` and `last_out` are optional
+    float32 (sequences, dim) states; `workspace` holds gated_scan_workspace_bytes(n, dim, sequences)."""
+    what = "cvlc_gated_scan"
+    if x.dim() != 2:
+        _refuse(what, "x is not a matrix")
+    n, dim = x.shape
+    (xp, xs, gp, gs, hp, hs), kind = _alike(what, n, dim, x=x, gate=gate, h=h)
+    count, sp, size = _sequences(what, n, starts, sequences)
+    fp, lp = _vector(what, "h0", h0, (count, dim)), _vector(what, "last_out", last_out, (count, dim))
+    st = _status(what, status)
+    stream = _stream_of(what, x, gate, h, workspace, starts, h0, last_out, status)
+    _check(lib().cvlc_gated_scan(n, dim, xp, xs, gp, gs, kind, count, sp, size, fp, hp, hs, lp, workspace.data_ptr(),
+                                 workspace.numel(), st, stream), what)
+
+
+def gated_scan_grad(dy: torch.Tensor, x: torch.Tensor, gate: torch.Tensor, h: torch.Tensor, dx: torch.Tensor, dgate: torch.Tensor,
+                    workspace: torch.Tensor, starts: Optional[torch.Tensor] = None, sequences: Optional[int] = None,
+                    h0: Optional[torch.Tensor] = None, dlast: Optional[torch.Tensor] = None, dh0_out: Optional[torch.Tensor] = None,
+                    status: Optional[torch.Tensor] = None) -> None:
+    """cvlc_gated_scan_grad on the current stream: the gradients of `x`, `gate` and h0 from those of gated_scan's results
+    (`dy` of h, `dlast` of last_out or None) and from `h` as it wrote it.  Arguments otherwise as there."""
+    what = "cvlc_gated_scan_grad"
+    if x.dim() != 2:
+        _refuse(what, "x is not a matrix")
+    n, dim = x.shape
+    (yp, ys, xp, xs, gp, gs, hp, hs, dxp, dxs, dgp, dgs), kind = _alike(what, n, dim, dy=dy, x=x, gate=gate, h=h, dx=dx, dgate=dgate)
+    count, sp, size = _sequences(what, n, starts, sequences)
+    fp, ep, op = (_vector(what, name, t, (count, dim)) for name, t in (("h0", h0), ("dlast", dlast), ("dh0_out", dh0_out)))
+    st = _status(what, status)
+    stream = _stream_of(what, x, dy, gate, h, dx, dgate, workspace, starts, h0, dlast, dh0_out, status)
+    _check(lib().cvlc_gated_scan_grad(n, dim, yp, ys, xp, xs, gp, gs, hp, hs, kind, count, sp, size, fp, ep, dxp, dxs, dgp, dgs, op,
+                                      workspace.data_ptr(), workspace.numel(), st, stream), what)
+
+
+def gated_scan_step(x: torch.Tensor, gate: torch.Tensor, states: torch.Tensor, h: torch.Tensor, slots: Optional[torch.Tensor] = None,
+                    status: Optional[torch.Tensor] = None) -> None:
+    """cvlc_gated_scan_step on the current stream: one token of each of n sequences.  `states` is float32 (slots, dim) and is
+    taken one step on where `slots` (an int32 or int64 tensor of n different numbers, negative ones for padding; None: row
+    i's is i) says; `h` receives the new states.  `status` receives DEV_INDEX for a slot that is not there or named twice."""
+    what = "cvlc_gated_scan_step"
+    if x.dim() != 2 or states.dim() != 2:
+        _refuse(what, "x or states is not a matrix")
+    n, dim = x.shape
+    (xp, xs, gp, gs, hp, hs), kind = _alike(what, n, dim, x=x, gate=gate, h=h)
+    sp = _vector(what, "states", states, (states.shape[0], dim))
+    size = 0
+    if slots is not None:
+        size = _id_bytes(what, "slots", slots, 1)
+        if slots.numel() != n:
+            _refuse(what, f"slots are {slots.numel()}, not {n}")
+    st = _status(what, status)
+    stream = _stream_of(what, x, gate, states, h, slots, status)
+    _check(lib().cvlc_gated_scan_step(n, dim, xp, xs, gp, gs, kind, slots.data_ptr() if slots is not None else None, size,
+                                      states.shape[0], sp, hp, hs, st, stream), what)
 
 
 class AdamwPlan:

@@ -262,3 +262,270 @@ def test_adamw_plans_are_refused():
         assert refused(cv.AdamwPlan, *args)
     assert refused(cv.AdamwPlan, [t(4)], [t(4)], [t(4)], [t(4)], copies=[t(4)])
     assert refused(cv.AdamwPlan, [t(4)], [t(4)], [t(4)], [t(4)], scales=[t(2).view(1, 2)])
+
+
+# ----------------------------------------------------------------------------- the gated scan
+def cuts(lengths, before=0):
+    starts = np.concatenate([[0], np.cumsum(lengths)]) + before
+    return starts, list(zip(starts[:-1].tolist(), starts[1:].tolist()))
+
+
+class Scan:
+    def __init__(self, n, dim, dtype, sequences, extra=0, offset=0, seed=1, states=True):
+        self.n, self.dim, self.dtype, self.extra, self.offset = n, dim, dtype, extra, offset
+        self.x = random_matrix(n, dim, dtype, seed, extra, offset)
+        self.gate = random_matrix(n, dim, dtype, seed + 1, extra, offset, scale=4.0, shift=1.0)
+        self.dy = random_matrix(n, dim, dtype, seed + 2, extra, offset)
+        g = torch.Generator().manual_seed(seed + 3)
+        self.h0, self.dlast = (torch.randn(sequences, dim, generator=g).to(DEV) if states else None for _ in range(2))
+        self.last, self.dh0 = (torch.full((sequences, dim), 7.0, device=DEV) if states else None for _ in range(2))
+        self.h, self.h_flat = matrix(n, dim, dtype, extra, offset, fill=5.0)
+        self.dx, self.dx_flat = matrix(n, dim, dtype, extra, offset, fill=5.0)
+        self.dgate, self.dgate_flat = matrix(n, dim, dtype, extra, offset, fill=5.0)
+        self.ws = cv.new_workspace(cv.gated_scan_workspace_bytes(n, dim, sequences), DEV)
+        self.ws.fill_(0xFF)
+
+    def forward(self, **cut):
+        cv.gated_scan(self.x, self.gate, self.h, self.ws, h0=self.h0, last_out=self.last, **cut)
+
+    def backward(self, **cut):
+        cv.gated_scan_grad(self.dy, self.x, self.gate, self.h, self.dx, self.dgate, self.ws, h0=self.h0, dlast=self.dlast,
+                           dh0_out=self.dh0, **cut)
+
+    def check(self, bounds):
+        opt = lambda t: None if t is None else f64(t)  # noqa: E731
+        low, high = bounds[0][0], bounds[-1][1]
+        h, off, last, off_last = ref.gated_scan(f64(self.x), f64(self.gate), bounds, opt(self.h0))
+        assert_near(self.h[low:high], h[low:high], off[low:high], self.dtype, "h")
+        dx, off_x, dgate, off_g, dh0, off_0 = ref.gated_scan_grad(f64(self.dy), f64(self.x), f64(self.gate), f64(self.h), bounds,
+                                                                  opt(self.h0), opt(self.dlast))
+        assert_near(self.dx[low:high], dx[low:high], off_x[low:high], self.dtype, "dx")
+        assert_near(self.dgate[low:high], dgate[low:high], off_g[low:high], self.dtype, "dgate")
+        if self.h0 is not None:
+            assert_near(self.last, last, off_last, F32, "last")
+            assert_near(self.dh0, dh0, off_0, F32, "dh0")
+        for m, flat in ((self.h, self.h_flat), (self.dx, self.dx_flat), (self.dgate, self.dgate_flat)):
+            m[low:high] = 5.0
+            assert bool((flat == 5.0).all()), "something else was written"
+
+
+LENGTHS = [[1], [0, 1, 0, 5, 0], [2, 3, 300, 1], [257, 0, 0, 256], [1] * 600, [0] * 700 + [40, 3], [1500]]
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("dim,extra,offset", [(1, 0, 0), (7, 1, 1), (130, 3, 1), (64, 0, 0)])
+@pytest.mark.parametrize("lengths", LENGTHS, ids=lambda v: f"{len(v)}of{sum(v)}")
+def test_gated_scan(dtype, dim, extra, offset, lengths):
+    """Sequences of any lengths, rows before and behind them that hold NaN and stay as they are."""
+    n = sum(lengths) + 5
+    starts, bounds = cuts(lengths, before=2)
+    s = Scan(n, dim, dtype, len(lengths), extra, offset, states=dim != 64)
+    for m in (s.x, s.gate, s.dy):
+        m[:2] = float("nan")
+        m[n - 3:] = float("nan")
+    cut = dict(starts=torch.from_numpy(starts).to(torch.int32 if dim % 2 else torch.int64).to(DEV), status=torch.zeros(1, dtype=torch.int32, device=DEV))
+    s.forward(**cut)
+    s.backward(**cut)
+    assert cut["status"].item() == 0
+    s.check(bounds)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("sequences,length,dim", [(1, 1, 5), (3, 1, 40), (1, 2500, 130), (2, 700, 1000), (300, 4, 16), (40, 300, 64), (1, 9000, 8), (5, 1025, 260)])
+def test_gated_scan_of_equal_lengths(dtype, sequences, length, dim):
+    s = Scan(sequences * length, dim, dtype, sequences, extra=2)
+    s.forward(sequences=sequences)
+    s.backward(sequences=sequences)
+    _, bounds = cuts([length] * sequences)
+    s.check(bounds)
+
+
+@gpu
+def test_gated_scan_cut_both_ways_agrees():
+    """Offsets of equal lengths against the lengths alone: the same values up to the order of joining."""
+    a, b = (Scan(8 * 600, 200, F32, 8) for _ in range(2))
+    starts, bounds = cuts([600] * 8)
+    a.forward(sequences=8)
+    a.backward(sequences=8)
+    b.forward(starts=torch.from_numpy(starts).to(DEV))
+    b.backward(starts=torch.from_numpy(starts).to(DEV))
+    a.check(bounds)
+    b.check(bounds)
+
+
+@gpu
+def test_gated_scan_of_far_gates():
+    """Gates that keep or replace everything, infinite ones too; a NaN reaches the rows behind it in its channel and sequence only."""
+    n, dim = 600, 24
+    s = Scan(2 * n, dim, F32, 2)
+    s.gate[:, :8] = torch.linspace(-150.0, 150.0, 2 * n, device=DEV)[:, None]
+    s.gate[:, 8], s.gate[:, 9] = float("inf"), -float("inf")
+    s.x[100, 20] = float("nan")
+    s.forward(sequences=2)
+    h = s.h.clone()
+    want, off, last, off_last = ref.gated_scan(f64(s.x), f64(s.gate), [(0, n), (n, 2 * n)], f64(s.h0))
+    assert np.isnan(f64(h)[100:n, 20]).all() and np.isnan(want[100:n, 20]).all() and np.isnan(f64(h)).sum() == n - 100
+    some = [c for c in range(dim) if c != 20]
+    assert_near(h[:, some], want[:, some], off[:, some])
+    assert_near(s.last[:, some], last[:, some], off_last[:, some])
+    assert torch.equal(h[:n, 8], s.h0[0, 8].expand(n)) and torch.equal(h[:, 9], s.x[:, 9])
+
+
+@gpu
+def test_gated_scan_grad_against_differences():
+    """The gradient of a random projection of all results, in the oracle's 64 bits, against central differences."""
+    n, dim, bounds = 23, 3, [(0, 9), (9, 9), (9, 23)]
+    s = Scan(n, dim, F32, 3)
+    starts = torch.tensor([0, 9, 9, 23], device=DEV)
+    s.forward(starts=starts)
+    s.backward(starts=starts)
+    x, gate, h0, dy, dlast = (f64(t) for t in (s.x, s.gate, s.h0, s.dy, s.dlast))
+
+    def value(x, gate, h0):
+        h, _, last, _ = ref.gated_scan(x, gate, bounds, h0)
+        return (h * dy).sum() + (last * dlast).sum()
+
+    rng = np.random.default_rng(3)
+    for k, got in enumerate((s.dx, s.dgate, s.dh0)):
+        way = rng.standard_normal(f64(got).shape)
+        step, args = 1e-5, [x, gate, h0]
+        ends = [value(*(a + sign * step * way if i == k else a for i, a in enumerate(args))) for sign in (1, -1)]
+        want = (ends[0] - ends[1]) / (2 * step)
+        # third derivatives of some tens times step^2, and fp32's error of every entry (h's rounding in dgate among it)
+        assert abs((f64(got) * way).sum() - want) <= 1e-7 + 2e-6 * np.abs(f64(got) * way).sum()
+
+
+@gpu
+def test_gated_scan_offsets_that_do_not_go():
+    """Descending, negative or too large ones are told of, and nothing outside the matrices is written."""
+    for bad in ([0, 50, 40, 100], [-3, 50, 60, 100], [0, 50, 60, 1000], [2 ** 40, 0, 0, 0]):
+        s = Scan(100, 20, BF16, 3)
+        status = torch.zeros(1, dtype=torch.int32, device=DEV)
+        s.forward(starts=torch.tensor(bad, device=DEV), status=status)
+        assert status.item() == cv.DEV_INDEX
+        status.zero_()
+        s.backward(starts=torch.tensor(bad, device=DEV), status=status)
+        assert status.item() == cv.DEV_INDEX
+        for m, flat in ((s.h, s.h_flat), (s.dx, s.dx_flat), (s.dgate, s.dgate_flat)):
+            assert untouched(flat, m, 5.0)
+
+
+@gpu
+def test_gated_scan_without_rows():
+    s = Scan(0, 12, F32, 4)
+    s.forward(sequences=4)
+    s.backward(starts=torch.zeros(5, dtype=torch.int64, device=DEV))
+    assert torch.equal(s.last, s.h0) and torch.equal(s.dh0, s.dlast)
+    s.h0 = s.dlast = None
+    s.forward(starts=torch.zeros(5, dtype=torch.int64, device=DEV))
+    s.backward(sequences=4)
+    assert not s.last.any() and not s.dh0.any()
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("n,dim,slots,extra", [(1, 1, 1, 0), (5, 7, 5, 1), (64, 130, 200, 3), (300, 2049, 301, 0)])
+def test_gated_scan_step(dtype, n, dim, slots, extra):
+    x, gate = random_matrix(n, dim, dtype, 1, extra, 1), random_matrix(n, dim, dtype, 2, extra, 1, scale=3.0)
+    h, flat = matrix(n, dim, dtype, extra, 1, fill=5.0)
+    g = torch.Generator().manual_seed(3)
+    states, at = torch.randn(slots, dim, generator=g).to(DEV), torch.randperm(slots, generator=g)[:n]
+    at[n // 2] = -1 if n > 1 else at[0]
+    before, status = f64(states), torch.zeros(1, dtype=torch.int32, device=DEV)
+    cv.gated_scan_step(x, gate, states, h, slots=at.to(torch.int32 if n % 2 else torch.int64).to(DEV), status=status)
+    want_h, off_h, want, off = np.zeros((n, dim)), np.zeros((n, dim)), before.copy(), np.zeros((slots, dim))
+    for i, slot in enumerate(at.tolist()):
+        if slot >= 0:
+            want_h[i:i + 1], off_h[i:i + 1], want[slot:slot + 1], off[slot:slot + 1] = ref.gated_scan(f64(x)[i:i + 1], f64(gate)[i:i + 1], [(0, 1)], before[slot:slot + 1])
+    assert_near(h, want_h, off_h, dtype)
+    assert_near(states, want, off)
+    assert status.item() == 0 and untouched(flat, h, 5.0)
+
+
+@gpu
+def test_gated_scan_step_of_slots_that_do_not_go():
+    """One that is not there and one that two rows name: zeros and a status; the first row that names a slot has it."""
+    n, dim = 600, 20
+    x, gate = random_matrix(n, dim, F32, 1), random_matrix(n, dim, F32, 2)
+    at = torch.arange(n)
+    at[3], at[599], at[400], at[401] = 1000, 7, 2 ** 40, -5
+    states, h = torch.ones(1000, dim, device=DEV), torch.empty(n, dim, device=DEV)
+    status = torch.zeros(1, dtype=torch.int32, device=DEV)
+    cv.gated_scan_step(x, gate, states, h, slots=at.to(DEV), status=status)
+    assert status.item() == cv.DEV_INDEX
+    live = [i for i in range(n) if i not in (3, 599, 400, 401)]
+    want, off, _, _ = ref.gated_scan(f64(x[live]), f64(gate[live]), [(i, i + 1) for i in range(len(live))], np.ones((len(live), dim)))
+    assert_near(h[live], want, off)
+    assert not h[[3, 599, 400, 401]].any() and torch.equal(states[live], h[live])
+    assert bool((states[[3, 400, 401, *range(600, 1000)]] == 1.0).all())
+    cv.gated_scan_step(x, gate, states, h)                              # without slots: a row each, nothing told
+
+
+@gpu
+def test_gated_scan_steps_walk_as_the_scan_does():
+    n, dim = 40, 33
+    s = Scan(3 * n, dim, F32, 3)
+    s.forward(sequences=3)
+    states, h = s.h0.clone(), torch.empty(3, dim, device=DEV)
+    rows = torch.empty(3 * n, dim, device=DEV)
+    for t in range(n):
+        at = [t, n + t, 2 * n + t]
+        cv.gated_scan_step(s.x[at], s.gate[at], states, h)
+        rows[at] = h
+    want, off, last, off_last = ref.gated_scan(f64(s.x), f64(s.gate), [(0, n), (n, 2 * n), (2 * n, 3 * n)], f64(s.h0))
+    assert_near(rows, want, off)
+    assert_near(states, last, off_last)
+
+
+def test_gated_scan_refusals():
+    def t(*shape, dtype=F32):
+        return torch.zeros(*shape, dtype=dtype)
+
+    x, ws = t(6, 4), torch.zeros(1 << 20, dtype=torch.uint8)
+    good = dict(x=x, gate=x, h=x, workspace=ws)
+    for kw in (dict(), dict(sequences=2, starts=t(3, dtype=torch.int64)), dict(sequences=4), dict(sequences=0), dict(sequences=-1), dict(starts=t(3)),
+               dict(starts=t(0, dtype=torch.int32)), dict(sequences=2, gate=t(6, 5)), dict(sequences=2, h=t(6, 4, dtype=BF16)),
+               dict(sequences=2, x=t(4, 6).t()), dict(sequences=2, h0=t(3, 4)), dict(sequences=2, last_out=t(2, 4, dtype=BF16)),
+               dict(sequences=2, status=t(1)), dict(sequences=2)):           # the last: on no GPU
+        assert refused(cv.gated_scan, **(good | kw)), kw
+    good = dict(dy=x, x=x, gate=x, h=x, dx=x, dgate=x, workspace=ws)
+    for kw in (dict(), dict(sequences=2, dgate=t(6, 4, dtype=F16)), dict(sequences=2, dlast=t(2, 5)), dict(sequences=2, dh0_out=t(6, 4)), dict(sequences=2)):
+        assert refused(cv.gated_scan_grad, **(good | kw)), kw
+    good = dict(x=x, gate=x, states=t(9, 4), h=x)
+    for kw in (dict(states=t(9, 5)), dict(states=t(4)), dict(slots=t(5, dtype=torch.int64)), dict(slots=t(6)), dict(states=t(9, 4, dtype=BF16)), dict()):
+        assert refused(cv.gated_scan_step, **(good | kw)), kw
+
+
+def test_gated_scan_refusals_on_the_host():
+    lib, ok = cv.lib(), 1 << 20
+    need = lib.cvlc_gated_scan_workspace_bytes(6, 4, 2)
+
+    def forward(**kw):
+        a = dict(n=6, dim=4, x=ok, xs=4, gate=ok, gs=4, kind=0, count=2, starts=None, size=0, h0=None, h=ok, hs=4, last=None, ws=ok, bytes=need,
+                 status=None) | kw
+        return lib.cvlc_gated_scan(*a.values(), None)
+
+    for kw in (dict(dim=0), dict(n=1 << 31), dict(kind=3), dict(xs=3), dict(gs=3), dict(hs=3), dict(x=None), dict(gate=ok + 2), dict(h=None), dict(count=4),
+               dict(count=0), dict(starts=ok, size=2), dict(starts=ok + 4, size=8), dict(h0=ok + 2), dict(last=ok + 1), dict(ws=None), dict(ws=ok + 8),
+               dict(status=ok + 2)):
+        assert forward(**kw) == cv.ERR_ARG, kw
+    assert forward(bytes=need - 1) == -4
+
+    def backward(**kw):
+        a = dict(n=6, dim=4, dy=ok, ys=4, x=ok, xs=4, gate=ok, gs=4, h=ok, hs=4, kind=1, count=2, starts=None, size=0, h0=None, dlast=None, dx=ok, dxs=4,
+                 dgate=ok, dgs=4, dh0=None, ws=ok, bytes=need, status=None) | kw
+        return lib.cvlc_gated_scan_grad(*a.values(), None)
+
+    for kw in (dict(ys=3), dict(dxs=0), dict(dgs=3), dict(dy=None), dict(dx=ok + 1), dict(dgate=None), dict(dlast=ok + 2), dict(dh0=ok + 3), dict(kind=9)):
+        assert backward(**kw) == cv.ERR_ARG, kw
+
+    def step(**kw):
+        a = dict(n=6, dim=4, x=ok, xs=4, gate=ok, gs=4, kind=0, slots=None, size=0, count=6, states=ok, h=ok, hs=4, status=None) | kw
+        return lib.cvlc_gated_scan_step(*a.values(), None)
+
+    for kw in (dict(dim=0), dict(count=5), dict(slots=ok, size=1), dict(slots=ok + 4, size=8), dict(states=None), dict(states=ok + 2), dict(x=None), dict(hs=2),
+               dict(status=ok + 1)):
+        assert step(**kw) == cv.ERR_ARG, kw
+    assert step(n=0, x=None, gate=None, h=None, states=None) == 0
