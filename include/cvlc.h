@@ -445,6 +445,56 @@ int cvlc_distill_grad(uint32_t n, uint32_t vocab, const void* d_logits, uint32_t
                       const float* d_stats, void* d_dlogits, uint64_t dlogits_stride, uint32_t* d_status,
                       void* hip_stream);
 
+/* GPU.  Softmax cross entropy of a language model's logits over its vocabulary,
+ * z_i = scale * hidden_i table^t, which are never kept:
+ *   loss_i = w_i (ln sum_v exp z_iv - z_i,label).
+ *   d_hidden   n rows of dim elements, n up to 2^22, dim up to 2^20
+ *   d_table    vocab rows of dim elements of the same type
+ *   d_labels   n tokens of id_bytes = 4 or 8 bytes, signed.  A negative one is
+ *              padding; one at or beyond `vocab` sets CVLC_DEV_INDEX and counts as
+ *              padding too
+ *   d_weights  n fp32 w_i, or NULL (all 1)
+ *   d_loss     NULL, or n fp32
+ *   d_stats    NULL, or n times {m, S}, fp32, 8-byte aligned, for
+ *              cvlc_linear_xent_grad: the largest logit and the sum of exp(z - m)
+ *   d_workspace  device, 256-byte aligned, ws_bytes >=
+ *              cvlc_linear_xent_workspace_bytes(n, vocab, dim, type); holds no status word
+ *   d_status   as for cvlc_embed
+ * A row of padding or of weight 0 is not looked at: loss, statistics and gradient
+ * are zeros.  Other rows, and the table, must be finite, and so must their logits.
+ * Products are exact in 16-bit types and to 2^-23 of a term or better in fp32,
+ * sums are fp32.  The call is made of launches whose threads number fewer than
+ * 2^32, and sizes that this does not hold are refused (2^19 rows of a vocabulary
+ * of 2^17 are not). */
+size_t cvlc_linear_xent_workspace_bytes(uint32_t n, uint32_t vocab, uint32_t dim, uint32_t type);
+int cvlc_linear_xent(uint32_t n, uint32_t vocab, uint32_t dim, const void* d_hidden, uint64_t hidden_stride,
+                     const void* d_table, uint64_t table_stride, uint32_t type, const void* d_labels, uint32_t id_bytes,
+                     float scale, const float* d_weights, float* d_loss, float* d_stats, void* d_workspace,
+                     size_t ws_bytes, uint32_t* d_status, void* hip_stream);
+
+/* GPU.  The gradients of the losses' sum, from the statistics of an earlier
+ * cvlc_linear_xent on the same hidden rows, table, labels and scale; the weights
+ * may be others, but a row that had none has no statistics.  With
+ * G_iv = scale w_i (exp(z_iv - m_i) / S_i - [v = label_i]):
+ *   dhidden = G table,   dtable = G^t hidden.
+ *   d_dhidden  n rows of dim elements of the hidden rows' type, or NULL
+ *   d_dtable   vocab rows of dim elements, fp32 or of the table's type, or NULL
+ *              (not both; dtable_type and its stride do not matter then).  Every
+ *              row is written
+ *   flags      CVLC_GRAD_ACCUMULATE: add to d_dtable instead
+ *   d_workspace  device, 256-byte aligned, ws_bytes >=
+ *              cvlc_linear_xent_grad_workspace_bytes(n, vocab, dim, type, dtable_type)
+ *              (without d_dtable: of the table's type); holds no status word
+ * G is rounded to the type of 16-bit results, to 2^-18 of itself for an fp32
+ * dtable of 16-bit matrices; entries below 2^-36 of the largest weight may be lost
+ * in fp16. */
+size_t cvlc_linear_xent_grad_workspace_bytes(uint32_t n, uint32_t vocab, uint32_t dim, uint32_t type, uint32_t dtable_type);
+int cvlc_linear_xent_grad(uint32_t n, uint32_t vocab, uint32_t dim, const void* d_hidden, uint64_t hidden_stride,
+                          const void* d_table, uint64_t table_stride, uint32_t type, const void* d_labels,
+                          uint32_t id_bytes, float scale, const float* d_weights, const float* d_stats, void* d_dhidden,
+                          uint64_t dhidden_stride, void* d_dtable, uint32_t dtable_type, uint64_t dtable_stride,
+                          uint32_t flags, void* d_workspace, size_t ws_bytes, uint32_t* d_status, void* hip_stream);
+
 /* A gated linear recurrence, channel by channel, over sequences of rows: with
  * f = 1 / (1 + exp(-gate)),
  *   h_t = f_t h_(t-1) + (1 - f_t) x_t.

@@ -6,7 +6,7 @@ from __future__ import annotations
 
 import numpy as np
 
-from .local_step import U
+from .local_step import U, depth
 
 # ----------------------------------------------------------------------------- AdamW
 BLOCK, TOP, TINY = 256, 448.0, 2.0 ** -100
@@ -133,3 +133,55 @@ def gated_scan_grad(dy, x, gate, h, bounds, h0=None, dlast=None):
             far = f[t] * far + 16 * U * size + 2.0 ** -126
         dh0[s], off_0[s] = c, far
     return dx, off_x, dgate, off_g, dh0, off_0
+
+
+# ----------------------------------------------------------------------------- the loss over a vocabulary
+ROUNDS = {("f32", "f32"): 2.0 ** -23, ("bf16", "f32"): 2.0 ** -17, ("f16", "f32"): 2.0 ** -21, ("bf16", "bf16"): 2.0 ** -8, ("f16", "f16"): 2.0 ** -11}
+
+
+def linear_xent(hidden, table, labels, scale=1.0, weights=None, cut=0.0):
+    """Losses, stats (m, S), and what the gradients need; with how far off each.  `cut`: what of a product's term is left out.
+    A logit is a sum of fp32 terms in any order."""
+    h, t = hidden.astype(np.float64), table.astype(np.float64)
+    n, vocab, dim = h.shape[0], t.shape[0], h.shape[1]
+    s = float(np.float32(scale))
+    labels = np.asarray(labels)
+    w = np.ones(n) if weights is None else np.asarray(weights, np.float64)
+    live = (labels >= 0) & (labels < vocab) & (w != 0)
+    h = np.where(live[:, None], h, 0.0)
+    z = s * (h @ t.T)
+    far = abs(s) * (np.abs(h) @ np.abs(t).T) * ((dim + 2) * U + cut) + 2 * U * np.abs(z)
+    m = z.max(1)
+    off_m = far.max(1)
+    d = z - m[:, None]
+    rel = far + off_m[:, None] + (4 * np.abs(d) + 6) * U
+    e = np.exp(d)
+    S = e.sum(1)
+    rel_S = (e * rel).sum(1) / S + (depth(vocab) + 8) * U
+    at = np.where(live, labels, 0)
+    rows = np.arange(n)
+    loss = np.where(live, w * (np.log(S) - d[rows, at]), 0.0)
+    tol = np.where(live, np.abs(w) * (rel_S + far[rows, at] + off_m + 4 * U * (np.abs(np.log(S)) + np.abs(d[rows, at]) + np.abs(m))) + 4 * U * np.abs(loss), 0.0)
+    stats = np.where(live[:, None], np.stack([m, S], 1), 0.0)
+    stats_tol = np.where(live[:, None], np.stack([off_m, S * (rel_S + off_m)], 1), 0.0)
+    p = e / S[:, None]
+    G = p.copy()
+    G[rows, at] -= 1.0
+    off_G = p * (rel + rel_S[:, None] + 4 * U) + 4 * U * np.abs(G)
+    mask = (live * np.where(live, w, 0.0) * s)[:, None]
+    return loss, tol, stats, stats_tol, G * mask, off_G * np.abs(mask), h, t
+
+
+def linear_xent_grad(G, off_G, h, t, round_h, round_t, cut=0.0, start=None):
+    """dh and dT and how far off: G is rounded (`round_h`, `round_t` of itself, beside what fp16 may lose below), terms are
+    added in fp32 in any order, in pieces that are added in turn."""
+    n, vocab = G.shape
+    lost = 2.0 ** -37 * np.abs(G).max() if G.size else 0.0
+    dh, dt = G @ t, G.T @ h
+    size = np.abs(G)
+    off_h = (off_G + round_h * size + lost) @ np.abs(t) + ((vocab + 8) * U + cut) * (size @ np.abs(t)) + 3 * U * np.abs(dh)
+    off_t = (off_G + round_t * size + lost).T @ np.abs(h) + ((n + 8) * U + cut) * (size.T @ np.abs(h)) + 3 * U * np.abs(dt)
+    if start is not None:
+        dt = dt + start
+        off_t = off_t + U * np.abs(dt)
+    return dh, off_h, dt, off_t

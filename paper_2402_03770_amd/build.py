@@ -10,7 +10,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libcvlc.so")
 SOURCES = ["cvlc_plan.cpp", "cvlc_encode.hip", "cvlc_decode.hip", "cvlc_rank.hip", "cvlc_packet.hip", "cvlc_embed.hip",
            "cvlc_norm.hip", "cvlc_distill.hip", "cvlc_adamw.hip",
-           "cvlc_scan.hip"]
+           "cvlc_scan.hip", "cvlc_xent.hip"]
 HEADERS = ["cvlc_common.h", "cvlc_select.h", "cvlc_elem.h"]
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",

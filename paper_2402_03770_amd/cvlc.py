@@ -157,6 +157,13 @@ def lib() -> C.CDLL:
         L.cvlc_distill.argtypes = [u32, u32, vp, u32, u64, u32, vp, u32, vp, u32, f32, u32, vp, vp, vp, vp, u64, vp,
                                    C.c_size_t, vp, vp]
         L.cvlc_distill_grad.argtypes = [u32, u32, vp, u32, u64, u32, vp, u32, vp, u32, f32, u32, vp, vp, vp, u64, vp, vp]
+        L.cvlc_linear_xent_workspace_bytes.argtypes = [u32, u32, u32, u32]
+        L.cvlc_linear_xent_workspace_bytes.restype = C.c_size_t
+        L.cvlc_linear_xent.argtypes = [u32, u32, u32, vp, u64, vp, u64, u32, vp, u32, f32, vp, vp, vp, vp, C.c_size_t, vp, vp]
+        L.cvlc_linear_xent_grad_workspace_bytes.argtypes = [u32, u32, u32, u32, u32]
+        L.cvlc_linear_xent_grad_workspace_bytes.restype = C.c_size_t
+        L.cvlc_linear_xent_grad.argtypes = [u32, u32, u32, vp, u64, vp, u64, u32, vp, u32, f32, vp, vp, vp, u64, vp, u32, u64, u32, vp,
+                                            C.c_size_t, vp, vp]
         L.cvlc_gated_scan_workspace_bytes.argtypes = [u32, u32, u32]
         L.cvlc_gated_scan_workspace_bytes.restype = C.c_size_t
         L.cvlc_gated_scan.argtypes = [u32, u32, vp, u64, vp, u64, u32, u32, vp, u32, vp, vp, u64, vp, vp, C.c_size_t, vp, vp]
@@ -593,6 +600,72 @@ def distill_grad(logits: torch.Tensor, teacher_ids: torch.Tensor, teacher_values
     _check(lib().cvlc_distill_grad(n, vocab, zp, zt, zs, k, teacher_ids.data_ptr(), size, teacher_values.data_ptr(),
                                    kind, temperature, DISTILL_LOGPROBS if logprobs else 0, wp, sp, dp, ds, st,
                                    stream), what)
+
+
+def _kind(dtype: torch.dtype) -> int:
+    if dtype not in _TYPES:
+        _refuse("cvlc_linear_xent", f"{dtype} is not float32, bfloat16 or float16")
+    return _TYPES[dtype]
+
+
+def linear_xent_workspace_bytes(n: int, vocab: int, dim: int, dtype: torch.dtype) -> int:
+    return int(lib().cvlc_linear_xent_workspace_bytes(n, vocab, dim, _kind(dtype)))
+
+
+def linear_xent_grad_workspace_bytes(n: int, vocab: int, dim: int, dtype: torch.dtype, dtable_dtype: Optional[torch.dtype] = None) -> int:
+    kind = _kind(dtype)
+    return int(lib().cvlc_linear_xent_grad_workspace_bytes(n, vocab, dim, kind, kind if dtable_dtype is None else _kind(dtable_dtype)))
+
+
+def _logits_of(what: str, hidden: torch.Tensor, table: torch.Tensor, labels: torch.Tensor, weights: Optional[torch.Tensor],
+               workspace: torch.Tensor):
+    """Sizes and the arguments that the loss and its gradients share."""
+    if hidden.dim() != 2 or table.dim() != 2:
+        _refuse(what, "hidden or table is not a matrix")
+    (n, dim), vocab = hidden.shape, table.shape[0]
+    hp, kind, hs = _matrix(what, "hidden", hidden, n, dim)
+    tp, other, ts = _matrix(what, "table", table, vocab, dim)
+    if other != kind:
+        _refuse(what, "hidden and table are not of one type")
+    size = _id_bytes(what, "labels", labels, 1)
+    if labels.numel() != n:
+        _refuse(what, f"labels are {labels.numel()}, not {n}")
+    return n, vocab, dim, kind, (n, vocab, dim, hp, hs, tp, ts, kind, labels.data_ptr(), size), _vector(what, "weights", weights, (n,))
+
+
+def linear_xent(hidden: torch.Tensor, table: torch.Tensor, labels: torch.Tensor, loss_out: Optional[torch.Tensor], workspace: torch.Tensor,
+                scale: float = 1.0, weights: Optional[torch.Tensor] = None, stats_out: Optional[torch.Tensor] = None,
+                status: Optional[torch.Tensor] = None) -> None:
+    """cvlc_linear_xent on the current stream: every row's softmax cross entropy (float32, n entries) of the logits
+    scale * hidden @ table.T, which are never kept.  `hidden` is (n, dim), `table` (vocab, dim) of the same type, `labels` an int32
+    or int64 tensor of n tokens, negative ones for padding; `weights` float32 of n entries or None; `stats_out` an optional
+    float32 (n, 2) for linear_xent_grad; `workspace` holds linear_xent_workspace_bytes(n, vocab, dim, dtype)."""
+    what = "cvlc_linear_xent"
+    n, vocab, dim, kind, args, wp = _logits_of(what, hidden, table, labels, weights, workspace)
+    lp, sp, st = _vector(what, "loss_out", loss_out, (n,)), _vector(what, "stats_out", stats_out, (n, 2)), _status(what, status)
+    stream = _stream_of(what, hidden, table, labels, weights, loss_out, stats_out, workspace, status)
+    _check(lib().cvlc_linear_xent(*args, scale, wp, lp, sp, workspace.data_ptr(), workspace.numel(), st, stream), what)
+
+
+def linear_xent_grad(hidden: torch.Tensor, table: torch.Tensor, labels: torch.Tensor, stats: torch.Tensor, dhidden: Optional[torch.Tensor],
+                     dtable: Optional[torch.Tensor], workspace: torch.Tensor, scale: float = 1.0, weights: Optional[torch.Tensor] = None,
+                     accumulate: bool = False, status: Optional[torch.Tensor] = None) -> None:
+    """cvlc_linear_xent_grad on the current stream: the gradients of the losses' sum from the statistics that linear_xent kept.
+    `dhidden` is of hidden's type, `dtable` float32 (as a slice of an update vector is) or of the table's, added to with
+    `accumulate`; either may be None.  `workspace` holds linear_xent_grad_workspace_bytes(n, vocab, dim, dtype, dtable's)."""
+    what = "cvlc_linear_xent_grad"
+    n, vocab, dim, kind, args, wp = _logits_of(what, hidden, table, labels, weights, workspace)
+    sp, st = _vector(what, "stats", stats, (n, 2)), _status(what, status)
+    dhp, dhs, dtp, dtt, dts = None, 0, None, kind, 0
+    if dhidden is not None:
+        dhp, other, dhs = _matrix(what, "dhidden", dhidden, n, dim)
+        if other != kind:
+            _refuse(what, "dhidden is not of hidden's type")
+    if dtable is not None:
+        dtp, dtt, dts = _matrix(what, "dtable", dtable, vocab, dim)
+    stream = _stream_of(what, hidden, table, labels, weights, stats, dhidden, dtable, workspace, status)
+    _check(lib().cvlc_linear_xent_grad(*args, scale, wp, sp, dhp, dhs, dtp, dtt, dts, GRAD_ACCUMULATE if accumulate else 0,
+                                       workspace.data_ptr(), workspace.numel(), st, stream), what)
 
 
 def gated_scan_workspace_bytes(n: int, dim: int, sequences: int) -> int:

@@ -529,3 +529,215 @@ def test_gated_scan_refusals_on_the_host():
                dict(status=ok + 1)):
         assert step(**kw) == cv.ERR_ARG, kw
     assert step(n=0, x=None, gate=None, h=None, states=None) == 0
+
+
+# ----------------------------------------------------------------------------- the loss over a vocabulary
+NAMES = {F32: "f32", BF16: "bf16", F16: "f16"}
+
+
+class Xent:
+    def __init__(self, n, dim, vocab, dtype, dtable=None, extra=0, offset=0, weights=True, padding=0.2, seed=1, spread=2.0, kind=torch.int64):
+        self.n, self.dim, self.vocab, self.dtype, self.dtable_type = n, dim, vocab, dtype, dtable or dtype
+        self.hidden = random_matrix(n, dim, dtype, seed, extra, offset)
+        self.table = random_matrix(vocab, dim, dtype, seed + 1, extra, offset, scale=spread * dim ** -0.5)
+        self.labels = tokens(n, vocab, seed + 2, padding, kind).to(DEV)
+        g = torch.Generator().manual_seed(seed + 3)
+        self.weights = None
+        if weights:
+            self.weights = (torch.rand(n, generator=g) / n).to(DEV)
+            self.weights[::7] = 0.0
+        self.loss, self.stats = torch.full((n,), 7.0, device=DEV), torch.full((n, 2), 7.0, device=DEV)
+        self.dhidden, self.dhidden_flat = matrix(n, dim, dtype, extra, offset, fill=5.0)
+        self.dtable, self.dtable_flat = matrix(vocab, dim, self.dtable_type, extra, offset, fill=5.0)
+        need = max(cv.linear_xent_workspace_bytes(n, vocab, dim, dtype), cv.linear_xent_grad_workspace_bytes(n, vocab, dim, dtype, self.dtable_type))
+        self.ws = cv.new_workspace(need, DEV)
+        self.ws.fill_(0xFF)                                            # NaN in every type
+        self.status = torch.zeros(1, dtype=torch.int32, device=DEV)
+
+    def forward(self, scale=1.0):
+        cv.linear_xent(self.hidden, self.table, self.labels, self.loss, self.ws, scale=scale, weights=self.weights, stats_out=self.stats, status=self.status)
+
+    def backward(self, scale=1.0, accumulate=False, dhidden=True, dtable=True):
+        cv.linear_xent_grad(self.hidden, self.table, self.labels, self.stats, self.dhidden if dhidden else None, self.dtable if dtable else None, self.ws,
+                            scale=scale, weights=self.weights, accumulate=accumulate, status=self.status)
+
+    def check(self, scale=1.0, start=None, dhidden=True, dtable=True):
+        name, out = NAMES[self.dtype], NAMES[self.dtable_type]
+        cut = 2.0 ** -22 if self.dtype == F32 else 0.0
+        hidden = np.nan_to_num(f64(self.hidden)) * (self.labels.cpu().numpy() >= 0)[:, None]
+        loss, tol, stats, stats_tol, G, off_G, h, t = ref.linear_xent(hidden, f64(self.table), self.labels.cpu().numpy(), scale,
+                                                                      None if self.weights is None else f64(self.weights), cut)
+        assert_near(self.loss, loss, tol, F32, "loss")
+        assert_near(self.stats, stats, stats_tol, F32, "stats")
+        dh, off_h, dt, off_t = ref.linear_xent_grad(G, off_G, h, t, ref.ROUNDS[name, name], ref.ROUNDS[name, out], cut, start)
+        for on, m, flat, want, off, kind, what in ((dhidden, self.dhidden, self.dhidden_flat, dh, off_h, self.dtype, "dhidden"),
+                                                   (dtable, self.dtable, self.dtable_flat, dt, off_t, self.dtable_type, "dtable")):
+            if on:
+                assert_near(m, want, off, kind, what)
+                assert untouched(flat, m, 5.0), what
+            else:
+                assert bool((flat == 5.0).all()), what
+
+
+XENT_TYPES = [(F32, F32), (BF16, F32), (BF16, BF16), (F16, F32), (F16, F16)]
+
+
+@gpu
+@pytest.mark.parametrize("dtype,dtable", XENT_TYPES)
+@pytest.mark.parametrize("n,dim,vocab,extra,offset", [(1, 1, 1, 0, 0), (3, 5, 7, 1, 1), (64, 64, 1000, 0, 0), (33, 100, 300, 3, 1), (130, 128, 257, 8, 8),
+                                                      (32, 65, 2049, 0, 0), (257, 192, 1030, 1, 1)])
+def test_linear_xent(dtype, dtable, n, dim, vocab, extra, offset):
+    x = Xent(n, dim, vocab, dtype, dtable, extra, offset, weights=n != 64, kind=torch.int32 if n % 2 else torch.int64)
+    if n > 1:
+        x.hidden[x.labels < 0] = float("nan")                          # padded rows may hold anything
+    x.forward(0.7)
+    x.backward(0.7)
+    x.check(0.7)
+    assert x.status.item() == 0
+
+
+@gpu
+@pytest.mark.parametrize("dtype,dtable,n,dim,vocab", [(BF16, F32, 2100, 128, 8000), (F16, F16, 100, 1536, 8200), (BF16, BF16, 3200, 4096, 300),
+                                                      (F32, F32, 2000, 64, 20000), (F32, F32, 700, 300, 3000)])
+def test_linear_xent_of_large_tiles_and_pieces(dtype, dtable, n, dim, vocab):
+    """Sizes at which every product takes the large tiles, and at which the vocabulary goes in several pieces."""
+    x = Xent(n, dim, vocab, dtype, dtable, weights=False)
+    x.forward()
+    x.backward()
+    x.check()
+
+
+@gpu
+@pytest.mark.parametrize("dtype,dtable", XENT_TYPES)
+def test_linear_xent_gradients_alone_and_added(dtype, dtable):
+    x = Xent(90, 72, 500, dtype, dtable)
+    x.forward()
+    x.backward(dtable=False)
+    x.check(dtable=False)
+    x = Xent(90, 72, 500, dtype, dtable)
+    x.forward()
+    x.backward(dhidden=False)
+    x.check(dhidden=False)
+    start = f64(random_matrix(500, 72, dtable, 9, scale=1e-3))
+    x.dtable.copy_(torch.from_numpy(start))
+    x.dhidden.fill_(5.0)
+    x.backward(accumulate=True, dhidden=False)
+    x.check(dhidden=False, start=start)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("weight", [1e-30, 1e-6, 1e6, 1e25])
+def test_linear_xent_of_far_weights(dtype, weight):
+    """Weights far from 1, among them rows a millionth of the others: G is scaled, so all keep their bits."""
+    x = Xent(80, 64, 300, dtype, F32, padding=0.0)
+    x.weights = torch.full((80,), weight, device=DEV)
+    x.weights[::3] *= 1e-6
+    if dtype == F16:                                                   # dhidden of such weights is beyond its type
+        x.weights *= min(1.0, 1e3 / weight) if weight > 1 else 1.0
+    x.forward()
+    x.backward()
+    x.check()
+
+
+@gpu
+def test_linear_xent_without_rows_or_loss():
+    x = Xent(0, 16, 30, F32)
+    x.forward()
+    x.backward()
+    assert not x.dtable.any() and untouched(x.dtable_flat, x.dtable, 5.0)
+    x.dtable.fill_(3.0)
+    x.backward(accumulate=True)
+    assert bool((x.dtable == 3.0).all())
+    x = Xent(20, 16, 30, BF16, F32)
+    x.labels.fill_(-1)
+    x.hidden.fill_(float("nan"))
+    x.forward()
+    x.backward()
+    assert not x.loss.any() and not x.stats.any() and not x.dhidden.any() and not x.dtable.any()
+
+
+@gpu
+def test_linear_xent_labels_beyond_the_vocabulary():
+    x = Xent(40, 24, 100, F32, weights=False)
+    x.labels[3], x.labels[5] = 100, 2 ** 40
+    x.forward()
+    assert x.status.item() == cv.DEV_INDEX
+    x.status.zero_()
+    x.backward()
+    assert x.status.item() == cv.DEV_INDEX
+    x.labels[[3, 5]] = -1
+    x.check()
+
+
+@gpu
+def test_linear_xent_grad_against_differences():
+    """Gradients along a random way against central differences of the oracle's loss in 64 bits."""
+    x = Xent(20, 12, 50, F32)
+    x.forward()
+    x.backward()
+    rng = np.random.default_rng(5)
+    args = [f64(x.hidden), f64(x.table)]
+    for k, got in enumerate((x.dhidden, x.dtable)):
+        way, step = rng.standard_normal(args[k].shape), 1e-4
+        ends = [ref.linear_xent(*(a + sign * step * way if i == k else a for i, a in enumerate(args)), x.labels.cpu().numpy(), 1.0, f64(x.weights))[0].sum()
+                for sign in (1, -1)]
+        want = (ends[0] - ends[1]) / (2 * step)
+        # a third derivative of some tens of logits cubed (weights add up to 1 at most) times step^2, and fp32's roundings
+        assert abs((f64(got) * way).sum() - want) <= 1e-6 + 1e-5 * np.abs(f64(got) * way).sum()
+
+
+@gpu
+def test_linear_xent_repeats_its_bits():
+    x = Xent(500, 200, 3001, BF16, F32)
+    x.forward()
+    x.backward()
+    kept = [t.clone() for t in (x.loss, x.stats, x.dhidden, x.dtable)]
+    for _ in range(3):
+        x.ws.fill_(0xFF)
+        x.forward()
+        x.backward()
+        assert all(torch.equal(a, b) for a, b in zip(kept, (x.loss, x.stats, x.dhidden, x.dtable)))
+
+
+def test_linear_xent_refusals():
+    def t(*shape, dtype=F32):
+        return torch.zeros(*shape, dtype=dtype)
+
+    h, table, labels, ws = t(6, 4), t(9, 4), t(6, dtype=torch.int64), torch.zeros(1 << 20, dtype=torch.uint8)
+    good = dict(hidden=h, table=table, labels=labels, loss_out=t(6), workspace=ws)
+    for kw in (dict(hidden=t(6)), dict(table=t(9, 5)), dict(table=t(9, 4, dtype=BF16)), dict(labels=t(6)), dict(labels=labels[:5]), dict(loss_out=t(5)),
+               dict(weights=t(6, dtype=BF16)), dict(stats_out=t(6)), dict(status=t(1)), dict(hidden=t(4, 6).t()), dict()):   # the last: on no GPU
+        assert refused(cv.linear_xent, **(good | kw)), kw
+    good = dict(hidden=h, table=table, labels=labels, stats=t(6, 2), dhidden=t(6, 4), dtable=t(9, 4), workspace=ws)
+    for kw in (dict(stats=t(6)), dict(dhidden=t(6, 4, dtype=F16)), dict(dtable=t(8, 4)), dict(dtable=t(9, 4, dtype=torch.float64)), dict()):
+        assert refused(cv.linear_xent_grad, **(good | kw)), kw
+    assert refused(cv.linear_xent_workspace_bytes, 6, 9, 4, torch.float64)
+
+
+def test_linear_xent_refusals_on_the_host():
+    lib, ok = cv.lib(), 1 << 20
+    need = lib.cvlc_linear_xent_workspace_bytes(6, 9, 4, 1)
+
+    def loss(**kw):
+        a = dict(n=6, vocab=9, dim=4, h=ok, hs=4, t=ok, ts=4, kind=1, labels=ok, size=8, scale=1.0, w=None, loss=ok, stats=None, ws=ok, bytes=need, status=None) | kw
+        return lib.cvlc_linear_xent(*a.values(), None)
+
+    for kw in (dict(vocab=0), dict(dim=0), dict(dim=(1 << 20) + 1, hs=1 << 21, ts=1 << 21), dict(n=(1 << 22) + 1), dict(h=None), dict(h=ok + 1), dict(hs=3), dict(t=ok + 1),
+               dict(ts=3), dict(kind=3), dict(labels=None), dict(labels=ok + 4), dict(size=2), dict(scale=float("nan")), dict(w=ok + 2), dict(loss=None),
+               dict(loss=ok + 2), dict(stats=ok + 4), dict(ws=None), dict(ws=ok + 4), dict(status=ok + 2), dict(n=1 << 22, vocab=1 << 20)):
+        assert loss(**kw) == cv.ERR_ARG, kw
+    assert loss(bytes=need - 1) == -4
+    assert loss(n=0, h=None, t=None, labels=None, loss=None) == 0
+    need = lib.cvlc_linear_xent_grad_workspace_bytes(6, 9, 4, 1, 0)
+
+    def grad(**kw):
+        a = dict(n=6, vocab=9, dim=4, h=ok, hs=4, t=ok, ts=4, kind=1, labels=ok, size=4, scale=1.0, w=None, stats=ok, dh=ok, dhs=4, dt=ok, dtt=0, dts=4, flags=0,
+                 ws=ok, bytes=need, status=None) | kw
+        return lib.cvlc_linear_xent_grad(*a.values(), None)
+
+    for kw in (dict(stats=None), dict(stats=ok + 4), dict(dh=None, dt=None), dict(dh=ok + 1), dict(dhs=3), dict(dt=ok + 2), dict(dtt=2), dict(dts=3), dict(flags=2),
+               dict(kind=0, dtt=1)):
+        assert grad(**kw) == cv.ERR_ARG, kw
+    assert grad(bytes=need - 1) == -4
+    assert grad(n=0, h=None, t=None, labels=None, stats=None, dt=None) == 0
