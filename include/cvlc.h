@@ -462,8 +462,9 @@ int cvlc_distill_grad(uint32_t n, uint32_t vocab, const void* d_logits, uint32_t
  *   d_status   as for cvlc_embed
  * A row of padding or of weight 0 is not looked at: loss, statistics and gradient
  * are zeros.  Other rows, and the table, must be finite, and so must their logits.
- * Products are exact in 16-bit types and to 2^-23 of a term or better in fp32,
- * sums are fp32.  The call is made of launches whose threads number fewer than
+ * Products are exact in 16-bit types; fp32 elements are held to 2^-23 of
+ * themselves or 2^-39 of their matrix's largest, products to 2^-22; sums are
+ * fp32.  The call is made of launches whose threads number fewer than
  * 2^32, and sizes that this does not hold are refused (2^19 rows of a vocabulary
  * of 2^17 are not). */
 size_t cvlc_linear_xent_workspace_bytes(uint32_t n, uint32_t vocab, uint32_t dim, uint32_t type);
@@ -485,9 +486,9 @@ int cvlc_linear_xent(uint32_t n, uint32_t vocab, uint32_t dim, const void* d_hid
  *   d_workspace  device, 256-byte aligned, ws_bytes >=
  *              cvlc_linear_xent_grad_workspace_bytes(n, vocab, dim, type, dtable_type)
  *              (without d_dtable: of the table's type); holds no status word
- * G is rounded to the type of 16-bit results, to 2^-18 of itself for an fp32
- * dtable of 16-bit matrices; entries below 2^-36 of the largest weight may be lost
- * in fp16. */
+ * G is rounded to the type of 16-bit results; for fp32 results to 2^-18 of itself
+ * beside bfloat16 matrices, else to 2^-23.  Beside others than bfloat16 it loses
+ * what is below 2^-38 of scale times the largest weight. */
 size_t cvlc_linear_xent_grad_workspace_bytes(uint32_t n, uint32_t vocab, uint32_t dim, uint32_t type, uint32_t dtable_type);
 int cvlc_linear_xent_grad(uint32_t n, uint32_t vocab, uint32_t dim, const void* d_hidden, uint64_t hidden_stride,
                           const void* d_table, uint64_t table_stride, uint32_t type, const void* d_labels,

@@ -151,6 +151,8 @@ def linear_xent(hidden, table, labels, scale=1.0, weights=None, cut=0.0):
     h = np.where(live[:, None], h, 0.0)
     z = s * (h @ t.T)
     far = abs(s) * (np.abs(h) @ np.abs(t).T) * ((dim + 2) * U + cut) + 2 * U * np.abs(z)
+    if cut:                                                     # elements far below their matrix's largest
+        far = far + abs(s) * 2.0 ** -38 * (np.abs(t).max() * np.abs(h).sum(1)[:, None] + np.abs(h).max() * np.abs(t).sum(1))
     m = z.max(1)
     off_m = far.max(1)
     d = z - m[:, None]
@@ -181,6 +183,9 @@ def linear_xent_grad(G, off_G, h, t, round_h, round_t, cut=0.0, start=None):
     size = np.abs(G)
     off_h = (off_G + round_h * size + lost) @ np.abs(t) + ((vocab + 8) * U + cut) * (size @ np.abs(t)) + 3 * U * np.abs(dh)
     off_t = (off_G + round_t * size + lost).T @ np.abs(h) + ((n + 8) * U + cut) * (size.T @ np.abs(h)) + 3 * U * np.abs(dt)
+    if cut:
+        off_h = off_h + 2.0 ** -38 * np.abs(t).max() * size.sum(1)[:, None]
+        off_t = off_t + 2.0 ** -38 * np.abs(h).max() * size.sum(0)[:, None]
     if start is not None:
         dt = dt + start
         off_t = off_t + U * np.abs(dt)

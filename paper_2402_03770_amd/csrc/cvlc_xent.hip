@@ -4,14 +4,15 @@
 //
 // Products of matrices do nearly all the work: z once for the loss, once more for the gradients (a row's softmax needs its
 // whole sum first, and keeping z is what this call is there to avoid), then dh and dT.  All run on the matrix units from
-// 16-bit operands with K contiguous, sums in fp32:
+// 16-bit operands, sums in fp32:
 //   - bfloat16 and fp16 matrices as they are;
-//   - fp32 as three planes of bfloat16 (8 + 8 + 8 bits are its 24), of whose nine products the six largest are added: what is left
-//     out is below 2^-24 of a term.  An fp32 matrix instruction has a sixteenth of the rate.
+//   - fp32 as two planes of fp16 (11 + 11 bits) of the matrix times a power of two that brings its largest element to about 2^14;
+//     three of the four products of planes are added.  What is left out is below 2^-22 of a term, and an element is held to
+//     2^-23 of itself or 2^-39 of the largest.  An fp32 matrix instruction has a sixteenth of the rate.
 //   - G, in one plane where the result is of 16 bits (its rounding of 2^-9 or 2^-12 of a term is what the result's own is), in
-//     two where an fp32 gradient of the table is asked of 16-bit matrices (2^-18), in three beside fp32 matrices.
-// G is scaled by a power of two that brings the largest weight to about 2^13, so that neither tiny weights nor fp16 lose its
-// small entries.
+//     two for fp32 results (2^-18 in bfloat16, 2^-23 in fp16).
+// G is scaled so that the largest weight becomes 2^13: then neither tiny weights nor fp16 lose its small entries, and the
+// label's entry, softmax - 1, is next to a value that every type has.
 //
 // The loss's product ends in every tile's (max, sum of exponentials) per row, joined in order by a second launch.  The
 // gradients go over the vocabulary in pieces of a few thousand tokens whose G fits the last-level cache.
@@ -37,12 +38,12 @@ constexpr float kLift = 0x1p13f;   // G's largest entries
 uint64_t pad_to(uint64_t x, uint64_t to) { return (x + to - 1) / to * to; }
 
 // ------------------------------------------------------------------------------ planes
-// x as a sum of P values of a 16-bit type.  Three of bfloat16 cut bits off, which leaves the rest exact; one or two round.
+// x as a sum of P values of a 16-bit type.
 template <class H, uint32_t P>
 __device__ __forceinline__ void split(float x, Half (&out)[P]) {
 #pragma unroll
   for (uint32_t p = 0; p < P; ++p) {
-    const H h = P == 3 ? __builtin_bit_cast(H, (Half)(__float_as_uint(x) >> 16)) : (H)x;
+    const H h = (H)x;
     out[p] = __builtin_bit_cast(Half, h);
     x -= (float)h;
   }
@@ -63,87 +64,133 @@ struct Rows {
   }
 };
 
-// A matrix's planes, its rows as they are and turned; zeros beyond it up to whole tiles of K.
-constexpr uint32_t kPackSide = 64, kPackBlock = 256;
-struct PackArgs {
-  uint32_t rows, cols;
-  uint64_t stride;
-  Half *straight, *turned;          // either may be null
-  uint64_t straight_stride, straight_plane, turned_stride, turned_plane;
-  uint32_t masked;                  // rows that do not count become zeros
-  Rows who;
+// What a call's launches share, at the workspace's start.
+struct Factors {
+  float grad;               // by which G is multiplied ...
+  float back;               // ... and by which its products are then
+  float up[2], down[2];     // the same of hidden rows and table, powers of two
 };
 
-template <class T, class H, uint32_t P>
-__global__ __launch_bounds__(kPackBlock) void pack_kernel(PackArgs a, const T* src) {
-  __shared__ Half tile[P][kPackSide][kPackSide + 2];   // [column][row]
-  const uint32_t blocks = (a.cols + kPackSide - 1) / kPackSide;
-  const uint32_t r0 = blockIdx.x / blocks * kPackSide, c0 = blockIdx.x % blocks * kPackSide;
-  for (uint32_t k = threadIdx.x; k < kPackSide * kPackSide / 8; k += kPackBlock) {
-    const uint32_t r = k / 8, c = k % 8 * 8, row = r0 + r;
-    float x[8] = {};
-    if (row < a.rows && !(a.masked && !a.who.live(row))) load_row<8>(src + row * a.stride, c0 + c, a.cols, 0.0f, x);
-    Half h[P][8];
+constexpr uint32_t kSurveyBlock = 256, kSurveyGrid = 1024, kSurveyAlone = 1u << 17;
+struct Matrix {
+  const void* p;
+  uint64_t stride;
+  uint32_t rows;
+};
+
+// The largest magnitude of every workgroup's share of a matrix; rows that do not count are left out of the hidden ones.
+template <uint32_t THREADS>
+__device__ __forceinline__ float largest(const Matrix& m, uint32_t dim, const Rows* who, uint32_t part, uint32_t parts) {
+  const float* p = static_cast<const float*>(m.p);
+  const uint32_t across = (dim + 3) / 4;
+  const uint64_t all = (uint64_t)m.rows * across;
+  float top = 0.0f;
+  for (uint64_t k = (uint64_t)part * THREADS + threadIdx.x; k < all; k += (uint64_t)parts * THREADS) {
+    const uint32_t row = (uint32_t)(k / across), c = (uint32_t)(k % across) * 4;
+    if (who && !who->live(row)) continue;
+    float x[4];
+    load_row<4>(p + row * m.stride, c, dim, 0.0f, x);
 #pragma unroll
-    for (uint32_t i = 0; i < 8; ++i) {
-      Half part[P];
-      split<H, P>(x[i], part);
-#pragma unroll
-      for (uint32_t p = 0; p < P; ++p) {
-        h[p][i] = part[p];
-        tile[p][c + i][r] = part[p];
-      }
-    }
-    if (a.straight && row < a.rows)
-#pragma unroll
-      for (uint32_t p = 0; p < P; ++p)
-        *reinterpret_cast<Quad*>(a.straight + p * a.straight_plane + row * a.straight_stride + c0 + c) =
-            Quad{h[p][0] | (uint32_t)h[p][1] << 16, h[p][2] | (uint32_t)h[p][3] << 16, h[p][4] | (uint32_t)h[p][5] << 16,
-                 h[p][6] | (uint32_t)h[p][7] << 16};
+    for (uint32_t i = 0; i < 4; ++i) top = fmaxf(top, fabsf(x[i]));
   }
-  if (!a.turned) return;
+  return wave_max(top);
+}
+__global__ __launch_bounds__(kSurveyBlock) void survey_kernel(Matrix hidden, Matrix table, uint32_t dim, Rows who, float* tops) {
+  __shared__ float most[kSurveyBlock / kWave];
+  float top = blockIdx.y ? largest<kSurveyBlock>(table, dim, nullptr, blockIdx.x, gridDim.x)
+                         : largest<kSurveyBlock>(hidden, dim, &who, blockIdx.x, gridDim.x);
+  if (lane_id() == 0) most[wave_id()] = top;
   __syncthreads();
-  for (uint32_t k = threadIdx.x; k < kPackSide * kPackSide / 8; k += kPackBlock) {
-    const uint32_t c = k / 8, r = k % 8 * 8;
-    if (c0 + c >= a.cols) continue;
+  for (uint32_t w = 0; w < kSurveyBlock / kWave; ++w) top = fmaxf(top, most[w]);
+  if (threadIdx.x == 0) tops[blockIdx.y * gridDim.x + blockIdx.x] = top;
+}
+
+// The factors, and labels that are not there told of.  tops: what survey_kernel found (`parts` a matrix); null: small matrices,
+// looked over here, where they are given.
+__global__ __launch_bounds__(1024) void factors_kernel(Rows who, float scale, const float* tops, uint32_t parts, Matrix hidden, Matrix table,
+                                                       uint32_t dim, Factors* factors, uint32_t* status) {
+  __shared__ float most[3][16];
+  float m[3] = {0.0f, 0.0f, 0.0f};
+  bool wrong = false;
+  for (uint32_t i = threadIdx.x; i < who.n; i += 1024) {
+    wrong |= who.label(i) >= (int64_t)who.vocab;
+    if (who.live(i)) m[0] = fmaxf(m[0], fabsf(who.weight(i) * scale));
+  }
+  if (status && __ballot(wrong) && lane_id() == 0) atomicOr(status, CVLC_DEV_INDEX);
+  if (tops) {
+    for (uint32_t i = threadIdx.x; i < parts; i += 1024) {
+      m[1] = fmaxf(m[1], tops[i]);
+      m[2] = fmaxf(m[2], tops[parts + i]);
+    }
+  } else if (hidden.p) {
+    m[1] = largest<1024>(hidden, dim, &who, 0, 1);
+    m[2] = largest<1024>(table, dim, nullptr, 0, 1);
+  }
+#pragma unroll
+  for (uint32_t k = 0; k < 3; ++k) {
+    m[k] = wave_max(m[k]);
+    if (lane_id() == 0) most[k][wave_id()] = m[k];
+  }
+  __syncthreads();
+  if (threadIdx.x) return;
+  for (uint32_t k = 0; k < 3; ++k)
+    for (uint32_t w = 1; w < 16; ++w) m[k] = fmaxf(m[k], most[k][w]);
+  const bool some = m[0] >= 0x1p-100f && m[0] <= 0x1p100f;
+  factors->grad = some ? kLift / m[0] : 1.0f;
+  factors->back = some ? m[0] / kLift : 1.0f;
+  for (uint32_t k = 0; k < 2; ++k) {
+    const float top = m[k + 1];
+    const int e = top > 0.0f && top < INFINITY ? min(max(14 - ilogbf(top), -100), 100) : 0;
+    factors->up[k] = ldexpf(1.0f, e);
+    factors->down[k] = ldexpf(1.0f, -e);
+  }
+}
+
+// A matrix's planes with whole tiles of K in a row; zeros beyond it.
+constexpr uint32_t kPackBlock = 256;
+struct PackArgs {
+  Matrix from;
+  uint32_t cols, rows_to;           // rows that are written: those beyond the matrix's are zeros
+  Half* to;
+  uint64_t stride, plane;
+  const float* up;
+  uint32_t masked;                  // rows that do not count become zeros: they may hold anything, and G's zeros would not take a NaN away
+};
+template <class T, class H, uint32_t P>
+__global__ __launch_bounds__(kPackBlock) void pack_kernel(PackArgs first, PackArgs second, uint32_t grid, Rows who) {
+  const PackArgs& a = blockIdx.x < grid ? first : second;
+  const uint32_t block = blockIdx.x < grid ? blockIdx.x : blockIdx.x - grid, blocks = blockIdx.x < grid ? grid : gridDim.x - grid;
+  const uint32_t across = (uint32_t)(a.stride / 8);
+  const uint64_t all = (uint64_t)a.rows_to * across;
+  const float up = P > 1 ? *a.up : 1.0f;
+  for (uint64_t k = (uint64_t)block * kPackBlock + threadIdx.x; k < all; k += (uint64_t)blocks * kPackBlock) {
+    const uint32_t row = (uint32_t)(k / across), c = (uint32_t)(k % across) * 8;
+    float x[8] = {};
+    if (row < a.from.rows && !(a.masked && !who.live(row))) load_row<8>(static_cast<const T*>(a.from.p) + row * a.from.stride, c, a.cols, 0.0f, x);
+    Half h[8][P];
+#pragma unroll
+    for (uint32_t i = 0; i < 8; ++i) split<H, P>(P > 1 ? x[i] * up : x[i], h[i]);
 #pragma unroll
     for (uint32_t p = 0; p < P; ++p) {
       Quad q;
 #pragma unroll
-      for (uint32_t i = 0; i < 4; ++i) q[i] = tile[p][c][r + 2 * i] | (uint32_t)tile[p][c][r + 2 * i + 1] << 16;
-      *reinterpret_cast<Quad*>(a.turned + p * a.turned_plane + (c0 + c) * a.turned_stride + r0 + r) = q;
+      for (uint32_t i = 0; i < 4; ++i) q[i] = h[2 * i][p] | (uint32_t)h[2 * i + 1][p] << 16;
+      *reinterpret_cast<Quad*>(a.to + p * a.plane + row * a.stride + c) = q;
     }
   }
 }
 
-// factors[0]: by which G is scaled, factors[1]: by which its products are; labels that are not there are told of.
-__global__ __launch_bounds__(1024) void factors_kernel(Rows who, float scale, float* factors, uint32_t* status) {
-  __shared__ float most[16];
-  float m = 0.0f;
-  bool wrong = false;
-  for (uint32_t i = threadIdx.x; i < who.n; i += 1024) {
-    wrong |= who.label(i) >= (int64_t)who.vocab;
-    if (who.live(i)) m = fmaxf(m, fabsf(who.weight(i) * scale));
-  }
-  if (status && __ballot(wrong) && lane_id() == 0) atomicOr(status, CVLC_DEV_INDEX);
-  m = wave_max(m);
-  if (lane_id() == 0) most[wave_id()] = m;
-  __syncthreads();
-  if (threadIdx.x) return;
-  for (uint32_t w = 1; w < 16; ++w) m = fmaxf(m, most[w]);
-  const int e = m > 0.0f && m < INFINITY ? min(max(ilogbf(m), -100), 100) : 0;
-  factors[0] = ldexpf(kLift, -e);
-  factors[1] = ldexpf(1.0f / kLift, e);
-}
-
 // ------------------------------------------------------------------------------ the product
+// An operand is wide, its rows in memory those of the product and K along them, or tall, K from row to row.
 struct Operand {
   const Half* p;
   uint64_t stride, plane;   // elements from row to row, and from plane to plane
+  uint32_t along;           // tall: elements of a row that may be read, whole eights
+  uint32_t rows;            // rows that may be read; others are read as the last one, and count for nothing
 };
 struct Product {
-  Operand a, b;             // rows of both, K contiguous
-  uint32_t m, n;            // their numbers
+  Operand a, b;
+  uint32_t m, n;            // rows of a and of b
   uint32_t k_tiles;         // K in tiles of kDepth
   uint32_t pairs, a_planes, b_planes;  // which planes are multiplied: four bits a pair
   uint32_t slices;          // parts that all tiles of K are cut into
@@ -157,6 +204,8 @@ __device__ __forceinline__ Four mfma(Quad a, Quad b, Four c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(EightH, a), __builtin_bit_cast(EightH, b), c, 0, 0, 0);
 }
 
+constexpr uint32_t log2_of(uint32_t x) { return x < 2 ? 0 : 1 + log2_of(x / 2); }
+
 // A tile's shape: WM x WN wavefronts of MT x NT matrix instructions (16 x 16) each.
 template <uint32_t WM_, uint32_t WN_, uint32_t MT_, uint32_t NT_>
 struct Shape {
@@ -164,7 +213,72 @@ struct Shape {
   static constexpr uint32_t kStage = (TM + TN) * kDepth * 2;   // bytes of both operands' tiles
 };
 
-// Where a wavefront's lane has its values: value r of acc[i][j] is row m + 16 i + r, column n + 16 j.
+// One operand's tile in LDS: how it is fetched and read.  Tiles go straight to LDS, 16 bytes a lane in the order of the
+// lanes; where in memory a lane reads decides what lies where, and it is so that the lanes that read LDS together find
+// different banks:
+//   wide: a row has eight accesses, and sixteen rows are read at one K.  Access x of row r lies at x ^ key(r), with
+//     key in bits 1 to 3 of r, or, where a lane's results are `RUN` neighbouring rows (the MFMA's row i of sixteen is row
+//     RUN (i / 4) + i % 4 of the wavefront's then), in bit 1 and the two bits from RUN on.
+//   tall: sixteen neighbouring elements of a row are read from four rows by sixteen lanes, which hand them round (the read
+//     turns them).  Such a block b of row k lies at b ^ (k % 4 + 4 (k / 8 % 2)).
+template <bool TALL, uint32_t ROWS, uint32_t THREADS, uint32_t RUN>
+struct Tile {
+  static constexpr uint32_t kLoads = ROWS * 8 / THREADS;
+  static_assert(kLoads * THREADS == ROWS * 8, "whole loads");
+  uint32_t off[kLoads], placed;
+
+  static __device__ __forceinline__ uint32_t key(uint32_t r) {
+    return RUN ? (r >> 1 & 1) | (r >> log2_of(RUN) & 3) << 1 : r >> 1 & 7;
+  }
+  // Byte offsets from the tile's first row (and, tall, its first element) on, rows from `left` on being read as the one before.
+  __device__ __forceinline__ void place(const Operand& o, uint32_t first, uint32_t left) {
+    placed = left;
+#pragma unroll
+    for (uint32_t j = 0; j < kLoads; ++j) {
+      const uint32_t slot = j * THREADS + threadIdx.x;
+      if constexpr (TALL) {
+        constexpr uint32_t kAcross = ROWS / 8;
+        const uint32_t k = slot / kAcross, x = slot % kAcross, at = (x ^ ((k & 3) | (k >> 3 & 1) << 2) << 1) * 8;
+        off[j] = min(k, left - 1) * (uint32_t)(o.stride * 2) + min(at, o.along - first - 8) * 2;
+      } else {
+        const uint32_t r = slot / 8;
+        off[j] = min(r, left - 1) * (uint32_t)(o.stride * 2) + ((slot & 7) ^ key(r)) * 16;
+      }
+    }
+  }
+  __device__ __forceinline__ void fetch(const Operand& o, uint32_t plane, uint32_t first, uint32_t k, uint8_t* to) {
+    if constexpr (TALL) {
+      const uint32_t left = min(o.rows - k, kDepth);
+      if (left != placed) place(o, first, left);   // the last tile of K, and the first one of the next planes
+    }
+    const uint8_t* p = reinterpret_cast<const uint8_t*>(o.p + plane * o.plane + (TALL ? k * o.stride + first : first * o.stride + k));
+#pragma unroll
+    for (uint32_t j = 0; j < kLoads; ++j)
+      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(p + off[j]),
+                                       (__attribute__((address_space(3))) void*)(to + j * THREADS * 16), 16, 0, 0);
+  }
+  // What a lane takes to one matrix instruction: its row, the i-th sixteen of those from `rows` on, at 8 values of K, in the
+  // k-th half of the tile.
+  static __device__ __forceinline__ Quad read(const uint8_t* tile, uint32_t rows, uint32_t i, uint32_t k) {
+    const uint32_t lane = lane_id(), row = lane & 15, part = lane >> 4;
+    if constexpr (TALL) {
+      typedef short Turned __attribute__((ext_vector_type(4)));
+      const uint32_t at = k * 32 + part * 8 + (row >> 2);             // and four rows on: the same bits of the order
+      const uint32_t block = rows / 16 + i, where = (block ^ ((at & 3) | (at >> 3 & 1) << 2)) * 32 + (row & 3) * 8;
+      const uint8_t* p = tile + at * (ROWS * 2) + where;
+      auto turned = [](const uint8_t* q) {
+        return __builtin_bit_cast(Pair, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) Turned*)q));
+      };
+      const Pair low = turned(p), high = turned(p + 4 * (ROWS * 2));
+      return Quad{low[0], low[1], high[0], high[1]};
+    } else {
+      const uint32_t r = rows + (RUN ? (row >> 2) * RUN + i * 4 + (row & 3) : i * 16 + row);
+      return *reinterpret_cast<const Quad*>(tile + r * 128 + ((k * 4 + part) ^ key(r)) * 16);
+    }
+  }
+};
+
+// Where a wavefront's lane has its values: value r of acc[i][j] is row m + step i + r, column n + 16 j.
 struct Spot {
   uint32_t tile_m, tile_n, slice;   // of the workgroup
   uint32_t m0, n0;                  // the workgroup's first row and column
@@ -187,9 +301,11 @@ __device__ __forceinline__ void place(const Product& g, uint32_t tm, uint32_t tn
   s.tile_n = within / rows;
 }
 
-template <class H, class S, class E>
+// A wide first operand's results are runs of neighbouring rows in a lane.
+template <class H, class S, bool TALL_A, bool TALL_B, class E>
 __global__ __launch_bounds__(S::kThreads) void product_kernel(Product g, E epilogue) {
   __shared__ __attribute__((aligned(128))) uint8_t lds[2 * S::kStage];
+  constexpr uint32_t kRun = TALL_A ? 0 : S::MT * 4;
   const uint32_t lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(wave_id());
   Spot s;
   place(g, S::TM, S::TN, s);
@@ -197,63 +313,55 @@ __global__ __launch_bounds__(S::kThreads) void product_kernel(Product g, E epilo
   s.n0 = s.tile_n * S::TN;
   s.wm = wave / S::WN;
   s.wn = wave % S::WN;
-  s.m = s.m0 + s.wm * S::MT * 16 + (lane >> 4) * 4;
+  s.m = s.m0 + s.wm * S::MT * 16 + (lane >> 4) * (kRun ? kRun : 4);
   s.n = s.n0 + s.wn * S::NT * 16 + (lane & 15);
   const uint32_t all = g.pairs * g.k_tiles, per = (all + g.slices - 1) / g.slices;
   const uint32_t from = min(s.slice * per, all), to = min(from + per, all);
-  // Tiles go straight to LDS, 16 bytes a lane in the order of the lanes.  A row's eight accesses lie there in an order that
-  // depends on the row, so that the sixteen rows that a matrix instruction reads at one K are in sixteen different banks.
-  constexpr uint32_t kLoadsA = S::TM * 8 / S::kThreads, kLoadsB = S::TN * 8 / S::kThreads;
-  static_assert(kLoadsA * S::kThreads == S::TM * 8 && kLoadsB * S::kThreads == S::TN * 8, "whole loads");
-  uint32_t off_a[kLoadsA], off_b[kLoadsB];
-  {
-    const uint32_t slot = threadIdx.x, at = ((slot & 7) ^ ((slot >> 4) & 7)) * 16;
-    static_assert(S::kThreads % 128 == 0, "the order of accesses repeats every sixteen rows");
-#pragma unroll
-    for (uint32_t j = 0; j < kLoadsA; ++j)  // rows beyond the last one are read as the last one
-      off_a[j] = min((j * S::kThreads + slot) / 8, g.m - 1 - s.m0) * (uint32_t)(g.a.stride * 2) + at;
-#pragma unroll
-    for (uint32_t j = 0; j < kLoadsB; ++j) off_b[j] = min((j * S::kThreads + slot) / 8, g.n - 1 - s.n0) * (uint32_t)(g.b.stride * 2) + at;
-  }
-  auto fetch = [&](uint32_t tile, uint32_t stage) {
+  using TileA = Tile<TALL_A, S::TM, S::kThreads, kRun>;
+  using TileB = Tile<TALL_B, S::TN, S::kThreads, 0>;
+  TileA ta;
+  TileB tb;
+  ta.place(g.a, s.m0, TALL_A ? kDepth : g.a.rows - s.m0);
+  tb.place(g.b, s.n0, TALL_B ? kDepth : g.b.rows - s.n0);
+  auto fetch = [&](uint32_t tile) {
     const uint32_t pair = tile / g.k_tiles, k = tile % g.k_tiles * kDepth;
-    const uint8_t* a = reinterpret_cast<const uint8_t*>(g.a.p + (g.a_planes >> 4 * pair & 15) * g.a.plane + s.m0 * g.a.stride + k);
-    const uint8_t* b = reinterpret_cast<const uint8_t*>(g.b.p + (g.b_planes >> 4 * pair & 15) * g.b.plane + s.n0 * g.b.stride + k);
-    uint8_t* to = lds + stage * S::kStage + wave * kWave * 16;
-    auto go = [&](const uint8_t* p, uint8_t* l) {
-      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)p, (__attribute__((address_space(3))) void*)l, 16,
-                                       0, 0);
-    };
-#pragma unroll
-    for (uint32_t j = 0; j < kLoadsA; ++j) go(a + off_a[j], to + j * S::kThreads * 16);
-#pragma unroll
-    for (uint32_t j = 0; j < kLoadsB; ++j) go(b + off_b[j], to + S::TM * kDepth * 2 + j * S::kThreads * 16);
+    uint8_t* l = lds + (tile - from & 1) * S::kStage + wave * kWave * 16;
+    ta.fetch(g.a, g.a_planes >> 4 * pair & 15, s.m0, k, l);
+    tb.fetch(g.b, g.b_planes >> 4 * pair & 15, s.n0, k, l + S::TM * kDepth * 2);
   };
   Four acc[S::MT][S::NT];
 #pragma unroll
   for (uint32_t i = 0; i < S::MT; ++i)
 #pragma unroll
     for (uint32_t j = 0; j < S::NT; ++j) acc[i][j] = Four{0.0f, 0.0f, 0.0f, 0.0f};
-  const uint32_t row = lane & 15, order = row >> 1;
-  const uint32_t at_a = (s.wm * S::MT * 16 + row) * 128, at_b = S::TM * kDepth * 2 + (s.wn * S::NT * 16 + row) * 128;
-  if (from < to) fetch(from, 0);
-  for (uint32_t tile = from; tile < to; ++tile) {
-    const uint32_t stage = (tile - from) & 1;
-    __syncthreads();   // this tile has arrived, and the other stage's readers are done
-    if (tile + 1 < to) fetch(tile + 1, stage ^ 1);
-    const uint8_t* l = lds + stage * S::kStage;
+  Quad a[2][S::MT], b[2][S::NT];
+  auto read = [&](uint32_t tile, uint32_t k) {
+    const uint8_t* l = lds + (tile - from & 1) * S::kStage;
 #pragma unroll
-    for (uint32_t k = 0; k < 2; ++k) {
-      const uint32_t at = ((k * 4 + (lane >> 4)) ^ order) * 16;
-      Quad a[S::MT], b[S::NT];
+    for (uint32_t j = 0; j < S::NT; ++j) b[k][j] = TileB::read(l + S::TM * kDepth * 2, s.wn * S::NT * 16, j, k);
 #pragma unroll
-      for (uint32_t i = 0; i < S::MT; ++i) a[i] = *reinterpret_cast<const Quad*>(l + at_a + at + i * 16 * 128);
+    for (uint32_t i = 0; i < S::MT; ++i) a[k][i] = TileA::read(l, s.wm * S::MT * 16, i, k);
+  };
+  auto multiply = [&](uint32_t k) {
 #pragma unroll
-      for (uint32_t j = 0; j < S::NT; ++j) b[j] = *reinterpret_cast<const Quad*>(l + at_b + at + j * 16 * 128);
+    for (uint32_t i = 0; i < S::MT; ++i)
 #pragma unroll
-      for (uint32_t i = 0; i < S::MT; ++i)
-#pragma unroll
-        for (uint32_t j = 0; j < S::NT; ++j) acc[i][j] = mfma<H>(a[i], b[j], acc[i][j]);
+      for (uint32_t j = 0; j < S::NT; ++j) acc[i][j] = mfma<H>(a[k][i], b[k][j], acc[i][j]);
+  };
+  // Two stages.  What a half of a tile is multiplied from is read while the half before is multiplied; a stage is fetched into
+  // as soon as its second half is in registers, half a tile ahead of the barrier at which it has to be there.
+  if (from < to) {
+    fetch(from);
+    __syncthreads();
+    if (from + 1 < to) fetch(from + 1);
+    read(from, 0);
+    for (uint32_t tile = from; tile < to; ++tile) {
+      read(tile, 1);
+      multiply(0);
+      __syncthreads();   // the next tile has arrived, and all have read this one
+      if (tile + 2 < to) fetch(tile + 2);
+      if (tile + 1 < to) read(tile + 1, 0);
+      multiply(1);
     }
   }
   __syncthreads();
@@ -261,41 +369,56 @@ __global__ __launch_bounds__(S::kThreads) void product_kernel(Product g, E epilo
 }
 
 // ------------------------------------------------------------------------------ what becomes of it
+// exp(x) for x <= 0 of a difference: the difference's rounding is small where the exponential is large.
+__device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * 0x1.715476p+0f); }
+
 // Rows are the vocabulary's, columns are tokens.  Every tile's largest logit and sum of exponentials per token.
 struct StatsEnd {
   Rows who;
   uint32_t first, tile;     // the piece's first token of the vocabulary, and its first tile's number
   float scale;
+  const Factors* factors;   // null: matrices are multiplied as they are
   float2* partial;          // [tile][token]
   float* answer;            // the logit of every token's label
 
   template <class S>
   __device__ __forceinline__ void operator()(const Four (&acc)[S::MT][S::NT], const Spot& s, uint8_t* lds) const {
+    if (s.m0 + S::TM <= who.vocab - first)
+      tile_of<S, true>(acc, s, lds);
+    else
+      tile_of<S, false>(acc, s, lds);
+  }
+  template <class S, bool WHOLE>
+  __device__ __forceinline__ void tile_of(const Four (&acc)[S::MT][S::NT], const Spot& s, uint8_t* lds) const {
     float2* shared = reinterpret_cast<float2*>(lds);
     const uint32_t rest = who.vocab - first;   // rows that are there, counted from the piece's
+    const float f = factors ? scale * (factors->down[0] * factors->down[1]) : scale;
 #pragma unroll
     for (uint32_t j = 0; j < S::NT; ++j) {
       const uint32_t token = s.n + j * 16;
-      const int64_t label = token < who.n ? who.label(token) - first : -1;
-      float top = -INFINITY, sum = 0.0f;
+      const int64_t label = token < who.n ? who.label(token) - first - s.m : -1;
+      float top = -INFINITY, sum = 0.0f, z[S::MT][4];
 #pragma unroll
       for (uint32_t i = 0; i < S::MT; ++i)
 #pragma unroll
         for (uint32_t r = 0; r < 4; ++r) {
-          const uint32_t v = s.m + i * 16 + r;
-          if (v < rest) {
-            const float z = acc[i][j][r] * scale;
-            top = fmaxf(top, z);
-            if ((int64_t)v == label) answer[token] = z;
-          }
+          z[i][r] = acc[i][j][r] * f;
+          if (WHOLE || s.m + i * 4 + r < rest) top = fmaxf(top, z[i][r]);
         }
+      if (label >= 0 && label < 4 * (int64_t)S::MT && (WHOLE || s.m + label < rest)) {
+#pragma unroll
+        for (uint32_t i = 0; i < S::MT; ++i)
+#pragma unroll
+          for (uint32_t r = 0; r < 4; ++r)
+            if (i * 4 + r == (uint32_t)label) answer[token] = z[i][r];
+      }
       top = fmaxf(top, __shfl_xor(top, 16, 64));
       top = fmaxf(top, __shfl_xor(top, 32, 64));
 #pragma unroll
       for (uint32_t i = 0; i < S::MT; ++i)
 #pragma unroll
         for (uint32_t r = 0; r < 4; ++r)
-          if (s.m + i * 16 + r < rest) sum += __expf(acc[i][j][r] * scale - top);
+          if (WHOLE || s.m + i * 4 + r < rest) sum += exp_of(z[i][r] - top);
       sum += __shfl_xor(sum, 16, 64);
       sum += __shfl_xor(sum, 32, 64);
       if (lane_id() < 16) shared[s.wm * S::TN + token - s.n0] = float2{top, sum};
@@ -309,8 +432,7 @@ struct StatsEnd {
 #pragma unroll
       for (uint32_t w = 0; w < S::WM; ++w) {
         const float2 p = shared[w * S::TN + t];
-        if (p.x > -INFINITY) sum += p.y * __expf(p.x - top);      // else nothing was there
-        else sum += p.y;
+        sum += p.x > -INFINITY ? p.y * exp_of(p.x - top) : p.y;      // else nothing was there
       }
       partial[(uint64_t)(tile + s.tile_m) * who.n + s.n0 + t] = float2{top, sum};
     }
@@ -341,53 +463,51 @@ __global__ __launch_bounds__(kJoinTokens * kJoinRows) void loss_kernel(Rows who,
   if (stats) stats[token] = live ? all : float2{0.0f, 0.0f};
 }
 
-// G in PY planes with the vocabulary contiguous, for dh, and in PT with the tokens contiguous, for dT.
-template <class H, uint32_t PY, uint32_t PT>
+// G in P planes, the vocabulary along the rows.  Rows and columns up to whole tiles of K are zeros.
+template <class H, uint32_t P>
 struct GradEnd {
   Rows who;
   uint32_t first;
   float scale;
   const float2* stats;
-  const float* factors;
-  Half *g, *turned;
-  uint64_t g_stride, g_plane, turned_stride, turned_plane;
+  const Factors* factors;
+  uint32_t scaled;          // whether the operands were
+  Half* g;
+  float* rests;             // what is left of the label's entry, for dh
+  uint64_t stride, plane, tokens;
 
   template <class S>
   __device__ __forceinline__ void operator()(const Four (&acc)[S::MT][S::NT], const Spot& s, uint8_t*) const {
     const uint32_t rest = who.vocab - first;
+    const float f = scaled ? scale * (factors->down[0] * factors->down[1]) : scale;
 #pragma unroll
     for (uint32_t j = 0; j < S::NT; ++j) {
       const uint32_t token = s.n + j * 16;
       const bool live = token < who.n && who.live(token);
       const float2 st = live ? stats[token] : float2{0.0f, 1.0f};
-      const float over = 1.0f / st.y, w = live ? who.weight(token) * scale * factors[0] : 0.0f;
-      const int64_t label = live ? who.label(token) - first : -1;
+      const float w = live ? who.weight(token) * scale * factors->grad : 0.0f, over = w / st.y;
+      const int64_t label = live ? who.label(token) - first - s.m : -1;
+      const bool here = label >= 0 && label < 4 * (int64_t)S::MT;
+      const uint32_t there = live && s.m < rest ? rest - s.m : 0u;      // of the lane's rows
+      if (token >= tokens) continue;
 #pragma unroll
-      for (uint32_t i = 0; i < S::MT; ++i) {
-        Half y[PY][4], t[PT][4];
+      for (uint32_t i = 0; i < S::MT; i += 2) {
+        Half out[8][P];
 #pragma unroll
-        for (uint32_t r = 0; r < 4; ++r) {
-          const uint32_t v = s.m + i * 16 + r;
-          float x = __expf(acc[i][j][r] * scale - st.x) * over;
-          if ((int64_t)v == label) x -= 1.0f;
-          x = live && v < rest ? x * w : 0.0f;
-          Half part[PY > PT ? PY : PT];
-          split<H, (PY > PT ? PY : PT)>(x, part);
-#pragma unroll
-          for (uint32_t p = 0; p < PY; ++p) y[p][r] = part[p];
-#pragma unroll
-          for (uint32_t p = 0; p < PT; ++p) t[p][r] = part[p];
+        for (uint32_t r = 0; r < 8; ++r) {
+          float x = exp_of(acc[i + r / 4][j][r % 4] * f - st.x) * over;
+          if (here && i * 4 + r == (uint32_t)label) x -= w;
+          x = i * 4 + r < there ? x : 0.0f;
+          split<H, P>(x, out[r]);
+          if (here && i * 4 + r == (uint32_t)label) rests[token] = x - (float)__builtin_bit_cast(H, out[r][0]);
         }
-        const uint64_t v = s.m + i * 16;
-        if (token < who.n)
 #pragma unroll
-          for (uint32_t p = 0; p < PY; ++p)
-            *reinterpret_cast<Pair*>(g + p * g_plane + token * g_stride + v) = Pair{y[p][0] | (uint32_t)y[p][1] << 16, y[p][2] | (uint32_t)y[p][3] << 16};
-        if (token < turned_stride)
+        for (uint32_t p = 0; p < P; ++p) {
+          Quad q;
 #pragma unroll
-          for (uint32_t p = 0; p < PT; ++p)
-#pragma unroll
-            for (uint32_t r = 0; r < 4; ++r) turned[p * turned_plane + (v + r) * turned_stride + token] = t[p][r];
+          for (uint32_t r = 0; r < 4; ++r) q[r] = out[2 * r][p] | (uint32_t)out[2 * r + 1][p] << 16;
+          *reinterpret_cast<Quad*>(g + p * plane + token * stride + s.m + i * 4) = q;
+        }
       }
     }
   }
@@ -422,11 +542,12 @@ struct TableEnd {
   TO* out;
   uint64_t stride;
   uint32_t dim, count, add;   // count: the piece's
-  const float* factors;
+  const Factors* factors;
+  uint32_t scaled;
 
   template <class S>
   __device__ __forceinline__ void operator()(const Four (&acc)[S::MT][S::NT], const Spot& s, uint8_t*) const {
-    const float f = factors[1];
+    const float f = scaled ? factors->back * factors->down[0] : factors->back;
 #pragma unroll
     for (uint32_t j = 0; j < S::NT; ++j) {
       const uint32_t v = s.n + j * 16;
@@ -455,22 +576,30 @@ struct TableEnd {
   }
 };
 
-// dh: the slices added up.
+// dh: the slices added up, and what the rounding of the label's entry of G, its largest, has left.
 template <class T>
 __global__ __launch_bounds__(256) void hidden_kernel(Rows who, uint32_t dim, const float* sums, uint64_t stride, uint32_t slices,
-                                                     const float* factors, T* out, uint64_t out_stride) {
+                                                     const Factors* factors, uint32_t scaled, const float* rests, Matrix table, T* out,
+                                                     uint64_t out_stride) {
   const uint32_t blocks = (dim + 1023) / 1024;
   const uint32_t c = blockIdx.x % blocks * 1024 + threadIdx.x * 4;
   if (c >= dim) return;
-  const float f = factors[1];
+  const float f = scaled ? factors->back * factors->down[1] : factors->back;
   for (uint32_t i = blockIdx.x / blocks; i < who.n; i += gridDim.x / blocks) {
     float x[4] = {};
-    if (who.live(i))
+    if (who.live(i)) {
       for (uint32_t k = 0; k < slices; ++k) {
         const Four p = *reinterpret_cast<const Four*>(sums + ((uint64_t)k * who.n + i) * stride + c);
 #pragma unroll
         for (uint32_t r = 0; r < 4; ++r) x[r] += p[r];
       }
+      if (rests) {
+        float t[4];
+        load_row<4>(static_cast<const T*>(table.p) + (uint64_t)who.label(i) * table.stride, c, dim, 0.0f, t);
+#pragma unroll
+        for (uint32_t r = 0; r < 4; ++r) x[r] = fmaf(rests[i], t[r], x[r]);
+      }
+    }
 #pragma unroll
     for (uint32_t r = 0; r < 4; ++r) x[r] *= f;
     store_row<4>(out + i * out_stride, c, dim, x);
@@ -490,8 +619,8 @@ using Thin = Shape<4, 1, 4, 2>;    // 256 x 32: few tokens
 
 template <class T>
 struct Kind {                      // how matrices of a type are multiplied
-  using H = std::conditional_t<std::is_same_v<T, f16_t>, f16_t, bf16_t>;
-  static constexpr uint32_t P = sizeof(T) == 4 ? 3 : 1;
+  using H = std::conditional_t<std::is_same_v<T, bf16_t>, bf16_t, f16_t>;
+  static constexpr uint32_t P = sizeof(T) == 4 ? 2 : 1;
 };
 // The pairs of planes of (pa, pb) that count, the smallest products first.
 void set_pairs(Product& g, uint32_t pa, uint32_t pb) {
@@ -510,36 +639,46 @@ template <class S>
 uint64_t tiles_of(const Product& g) {
   return (uint64_t)((g.m + S::TM - 1) / S::TM) * ((g.n + S::TN - 1) / S::TN);
 }
-template <class H, class S, class E>
-void run_as(const Product& g, const E& end, hipStream_t stream) {
-  hipLaunchKernelGGL((product_kernel<H, S, E>), dim3((uint32_t)(tiles_of<S>(g) * g.slices)), dim3(S::kThreads), 0, stream, g, end);
-}
 constexpr uint32_t kCus = 256;
-bool large_goes(const Product& g) { return tiles_of<Large>(g) * g.slices >= kCus * 3 / 4; }
+// Large tiles take four times as long as small ones would each, but half of that a value, one to a CU where two small ones are.
+bool large_goes(const Product& g) {
+  const uint64_t large = (tiles_of<Large>(g) * g.slices + kCus - 1) / kCus * 4, small = (tiles_of<Small>(g) * g.slices + 2 * kCus - 1) / (2 * kCus) * 2;
+  return large * 3 <= small * 4;
+}
+template <class H, bool TALL_A, bool TALL_B, class S, class E>
+void run_as(const Product& g, const E& end, hipStream_t stream) {
+  hipLaunchKernelGGL((product_kernel<H, S, TALL_A, TALL_B, E>), dim3((uint32_t)(tiles_of<S>(g) * g.slices)), dim3(S::kThreads), 0, stream, g, end);
+}
+template <class H, bool TALL_A, bool TALL_B, class E>
+void run(const Product& g, const E& end, hipStream_t stream) {
+  if (large_goes(g))
+    run_as<H, TALL_A, TALL_B, Large>(g, end, stream);
+  else
+    run_as<H, TALL_A, TALL_B, Small>(g, end, stream);
+}
 
 struct Sizes {
   uint64_t depth, tokens, piece;      // dim and n in whole tiles of K; tokens of the vocabulary at a time
-  uint32_t planes, py, pt, slices;
+  uint32_t planes, g_planes, slices;
 };
 constexpr uint64_t kBudget = 256ull << 20;   // bytes of a piece's G and table
 Sizes sizes_for(uint32_t n, uint32_t vocab, uint32_t dim, uint32_t type, uint32_t dtable_type, bool grad) {
   Sizes z{};
   z.depth = pad_to(dim, kDepth);
   z.tokens = pad_to(n, kDepth);
-  z.planes = type == CVLC_F32 ? 3 : 1;
-  z.py = type == CVLC_F32 ? 3 : 1;
-  z.pt = type == CVLC_F32 ? 3 : dtable_type == CVLC_F32 ? 2 : 1;
-  const uint64_t each = z.depth * z.planes * 2 * (grad ? 2 : 1) + (grad ? z.tokens * 2 * (z.py + z.pt) : 0);
+  z.planes = type == CVLC_F32 ? 2 : 1;
+  z.g_planes = dtable_type == CVLC_F32 ? 2 : 1;
+  const uint64_t each = z.depth * z.planes * 2 + (grad ? z.tokens * z.g_planes * 2 : 0);
   z.piece = std::min(pad_to(vocab, kPadTo), std::max<uint64_t>(kPadTo, kBudget / each / kPadTo * kPadTo));
   // dh has few tiles where tokens and columns are few: K, a piece of the vocabulary, is cut then
-  const uint64_t tiles = ((z.depth + 127) / 128) * ((z.tokens + 127) / 128);
+  const uint64_t tiles = ((z.depth + 255) / 256) * ((z.tokens + 255) / 256);
   z.slices = (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>(kCus / std::max<uint64_t>(tiles, 1), z.piece / 512));
   return z;
 }
 
 struct Room {                          // parts of a workspace
   uint8_t* base;
-  uint64_t used = 256;                 // the factors lie first
+  uint64_t used;
   template <class P>
   P* take(uint64_t count) {
     P* p = reinterpret_cast<P*>(base + used);
@@ -554,6 +693,10 @@ struct Call {
   uint64_t hidden_stride, table_stride;
   Rows who;
   float scale;
+  Matrix hidden_matrix() const { return Matrix{hidden, hidden_stride, n}; }
+  Matrix table_matrix(uint64_t first, uint32_t count) const {
+    return Matrix{static_cast<const uint8_t*>(table) + first * table_stride * type_bytes(type), table_stride, count};
+  }
 };
 
 // Whether a matrix can be multiplied as it is: rows that begin at 16 bytes and end with a tile of K, near enough to each other
@@ -562,144 +705,156 @@ bool as_it_is(const void* p, uint64_t stride, uint32_t dim, uint32_t type) {
   return type != CVLC_F32 && dim % kDepth == 0 && stride % 8 == 0 && stride < (1u << 22) && reinterpret_cast<uintptr_t>(p) % 16 == 0;
 }
 
-template <class T>
-void pack(const T* src, const PackArgs& a, hipStream_t stream) {
-  const uint64_t grid = ((a.rows + kPackSide - 1) / kPackSide) * (uint64_t)((a.cols + kPackSide - 1) / kPackSide);
-  hipLaunchKernelGGL((pack_kernel<T, typename Kind<T>::H, Kind<T>::P>), dim3((uint32_t)grid), dim3(kPackBlock), 0, stream, a, src);
-}
-
-// The workspace of the loss; with base = null only its size.
-struct LossRoom {
-  uint64_t tiles;
+// The parts of a workspace; with base = null only its size.
+struct Parts {
+  Factors* factors;
+  float* tops;
+  Half *hidden, *table;
+  explicit Parts(Room& r, const Sizes& z) {
+    factors = r.take<Factors>(1);
+    tops = r.take<float>(z.planes > 1 ? 2 * kSurveyGrid : 0);
+    hidden = r.take<Half>(z.planes * z.tokens * z.depth);
+    table = r.take<Half>(z.planes * z.piece * z.depth);
+  }
+};
+struct LossParts : Parts {
   float2* partial;
   float* answer;
-  Half *hidden, *table;
   uint64_t bytes;
-  LossRoom(uint8_t* base, const Sizes& z, uint32_t n, uint32_t vocab) {
-    Room r{base};
-    tiles = vocab / 128 + vocab / z.piece + 2;
-    partial = r.take<float2>(tiles * n);
+  LossParts(Room r, const Sizes& z, uint32_t n, uint32_t vocab) : Parts(r, z) {
+    partial = r.take<float2>((vocab / 128 + vocab / z.piece + 2) * n);
     answer = r.take<float>(n);
-    hidden = r.take<Half>(z.planes * n * z.depth);
-    table = r.take<Half>(z.planes * z.piece * z.depth);
     bytes = r.used;
   }
 };
-struct GradRoom {
-  Half *hidden, *hidden_turned, *table, *table_turned, *g, *g_turned;
-  float* sums;
+struct GradParts : Parts {
+  Half* g;
+  float *sums, *rests;
   uint64_t bytes;
-  GradRoom(uint8_t* base, const Sizes& z, uint32_t n, uint32_t dim) {
-    Room r{base};
-    hidden = r.take<Half>(z.planes * n * z.depth);
-    hidden_turned = r.take<Half>(z.planes * dim * z.tokens);
-    table = r.take<Half>(z.planes * z.piece * z.depth);
-    table_turned = r.take<Half>(z.planes * dim * z.piece);
-    g = r.take<Half>(z.py * n * z.piece);
-    g_turned = r.take<Half>(z.pt * z.piece * z.tokens);
+  GradParts(Room r, const Sizes& z, uint32_t n) : Parts(r, z) {
+    g = r.take<Half>(z.g_planes * z.tokens * z.piece);
     sums = r.take<float>(z.slices * n * z.depth);
+    rests = r.take<float>(n);
     bytes = r.used;
   }
 };
 
+// The factors that a call goes by.
+void find_factors(const Call& c, const Sizes& z, const Parts& parts, uint32_t* status, hipStream_t stream) {
+  const Matrix hidden = c.hidden_matrix(), table = c.table_matrix(0, c.vocab), none{};
+  if (z.planes == 1) {
+    hipLaunchKernelGGL(factors_kernel, dim3(1), dim3(1024), 0, stream, c.who, c.scale, nullptr, 0, none, none, c.dim, parts.factors, status);
+  } else if ((uint64_t)(c.n + (uint64_t)c.vocab) * c.dim <= kSurveyAlone) {
+    hipLaunchKernelGGL(factors_kernel, dim3(1), dim3(1024), 0, stream, c.who, c.scale, nullptr, 0, hidden, table, c.dim, parts.factors, status);
+  } else {
+    hipLaunchKernelGGL(survey_kernel, dim3(kSurveyGrid, 2), dim3(kSurveyBlock), 0, stream, hidden, table, c.dim, c.who, parts.tops);
+    hipLaunchKernelGGL(factors_kernel, dim3(1), dim3(1024), 0, stream, c.who, c.scale, parts.tops, kSurveyGrid, none, none, c.dim,
+                       parts.factors, status);
+  }
+}
+
 template <class T>
-void loss_of(const Call& c, const Sizes& z, const LossRoom& room, float* loss, float2* stats, uint32_t* status, hipStream_t stream) {
+void pack(const Call& c, const PackArgs& first, const PackArgs& second, hipStream_t stream) {
+  auto grid = [](const PackArgs& a) {
+    return (uint32_t)std::min<uint64_t>(((uint64_t)a.rows_to * (a.stride / 8) + kPackBlock - 1) / kPackBlock, 1u << 16);
+  };
+  const uint32_t one = grid(first), two = grid(second);
+  if (one + two)
+    hipLaunchKernelGGL((pack_kernel<T, typename Kind<T>::H, Kind<T>::P>), dim3(one + two), dim3(kPackBlock), 0, stream, first, second, one, c.who);
+}
+
+template <class T>
+void loss_of(const Call& c, const Sizes& z, const LossParts& parts, float* loss, float2* stats, uint32_t* status, hipStream_t stream) {
   using H = typename Kind<T>::H;
-  const T *hidden = static_cast<const T*>(c.hidden), *table = static_cast<const T*>(c.table);
+  constexpr uint32_t P = Kind<T>::P;
   const bool hidden_goes = as_it_is(c.hidden, c.hidden_stride, c.dim, c.type), table_goes = as_it_is(c.table, c.table_stride, c.dim, c.type);
-  if (!hidden_goes)
-    pack<T>(hidden, PackArgs{c.n, c.dim, c.hidden_stride, room.hidden, nullptr, z.depth, c.n * z.depth, 0, 0, 0, c.who}, stream);
+  if (P > 1) find_factors(c, z, parts, nullptr, stream);
+  PackArgs hidden{c.hidden_matrix(), c.dim, c.n, parts.hidden, z.depth, z.tokens * z.depth, parts.factors->up, 0};
+  if (hidden_goes) hidden.rows_to = 0;
   Product g{};
-  g.b = hidden_goes ? Operand{static_cast<const Half*>(c.hidden), c.hidden_stride, 0} : Operand{room.hidden, z.depth, c.n * z.depth};
+  g.b = hidden_goes ? Operand{static_cast<const Half*>(c.hidden), c.hidden_stride, 0, 0, c.n} : Operand{parts.hidden, z.depth, z.tokens * z.depth, 0, c.n};
   g.n = c.n;
   g.k_tiles = (uint32_t)(z.depth / kDepth);
   g.slices = 1;
-  set_pairs(g, z.planes, z.planes);
+  set_pairs(g, P, P);
   uint32_t tile = 0;
   const uint64_t step = table_goes ? pad_to(c.vocab, kPadTo) : z.piece;
   for (uint64_t first = 0; first < c.vocab; first += step) {
     g.m = (uint32_t)std::min<uint64_t>(step, c.vocab - first);
-    if (table_goes) {
-      g.a = Operand{static_cast<const Half*>(c.table) + first * c.table_stride, c.table_stride, 0};
-    } else {
-      pack<T>(table + first * c.table_stride, PackArgs{g.m, c.dim, c.table_stride, room.table, nullptr, z.depth, z.piece * z.depth, 0, 0, 0, c.who}, stream);
-      g.a = Operand{room.table, z.depth, z.piece * z.depth};
-    }
-    const StatsEnd end{c.who, (uint32_t)first, tile, c.scale, room.partial, room.answer};
-    if (c.n <= Thin::TN) {
-      run_as<H, Thin>(g, end, stream);
-      tile += (g.m + Thin::TM - 1) / Thin::TM;
-    } else if (large_goes(g)) {
-      run_as<H, Large>(g, end, stream);
-      tile += (g.m + Large::TM - 1) / Large::TM;
-    } else {
-      run_as<H, Small>(g, end, stream);
-      tile += (g.m + Small::TM - 1) / Small::TM;
-    }
+    PackArgs table{c.table_matrix(first, g.m), c.dim, table_goes ? 0 : g.m, parts.table, z.depth, z.piece * z.depth, parts.factors->up + 1, 0};
+    pack<T>(c, hidden, table, stream);
+    hidden.rows_to = 0;
+    g.a = table_goes ? Operand{static_cast<const Half*>(c.table) + first * c.table_stride, c.table_stride, 0, 0, g.m}
+                     : Operand{parts.table, z.depth, z.piece * z.depth, 0, g.m};
+    const StatsEnd end{c.who, (uint32_t)first, tile, c.scale, P > 1 ? parts.factors : nullptr, parts.partial, parts.answer};
+    auto go = [&](auto shape) {
+      using S = decltype(shape);
+      run_as<H, false, false, S>(g, end, stream);
+      tile += (g.m + S::TM - 1) / S::TM;
+    };
+    if (c.n <= Thin::TN)
+      go(Thin{});
+    else if (large_goes(g))
+      go(Large{});
+    else
+      go(Small{});
   }
   hipLaunchKernelGGL(loss_kernel, dim3((c.n + kJoinTokens - 1) / kJoinTokens), dim3(kJoinTokens * kJoinRows), 0, stream, c.who, tile,
-                     room.partial, room.answer, loss, stats, status);
+                     parts.partial, parts.answer, loss, stats, status);
 }
 
 template <class T, class TO>
-void grad_of(const Call& c, const Sizes& z, const GradRoom& room, float* factors, const float2* stats, T* dhidden, uint64_t dhidden_stride,
-             TO* dtable, uint64_t dtable_stride, bool accumulate, uint32_t* status, hipStream_t stream) {
+void grad_of(const Call& c, const Sizes& z, const GradParts& parts, const float2* stats, T* dhidden, uint64_t dhidden_stride, TO* dtable,
+             uint64_t dtable_stride, bool accumulate, uint32_t* status, hipStream_t stream) {
   using H = typename Kind<T>::H;
-  constexpr uint32_t P = Kind<T>::P, PY = P, PT = P == 3 ? 3 : sizeof(TO) == 4 ? 2 : 1;
-  const T *hidden = static_cast<const T*>(c.hidden), *table = static_cast<const T*>(c.table);
-  const bool hidden_goes = as_it_is(c.hidden, c.hidden_stride, c.dim, c.type), table_goes = as_it_is(c.table, c.table_stride, c.dim, c.type);
-  hipLaunchKernelGGL(factors_kernel, dim3(1), dim3(1024), 0, stream, c.who, c.scale, factors, status);
-  // rows that do not count may hold anything, and G's zeros do not take a NaN away
-  pack<T>(hidden, PackArgs{c.n, c.dim, c.hidden_stride, hidden_goes ? nullptr : room.hidden, dtable ? room.hidden_turned : nullptr, z.depth,
-                           c.n * z.depth, z.tokens, c.dim * z.tokens, 1, c.who}, stream);
-  auto go = [&](const Product& g, const auto& end) {
-    if (large_goes(g))
-      run_as<H, Large>(g, end, stream);
-    else
-      run_as<H, Small>(g, end, stream);
-  };
+  constexpr uint32_t P = Kind<T>::P, PG = sizeof(TO) == 4 ? 2 : 1;
+  const bool table_goes = as_it_is(c.table, c.table_stride, c.dim, c.type);
+  find_factors(c, z, parts, status, stream);
+  PackArgs hidden{c.hidden_matrix(), c.dim, (uint32_t)z.tokens, parts.hidden, z.depth, z.tokens * z.depth, parts.factors->up, 1};
   for (uint64_t first = 0; first < c.vocab; first += z.piece) {
     const uint32_t count = (uint32_t)std::min<uint64_t>(z.piece, c.vocab - first);
-    if (!table_goes || dhidden)
-      pack<T>(table + first * c.table_stride, PackArgs{count, c.dim, c.table_stride, table_goes ? nullptr : room.table, dhidden ? room.table_turned : nullptr,
-                                                       z.depth, z.piece * z.depth, z.piece, c.dim * z.piece, 0, c.who}, stream);
+    PackArgs table{c.table_matrix(first, count), c.dim, table_goes ? 0 : count, parts.table, z.depth, z.piece * z.depth, parts.factors->up + 1, 0};
+    pack<T>(c, hidden, table, stream);
+    hidden.rows_to = 0;
     Product g{};
     g.slices = 1;
-    g.a = table_goes ? Operand{static_cast<const Half*>(c.table) + first * c.table_stride, c.table_stride, 0} : Operand{room.table, z.depth, z.piece * z.depth};
-    g.b = hidden_goes ? Operand{static_cast<const Half*>(c.hidden), c.hidden_stride, 0} : Operand{room.hidden, z.depth, c.n * z.depth};
+    g.a = table_goes ? Operand{static_cast<const Half*>(c.table) + first * c.table_stride, c.table_stride, 0, c.dim, count}
+                     : Operand{parts.table, z.depth, z.piece * z.depth, (uint32_t)z.depth, count};
+    g.b = Operand{parts.hidden, z.depth, z.tokens * z.depth, (uint32_t)z.depth, (uint32_t)z.tokens};
     g.m = count;
     g.n = c.n;
     g.k_tiles = (uint32_t)(z.depth / kDepth);
     set_pairs(g, P, P);
-    go(g, GradEnd<H, PY, PT>{c.who, (uint32_t)first, c.scale, stats, factors, room.g, room.g_turned, z.piece, c.n * z.piece, z.tokens,
-                             z.piece * z.tokens});
+    const Operand of_g{parts.g, z.piece, z.tokens * z.piece, (uint32_t)z.piece, (uint32_t)z.tokens};
+    run<H, false, false>(g, GradEnd<H, PG>{c.who, (uint32_t)first, c.scale, stats, parts.factors, P > 1, parts.g, parts.rests, z.piece,
+                                           z.tokens * z.piece, z.tokens}, stream);
     if (dhidden) {
       Product y{};
-      y.a = Operand{room.table_turned, z.piece, c.dim * z.piece};
-      y.b = Operand{room.g, z.piece, c.n * z.piece};
+      y.a = g.a;
+      y.b = of_g;
       y.m = c.dim;
       y.n = c.n;
       y.k_tiles = (uint32_t)(pad_to(count, kDepth) / kDepth);
       y.slices = z.slices;
-      set_pairs(y, P, PY);
-      go(y, HiddenEnd{room.sums, z.depth, c.n, first > 0});
+      set_pairs(y, P, P);   // 16-bit results: G's first plane alone
+      run<H, true, false>(y, HiddenEnd{parts.sums, z.depth, c.n, first > 0}, stream);
     }
     if (dtable) {
       Product t{};
-      t.a = Operand{room.hidden_turned, z.tokens, c.dim * z.tokens};
-      t.b = Operand{room.g_turned, z.tokens, z.piece * z.tokens};
+      t.a = g.b;
+      t.b = of_g;
       t.m = c.dim;
       t.n = count;
       t.k_tiles = (uint32_t)(z.tokens / kDepth);
       t.slices = 1;
-      set_pairs(t, P, PT);
-      go(t, TableEnd<TO>{dtable + first * dtable_stride, dtable_stride, c.dim, count, accumulate, factors});
+      set_pairs(t, P, PG);
+      run<H, true, true>(t, TableEnd<TO>{dtable + first * dtable_stride, dtable_stride, c.dim, count, accumulate, parts.factors, P > 1}, stream);
     }
   }
   if (dhidden) {
     const uint32_t blocks = (c.dim + 1023) / 1024;
-    hipLaunchKernelGGL(hidden_kernel<T>, dim3(std::min(c.n, std::max(1u, 8192u / blocks)) * blocks), dim3(256), 0, stream, c.who, c.dim, room.sums,
-                       z.depth, z.slices, factors, dhidden, dhidden_stride);
+    hipLaunchKernelGGL(hidden_kernel<T>, dim3(std::min(c.n, std::max(1u, 8192u / blocks)) * blocks), dim3(256), 0, stream, c.who, c.dim, parts.sums,
+                       z.depth, z.slices, parts.factors, P > 1, P == 1 ? parts.rests : nullptr, c.table_matrix(0, c.vocab), dhidden, dhidden_stride);
   }
 }
 
@@ -731,7 +886,7 @@ extern "C" {
 size_t cvlc_linear_xent_workspace_bytes(uint32_t n, uint32_t vocab, uint32_t dim, uint32_t type) {
   using namespace cvlc;
   if (!n || !vocab || !dim) return 256;
-  return (size_t)LossRoom(nullptr, sizes_for(n, vocab, dim, type, type, false), n, vocab).bytes;
+  return (size_t)LossParts(Room{}, sizes_for(n, vocab, dim, type, type, false), n, vocab).bytes;
 }
 
 int cvlc_linear_xent(uint32_t n, uint32_t vocab, uint32_t dim, const void* d_hidden, uint64_t hidden_stride, const void* d_table,
@@ -745,7 +900,7 @@ int cvlc_linear_xent(uint32_t n, uint32_t vocab, uint32_t dim, const void* d_hid
   if (ws_bytes < cvlc_linear_xent_workspace_bytes(n, vocab, dim, type)) return CVLC_ERR_CAPACITY;
   if (n == 0) return CVLC_OK;
   const Sizes z = sizes_for(n, vocab, dim, type, type, false);
-  const LossRoom room(static_cast<uint8_t*>(d_workspace), z, n, vocab);
+  const LossParts room(Room{static_cast<uint8_t*>(d_workspace), 0}, z, n, vocab);
   by_type(type, [&](auto t) {
     loss_of<decltype(t)>(c, z, room, d_loss, reinterpret_cast<float2*>(d_stats), d_status, static_cast<hipStream_t>(hip_stream));
   });
@@ -755,7 +910,7 @@ int cvlc_linear_xent(uint32_t n, uint32_t vocab, uint32_t dim, const void* d_hid
 size_t cvlc_linear_xent_grad_workspace_bytes(uint32_t n, uint32_t vocab, uint32_t dim, uint32_t type, uint32_t dtable_type) {
   using namespace cvlc;
   if (!n || !vocab || !dim) return 256;
-  return (size_t)GradRoom(nullptr, sizes_for(n, vocab, dim, type, dtable_type, true), n, dim).bytes;
+  return (size_t)GradParts(Room{}, sizes_for(n, vocab, dim, type, dtable_type, true), n).bytes;
 }
 
 int cvlc_linear_xent_grad(uint32_t n, uint32_t vocab, uint32_t dim, const void* d_hidden, uint64_t hidden_stride, const void* d_table,
@@ -784,13 +939,12 @@ int cvlc_linear_xent_grad(uint32_t n, uint32_t vocab, uint32_t dim, const void* 
     return hip_check(hipGetLastError());
   }
   const Sizes z = sizes_for(n, vocab, dim, type, out_type, true);
-  const GradRoom room(static_cast<uint8_t*>(d_workspace), z, n, dim);
-  float* factors = static_cast<float*>(d_workspace);
+  const GradParts room(Room{static_cast<uint8_t*>(d_workspace), 0}, z, n);
   by_type(type, [&](auto t) {
     using T = decltype(t);
     auto go = [&](auto to) {
       using TO = decltype(to);
-      grad_of<T, TO>(c, z, room, factors, reinterpret_cast<const float2*>(d_stats), static_cast<T*>(d_dhidden), dhidden_stride,
+      grad_of<T, TO>(c, z, room, reinterpret_cast<const float2*>(d_stats), static_cast<T*>(d_dhidden), dhidden_stride,
                      static_cast<TO*>(d_dtable), dtable_stride, accumulate, d_status, stream);
     };
     if (out_type == type)
