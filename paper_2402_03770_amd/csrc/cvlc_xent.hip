@@ -31,7 +31,7 @@ typedef __bf16 EightB __attribute__((ext_vector_type(8)));
 typedef _Float16 EightH __attribute__((ext_vector_type(8)));
 typedef uint16_t Half;  // 16 bits of either type
 
-constexpr uint32_t kDepth = 64;    // K of a tile: 128 bytes of a row
+constexpr uint32_t kDepth = 32;    // K of a tile: what one matrix instruction takes
 constexpr uint32_t kPadTo = 256;   // vocabulary pieces are whole tiles
 constexpr float kLift = 0x1p13f;   // G's largest entries
 
@@ -204,81 +204,94 @@ __device__ __forceinline__ Four mfma(Quad a, Quad b, Four c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(EightH, a), __builtin_bit_cast(EightH, b), c, 0, 0, 0);
 }
 
-constexpr uint32_t log2_of(uint32_t x) { return x < 2 ? 0 : 1 + log2_of(x / 2); }
-
-// A tile's shape: WM x WN wavefronts of MT x NT matrix instructions (16 x 16) each.
-template <uint32_t WM_, uint32_t WN_, uint32_t MT_, uint32_t NT_>
+// A tile's shape: WM x WN wavefronts of MT x NT matrix instructions (16 x 16) each; STAGES tiles of K are in LDS.
+template <uint32_t WM_, uint32_t WN_, uint32_t MT_, uint32_t NT_, uint32_t STAGES>
 struct Shape {
   static constexpr uint32_t WM = WM_, WN = WN_, MT = MT_, NT = NT_, TM = WM * MT * 16, TN = WN * NT * 16, kThreads = WM * WN * kWave;
-  static constexpr uint32_t kStage = (TM + TN) * kDepth * 2;   // bytes of both operands' tiles
+  static constexpr uint32_t kStages = STAGES, kStage = (TM + TN) * kDepth * 2;   // bytes of both operands' tiles
 };
+// Where a lane's rows are that belong to the i-th matrix instruction: eight neighbouring ones to two of them.
+constexpr __host__ __device__ uint32_t run_of(uint32_t i) { return i / 2 * 32 + i % 2 * 4; }
+
+// Eight reads of LDS that turn four rows of sixteen elements, FOUR bytes between the halves of a Quad.  One block of assembly with
+// its wait: the builtin's read is taken for one that needs all that is on its way into LDS, and waits for it.
+template <uint32_t FOUR>
+__device__ __forceinline__ void turned(uint32_t a, uint32_t b, uint32_t c, uint32_t d, Quad* out) {
+  Pair x[8];
+  asm volatile(
+      "ds_read_b64_tr_b16 %0, %8\n\tds_read_b64_tr_b16 %1, %8 offset:%12\n\tds_read_b64_tr_b16 %2, %9\n\tds_read_b64_tr_b16 %3, %9 offset:%12\n\t"
+      "ds_read_b64_tr_b16 %4, %10\n\tds_read_b64_tr_b16 %5, %10 offset:%12\n\tds_read_b64_tr_b16 %6, %11\n\tds_read_b64_tr_b16 %7, %11 offset:%12\n\t"
+      "s_waitcnt lgkmcnt(0)"
+      : "=&v"(x[0]), "=&v"(x[1]), "=&v"(x[2]), "=&v"(x[3]), "=&v"(x[4]), "=&v"(x[5]), "=&v"(x[6]), "=&v"(x[7])
+      : "v"(a), "v"(b), "v"(c), "v"(d), "n"(FOUR)
+      : "memory");
+#pragma unroll
+  for (uint32_t i = 0; i < 4; ++i) out[i] = Quad{x[2 * i][0], x[2 * i][1], x[2 * i + 1][0], x[2 * i + 1][1]};
+}
 
 // One operand's tile in LDS: how it is fetched and read.  Tiles go straight to LDS, 16 bytes a lane in the order of the
 // lanes; where in memory a lane reads decides what lies where, and it is so that the lanes that read LDS together find
 // different banks:
-//   wide: a row has eight accesses, and sixteen rows are read at one K.  Access x of row r lies at x ^ key(r), with
-//     key in bits 1 to 3 of r, or, where a lane's results are `RUN` neighbouring rows (the MFMA's row i of sixteen is row
-//     RUN (i / 4) + i % 4 of the wavefront's then), in bit 1 and the two bits from RUN on.
+//   wide: a row has four accesses, and sixteen rows are read at one K.  Access x of row r lies at x ^ key(r), with key in bits
+//     2 and 3 of r, or, where a lane's results are runs of neighbouring rows (the matrix instruction's row i of sixteen is row
+//     8 (i / 4) + i % 4 of the wavefront's then), in bits 3 and 4.
 //   tall: sixteen neighbouring elements of a row are read from four rows by sixteen lanes, which hand them round (the read
 //     turns them).  Such a block b of row k lies at b ^ (k % 4 + 4 (k / 8 % 2)).
-template <bool TALL, uint32_t ROWS, uint32_t THREADS, uint32_t RUN>
+template <bool TALL, uint32_t ROWS, uint32_t THREADS, bool RUNS>
 struct Tile {
-  static constexpr uint32_t kLoads = ROWS * 8 / THREADS;
-  static_assert(kLoads * THREADS == ROWS * 8, "whole loads");
-  uint32_t off[kLoads], placed;
+  static constexpr uint32_t kLoads = ROWS * 4 / THREADS;
+  static_assert(kLoads * THREADS == ROWS * 4, "whole loads");
+  static constexpr uint32_t kAcross = ROWS / 8;   // tall: accesses of a row
+  uint32_t off[kLoads];
 
-  static __device__ __forceinline__ uint32_t key(uint32_t r) {
-    return RUN ? (r >> 1 & 1) | (r >> log2_of(RUN) & 3) << 1 : r >> 1 & 7;
-  }
-  // Byte offsets from the tile's first row (and, tall, its first element) on, rows from `left` on being read as the one before.
-  __device__ __forceinline__ void place(const Operand& o, uint32_t first, uint32_t left) {
-    placed = left;
+  static __device__ __forceinline__ uint32_t key(uint32_t r) { return r >> (RUNS ? 3 : 2) & 3; }
+  // Byte offsets from the tile's first row on; tall: inside a row.  Rows that are not there are read as the last one.
+  __device__ __forceinline__ void place(const Operand& o, uint32_t first) {
 #pragma unroll
     for (uint32_t j = 0; j < kLoads; ++j) {
       const uint32_t slot = j * THREADS + threadIdx.x;
       if constexpr (TALL) {
-        constexpr uint32_t kAcross = ROWS / 8;
-        const uint32_t k = slot / kAcross, x = slot % kAcross, at = (x ^ ((k & 3) | (k >> 3 & 1) << 2) << 1) * 8;
-        off[j] = min(k, left - 1) * (uint32_t)(o.stride * 2) + min(at, o.along - first - 8) * 2;
+        const uint32_t k = slot / kAcross, at = (slot % kAcross ^ ((k & 3) | (k >> 3 & 1) << 2) << 1) * 8;
+        off[j] = min(at, o.along - first - 8) * 2;
       } else {
-        const uint32_t r = slot / 8;
-        off[j] = min(r, left - 1) * (uint32_t)(o.stride * 2) + ((slot & 7) ^ key(r)) * 16;
+        const uint32_t r = slot / 4;
+        off[j] = min(r, o.rows - first - 1) * (uint32_t)(o.stride * 2) + ((slot & 3) ^ key(r)) * 16;
       }
     }
   }
-  __device__ __forceinline__ void fetch(const Operand& o, uint32_t plane, uint32_t first, uint32_t k, uint8_t* to) {
-    if constexpr (TALL) {
-      const uint32_t left = min(o.rows - k, kDepth);
-      if (left != placed) place(o, first, left);   // the last tile of K, and the first one of the next planes
-    }
+  __device__ __forceinline__ void fetch(const Operand& o, uint32_t plane, uint32_t first, uint32_t k, uint8_t* to) const {
     const uint8_t* p = reinterpret_cast<const uint8_t*>(o.p + plane * o.plane + (TALL ? k * o.stride + first : first * o.stride + k));
 #pragma unroll
-    for (uint32_t j = 0; j < kLoads; ++j)
-      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(p + off[j]),
+    for (uint32_t j = 0; j < kLoads; ++j) {
+      uint32_t at = off[j];
+      if constexpr (TALL) at += min((j * THREADS + threadIdx.x) / kAcross, o.rows - 1 - k) * (uint32_t)(o.stride * 2);
+      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(p + at),
                                        (__attribute__((address_space(3))) void*)(to + j * THREADS * 16), 16, 0, 0);
+    }
   }
-  // What a lane takes to one matrix instruction: its row, the i-th sixteen of those from `rows` on, at 8 values of K, in the
-  // k-th half of the tile.
-  static __device__ __forceinline__ Quad read(const uint8_t* tile, uint32_t rows, uint32_t i, uint32_t k) {
+  // What a lane takes to COUNT matrix instructions: its rows, of the sixteens from `rows` on, at 8 values of K.
+  template <uint32_t COUNT>
+  static __device__ __forceinline__ void read(const uint8_t* tile, uint32_t rows, Quad (&out)[COUNT]) {
     const uint32_t lane = lane_id(), row = lane & 15, part = lane >> 4;
     if constexpr (TALL) {
-      typedef short Turned __attribute__((ext_vector_type(4)));
-      const uint32_t at = k * 32 + part * 8 + (row >> 2);             // and four rows on: the same bits of the order
-      const uint32_t block = rows / 16 + i, where = (block ^ ((at & 3) | (at >> 3 & 1) << 2)) * 32 + (row & 3) * 8;
-      const uint8_t* p = tile + at * (ROWS * 2) + where;
-      auto turned = [](const uint8_t* q) {
-        return __builtin_bit_cast(Pair, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) Turned*)q));
-      };
-      const Pair low = turned(p), high = turned(p + 4 * (ROWS * 2));
-      return Quad{low[0], low[1], high[0], high[1]};
+      const uint32_t at = part * 8 + (row >> 2);             // and four rows on: the same bits of the order
+      const uint32_t first = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const uint8_t*)tile + at * (ROWS * 2) +
+                             (rows / 16 ^ ((at & 3) | (at >> 3 & 1) << 2)) * 32 + (row & 3) * 8;
+      static_assert(COUNT % 4 == 0, "fours");
+#pragma unroll
+      for (uint32_t i = 0; i < COUNT; i += 4) turned<4 * ROWS * 2>(first ^ i * 32, first ^ (i + 1) * 32, first ^ (i + 2) * 32, first ^ (i + 3) * 32, out + i);
     } else {
-      const uint32_t r = rows + (RUN ? (row >> 2) * RUN + i * 4 + (row & 3) : i * 16 + row);
-      return *reinterpret_cast<const Quad*>(tile + r * 128 + ((k * 4 + part) ^ key(r)) * 16);
+#pragma unroll
+      for (uint32_t i = 0; i < COUNT; ++i) {
+        const uint32_t r = rows + (RUNS ? (row >> 2) * 8 + (row & 3) + run_of(i) : i * 16 + row);
+        out[i] = *reinterpret_cast<const Quad*>(tile + r * (kDepth * 2) + (part ^ key(r)) * 16);
+      }
     }
   }
 };
 
-// Where a wavefront's lane has its values: value r of acc[i][j] is row m + step i + r, column n + 16 j.
+// Where a wavefront's lane has its values: value r of acc[i][j] is row m + 16 i + r, or m + run_of(i) + r where the first
+// operand is wide, and column n + 16 j.
 struct Spot {
   uint32_t tile_m, tile_n, slice;   // of the workgroup
   uint32_t m0, n0;                  // the workgroup's first row and column
@@ -301,11 +314,23 @@ __device__ __forceinline__ void place(const Product& g, uint32_t tm, uint32_t tn
   s.tile_n = within / rows;
 }
 
-// A wide first operand's results are runs of neighbouring rows in a lane.
+// Waits until all but the last LOADS loads of this wavefront have arrived and its reads of LDS are done, and for all
+// wavefronts to have come here.
+template <uint32_t LOADS>
+__device__ __forceinline__ void arrive() {
+  __builtin_amdgcn_sched_barrier(0);
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LOADS) : "memory");
+  __builtin_amdgcn_sched_barrier(0);
+}
+__device__ __forceinline__ void meet() {
+  __builtin_amdgcn_sched_barrier(0);
+  asm volatile("s_barrier" ::: "memory");
+  __builtin_amdgcn_sched_barrier(0);
+}
+
 template <class H, class S, bool TALL_A, bool TALL_B, class E>
 __global__ __launch_bounds__(S::kThreads) void product_kernel(Product g, E epilogue) {
-  __shared__ __attribute__((aligned(128))) uint8_t lds[2 * S::kStage];
-  constexpr uint32_t kRun = TALL_A ? 0 : S::MT * 4;
+  __shared__ __attribute__((aligned(128))) uint8_t lds[S::kStages * S::kStage];
   const uint32_t lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(wave_id());
   Spot s;
   place(g, S::TM, S::TN, s);
@@ -313,56 +338,70 @@ __global__ __launch_bounds__(S::kThreads) void product_kernel(Product g, E epilo
   s.n0 = s.tile_n * S::TN;
   s.wm = wave / S::WN;
   s.wn = wave % S::WN;
-  s.m = s.m0 + s.wm * S::MT * 16 + (lane >> 4) * (kRun ? kRun : 4);
+  s.m = s.m0 + s.wm * S::MT * 16 + (lane >> 4) * (TALL_A ? 4 : 8);
   s.n = s.n0 + s.wn * S::NT * 16 + (lane & 15);
   const uint32_t all = g.pairs * g.k_tiles, per = (all + g.slices - 1) / g.slices;
-  const uint32_t from = min(s.slice * per, all), to = min(from + per, all);
-  using TileA = Tile<TALL_A, S::TM, S::kThreads, kRun>;
-  using TileB = Tile<TALL_B, S::TN, S::kThreads, 0>;
+  const uint32_t from = min(s.slice * per, all), count = min(from + per, all) - from;
+  using TileA = Tile<TALL_A, S::TM, S::kThreads, !TALL_A>;
+  using TileB = Tile<TALL_B, S::TN, S::kThreads, false>;
   TileA ta;
   TileB tb;
-  ta.place(g.a, s.m0, TALL_A ? kDepth : g.a.rows - s.m0);
-  tb.place(g.b, s.n0, TALL_B ? kDepth : g.b.rows - s.n0);
-  auto fetch = [&](uint32_t tile) {
-    const uint32_t pair = tile / g.k_tiles, k = tile % g.k_tiles * kDepth;
-    uint8_t* l = lds + (tile - from & 1) * S::kStage + wave * kWave * 16;
-    ta.fetch(g.a, g.a_planes >> 4 * pair & 15, s.m0, k, l);
-    tb.fetch(g.b, g.b_planes >> 4 * pair & 15, s.n0, k, l + S::TM * kDepth * 2);
+  ta.place(g.a, s.m0);
+  tb.place(g.b, s.n0);
+  uint32_t pair = from / g.k_tiles, k = from % g.k_tiles, fill = 0;   // of the next tile that is fetched, and its stage
+  auto fetch = [&]() {
+    uint8_t* l = lds + fill * S::kStage + wave * kWave * 16;
+    ta.fetch(g.a, g.a_planes >> 4 * pair & 15, s.m0, k * kDepth, l);
+    tb.fetch(g.b, g.b_planes >> 4 * pair & 15, s.n0, k * kDepth, l + S::TM * kDepth * 2);
+    const bool over = ++k == g.k_tiles;
+    k = over ? 0 : k;
+    pair += over;
+    fill = fill + 1 == S::kStages ? 0 : fill + 1;
   };
   Four acc[S::MT][S::NT];
 #pragma unroll
   for (uint32_t i = 0; i < S::MT; ++i)
 #pragma unroll
     for (uint32_t j = 0; j < S::NT; ++j) acc[i][j] = Four{0.0f, 0.0f, 0.0f, 0.0f};
-  Quad a[2][S::MT], b[2][S::NT];
-  auto read = [&](uint32_t tile, uint32_t k) {
-    const uint8_t* l = lds + (tile - from & 1) * S::kStage;
-#pragma unroll
-    for (uint32_t j = 0; j < S::NT; ++j) b[k][j] = TileB::read(l + S::TM * kDepth * 2, s.wn * S::NT * 16, j, k);
-#pragma unroll
-    for (uint32_t i = 0; i < S::MT; ++i) a[k][i] = TileA::read(l, s.wm * S::MT * 16, i, k);
+  // Every wavefront reads a tile from LDS, meets the others, multiplies it, meets them again; of the two that share a SIMD one is
+  // half a turn behind, so that one reads while the other multiplies.  The tiles behind are on their way into LDS: a stage is
+  // fetched into when the tile after the one it held is read, which the later ones have read too by then; what is read next has
+  // arrived, everybody's share of it, when all meet after reading.
+  constexpr uint32_t kLoads = TileA::kLoads + TileB::kLoads;
+  Quad a[S::MT], b[S::NT];
+  uint32_t take = 0;                                                  // the stage that is read next
+  auto read = [&]() {
+    const uint8_t* l = lds + take * S::kStage;
+    TileB::read(l + S::TM * kDepth * 2, s.wn * S::NT * 16, b);
+    TileA::read(l, s.wm * S::MT * 16, a);
+    take = take + 1 == S::kStages ? 0 : take + 1;
   };
-  auto multiply = [&](uint32_t k) {
+  auto multiply = [&]() {
 #pragma unroll
     for (uint32_t i = 0; i < S::MT; ++i)
 #pragma unroll
-      for (uint32_t j = 0; j < S::NT; ++j) acc[i][j] = mfma<H>(a[k][i], b[k][j], acc[i][j]);
+      for (uint32_t j = 0; j < S::NT; ++j) acc[i][j] = mfma<H>(a[i], b[j], acc[i][j]);
   };
-  // Two stages.  What a half of a tile is multiplied from is read while the half before is multiplied; a stage is fetched into
-  // as soon as its second half is in registers, half a tile ahead of the barrier at which it has to be there.
-  if (from < to) {
-    fetch(from);
-    __syncthreads();
-    if (from + 1 < to) fetch(from + 1);
-    read(from, 0);
-    for (uint32_t tile = from; tile < to; ++tile) {
-      read(tile, 1);
-      multiply(0);
-      __syncthreads();   // the next tile has arrived, and all have read this one
-      if (tile + 2 < to) fetch(tile + 2);
-      if (tile + 1 < to) read(tile + 1, 0);
-      multiply(1);
+  if (count) {
+    const bool behind = wave & 4;
+    for (uint32_t t = 0; t + 1 < S::kStages && t < count; ++t) fetch();
+    arrive<0>();
+    if (behind) meet();
+    uint32_t t = 0;
+    for (; t + S::kStages <= count; ++t) {
+      fetch();
+      read();
+      arrive<(S::kStages - 2) * kLoads>();
+      multiply();
+      meet();
     }
+    for (; t < count; ++t) {
+      read();
+      arrive<0>();
+      multiply();
+      meet();
+    }
+    if (!behind) meet();
   }
   __syncthreads();
   epilogue.template operator()<S>(acc, s, lds);
@@ -403,14 +442,14 @@ struct StatsEnd {
 #pragma unroll
         for (uint32_t r = 0; r < 4; ++r) {
           z[i][r] = acc[i][j][r] * f;
-          if (WHOLE || s.m + i * 4 + r < rest) top = fmaxf(top, z[i][r]);
+          if (WHOLE || s.m + run_of(i) + r < rest) top = fmaxf(top, z[i][r]);
         }
-      if (label >= 0 && label < 4 * (int64_t)S::MT && (WHOLE || s.m + label < rest)) {
+      if (label >= 0 && label < 16 * (int64_t)S::MT && label % 32 < 8) {
 #pragma unroll
         for (uint32_t i = 0; i < S::MT; ++i)
 #pragma unroll
           for (uint32_t r = 0; r < 4; ++r)
-            if (i * 4 + r == (uint32_t)label) answer[token] = z[i][r];
+            if (run_of(i) + r == (uint32_t)label) answer[token] = z[i][r];
       }
       top = fmaxf(top, __shfl_xor(top, 16, 64));
       top = fmaxf(top, __shfl_xor(top, 32, 64));
@@ -418,7 +457,7 @@ struct StatsEnd {
       for (uint32_t i = 0; i < S::MT; ++i)
 #pragma unroll
         for (uint32_t r = 0; r < 4; ++r)
-          if (WHOLE || s.m + i * 4 + r < rest) sum += exp_of(z[i][r] - top);
+          if (WHOLE || s.m + run_of(i) + r < rest) sum += exp_of(z[i][r] - top);
       sum += __shfl_xor(sum, 16, 64);
       sum += __shfl_xor(sum, 32, 64);
       if (lane_id() < 16) shared[s.wm * S::TN + token - s.n0] = float2{top, sum};
@@ -487,7 +526,7 @@ struct GradEnd {
       const float2 st = live ? stats[token] : float2{0.0f, 1.0f};
       const float w = live ? who.weight(token) * scale * factors->grad : 0.0f, over = w / st.y;
       const int64_t label = live ? who.label(token) - first - s.m : -1;
-      const bool here = label >= 0 && label < 4 * (int64_t)S::MT;
+      const bool here = label >= 0 && label < 16 * (int64_t)S::MT && label % 32 < 8;
       const uint32_t there = live && s.m < rest ? rest - s.m : 0u;      // of the lane's rows
       if (token >= tokens) continue;
 #pragma unroll
@@ -496,17 +535,17 @@ struct GradEnd {
 #pragma unroll
         for (uint32_t r = 0; r < 8; ++r) {
           float x = exp_of(acc[i + r / 4][j][r % 4] * f - st.x) * over;
-          if (here && i * 4 + r == (uint32_t)label) x -= w;
-          x = i * 4 + r < there ? x : 0.0f;
+          if (here && run_of(i) + r == (uint32_t)label) x -= w;
+          x = run_of(i) + r < there ? x : 0.0f;
           split<H, P>(x, out[r]);
-          if (here && i * 4 + r == (uint32_t)label) rests[token] = x - (float)__builtin_bit_cast(H, out[r][0]);
+          if (here && run_of(i) + r == (uint32_t)label) rests[token] = x - (float)__builtin_bit_cast(H, out[r][0]);
         }
 #pragma unroll
         for (uint32_t p = 0; p < P; ++p) {
           Quad q;
 #pragma unroll
           for (uint32_t r = 0; r < 4; ++r) q[r] = out[2 * r][p] | (uint32_t)out[2 * r + 1][p] << 16;
-          *reinterpret_cast<Quad*>(g + p * plane + token * stride + s.m + i * 4) = q;
+          *reinterpret_cast<Quad*>(g + p * plane + token * stride + s.m + run_of(i)) = q;
         }
       }
     }
@@ -613,9 +652,9 @@ __global__ __launch_bounds__(256) void zero_rows_kernel(uint64_t rows, uint32_t 
 }
 
 // ------------------------------------------------------------------------------ host
-using Large = Shape<2, 4, 8, 4>;   // 256 x 256
-using Small = Shape<2, 2, 4, 4>;   // 128 x 128
-using Thin = Shape<4, 1, 4, 2>;    // 256 x 32: few tokens
+using Large = Shape<2, 4, 8, 4, 5>;   // 256 x 256, all of a CU's LDS
+using Small = Shape<2, 2, 4, 4, 5>;   // 128 x 128, half of it
+using Thin = Shape<4, 1, 4, 4, 4>;    // 256 x 64, half of it: few tokens
 
 template <class T>
 struct Kind {                      // how matrices of a type are multiplied
