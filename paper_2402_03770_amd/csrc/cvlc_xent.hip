@@ -213,28 +213,59 @@ struct Shape {
 // Where a lane's rows are that belong to the i-th matrix instruction: eight neighbouring ones to two of them.
 constexpr __host__ __device__ uint32_t run_of(uint32_t i) { return i / 2 * 32 + i % 2 * 4; }
 
-// Eight reads of LDS that turn four rows of sixteen elements, FOUR bytes between the halves of a Quad.  One block of assembly with
-// its wait: the builtin's read is taken for one that needs all that is on its way into LDS, and waits for it.
-template <uint32_t FOUR>
-__device__ __forceinline__ void turned(uint32_t a, uint32_t b, uint32_t c, uint32_t d, Quad* out) {
-  Pair x[8];
-  asm volatile(
-      "ds_read_b64_tr_b16 %0, %8\n\tds_read_b64_tr_b16 %1, %8 offset:%12\n\tds_read_b64_tr_b16 %2, %9\n\tds_read_b64_tr_b16 %3, %9 offset:%12\n\t"
-      "ds_read_b64_tr_b16 %4, %10\n\tds_read_b64_tr_b16 %5, %10 offset:%12\n\tds_read_b64_tr_b16 %6, %11\n\tds_read_b64_tr_b16 %7, %11 offset:%12\n\t"
-      "s_waitcnt lgkmcnt(0)"
-      : "=&v"(x[0]), "=&v"(x[1]), "=&v"(x[2]), "=&v"(x[3]), "=&v"(x[4]), "=&v"(x[5]), "=&v"(x[6]), "=&v"(x[7])
-      : "v"(a), "v"(b), "v"(c), "v"(d), "n"(FOUR)
-      : "memory");
+// What lanes take to N matrix instructions, each from two reads of LDS that turn four rows of sixteen elements, FOUR bytes apart.
+// One block of assembly with its wait: the builtin's read is taken for one that needs all that is on its way into LDS, and waits
+// for it.
+template <uint32_t FOUR, uint32_t N>
+__device__ __forceinline__ void turned(const uint32_t (&at)[N], Quad (&out)[N]) {
+  static_assert(N == 4 || N == 8 || N == 12, "blocks by size");
+  Pair x[2 * N];
+  if constexpr (N == 4) {
+    asm volatile(
+        "ds_read_b64_tr_b16 %0, %8\n\tds_read_b64_tr_b16 %1, %8 offset:%12\n\tds_read_b64_tr_b16 %2, %9\n\tds_read_b64_tr_b16 %3, %9 offset:%12\n\t"
+        "ds_read_b64_tr_b16 %4, %10\n\tds_read_b64_tr_b16 %5, %10 offset:%12\n\tds_read_b64_tr_b16 %6, %11\n\tds_read_b64_tr_b16 %7, %11 offset:%12\n\t"
+        "s_waitcnt lgkmcnt(0)"
+        : "=&v"(x[0]), "=&v"(x[1]), "=&v"(x[2]), "=&v"(x[3]), "=&v"(x[4]), "=&v"(x[5]), "=&v"(x[6]), "=&v"(x[7])
+        : "v"(at[0]), "v"(at[1]), "v"(at[2]), "v"(at[3]), "n"(FOUR)
+        : "memory");
+  } else if constexpr (N == 8) {
+    asm volatile(
+        "ds_read_b64_tr_b16 %0, %16\n\tds_read_b64_tr_b16 %1, %16 offset:%24\n\tds_read_b64_tr_b16 %2, %17\n\tds_read_b64_tr_b16 %3, %17 offset:%24\n\t"
+        "ds_read_b64_tr_b16 %4, %18\n\tds_read_b64_tr_b16 %5, %18 offset:%24\n\tds_read_b64_tr_b16 %6, %19\n\tds_read_b64_tr_b16 %7, %19 offset:%24\n\t"
+        "ds_read_b64_tr_b16 %8, %20\n\tds_read_b64_tr_b16 %9, %20 offset:%24\n\tds_read_b64_tr_b16 %10, %21\n\tds_read_b64_tr_b16 %11, %21 offset:%24\n\t"
+        "ds_read_b64_tr_b16 %12, %22\n\tds_read_b64_tr_b16 %13, %22 offset:%24\n\tds_read_b64_tr_b16 %14, %23\n\tds_read_b64_tr_b16 %15, %23 offset:%24\n\t"
+        "s_waitcnt lgkmcnt(0)"
+        : "=&v"(x[0]), "=&v"(x[1]), "=&v"(x[2]), "=&v"(x[3]), "=&v"(x[4]), "=&v"(x[5]), "=&v"(x[6]), "=&v"(x[7]), "=&v"(x[8]),
+          "=&v"(x[9]), "=&v"(x[10]), "=&v"(x[11]), "=&v"(x[12]), "=&v"(x[13]), "=&v"(x[14]), "=&v"(x[15])
+        : "v"(at[0]), "v"(at[1]), "v"(at[2]), "v"(at[3]), "v"(at[4]), "v"(at[5]), "v"(at[6]), "v"(at[7]), "n"(FOUR)
+        : "memory");
+  } else {
+    asm volatile(
+        "ds_read_b64_tr_b16 %0, %24\n\tds_read_b64_tr_b16 %1, %24 offset:%36\n\tds_read_b64_tr_b16 %2, %25\n\tds_read_b64_tr_b16 %3, %25 offset:%36\n\t"
+        "ds_read_b64_tr_b16 %4, %26\n\tds_read_b64_tr_b16 %5, %26 offset:%36\n\tds_read_b64_tr_b16 %6, %27\n\tds_read_b64_tr_b16 %7, %27 offset:%36\n\t"
+        "ds_read_b64_tr_b16 %8, %28\n\tds_read_b64_tr_b16 %9, %28 offset:%36\n\tds_read_b64_tr_b16 %10, %29\n\tds_read_b64_tr_b16 %11, %29 offset:%36\n\t"
+        "ds_read_b64_tr_b16 %12, %30\n\tds_read_b64_tr_b16 %13, %30 offset:%36\n\tds_read_b64_tr_b16 %14, %31\n\tds_read_b64_tr_b16 %15, %31 offset:%36\n\t"
+        "ds_read_b64_tr_b16 %16, %32\n\tds_read_b64_tr_b16 %17, %32 offset:%36\n\tds_read_b64_tr_b16 %18, %33\n\tds_read_b64_tr_b16 %19, %33 offset:%36\n\t"
+        "ds_read_b64_tr_b16 %20, %34\n\tds_read_b64_tr_b16 %21, %34 offset:%36\n\tds_read_b64_tr_b16 %22, %35\n\tds_read_b64_tr_b16 %23, %35 offset:%36\n\t"
+        "s_waitcnt lgkmcnt(0)"
+        : "=&v"(x[0]), "=&v"(x[1]), "=&v"(x[2]), "=&v"(x[3]), "=&v"(x[4]), "=&v"(x[5]), "=&v"(x[6]), "=&v"(x[7]), "=&v"(x[8]),
+          "=&v"(x[9]), "=&v"(x[10]), "=&v"(x[11]), "=&v"(x[12]), "=&v"(x[13]), "=&v"(x[14]), "=&v"(x[15]), "=&v"(x[16]),
+          "=&v"(x[17]), "=&v"(x[18]), "=&v"(x[19]), "=&v"(x[20]), "=&v"(x[21]), "=&v"(x[22]), "=&v"(x[23])
+        : "v"(at[0]), "v"(at[1]), "v"(at[2]), "v"(at[3]), "v"(at[4]), "v"(at[5]), "v"(at[6]), "v"(at[7]), "v"(at[8]),
+          "v"(at[9]), "v"(at[10]), "v"(at[11]), "n"(FOUR)
+        : "memory");
+  }
 #pragma unroll
-  for (uint32_t i = 0; i < 4; ++i) out[i] = Quad{x[2 * i][0], x[2 * i][1], x[2 * i + 1][0], x[2 * i + 1][1]};
+  for (uint32_t i = 0; i < N; ++i) out[i] = Quad{x[2 * i][0], x[2 * i][1], x[2 * i + 1][0], x[2 * i + 1][1]};
 }
 
 // One operand's tile in LDS: how it is fetched and read.  Tiles go straight to LDS, 16 bytes a lane in the order of the
 // lanes; where in memory a lane reads decides what lies where, and it is so that the lanes that read LDS together find
 // different banks:
-//   wide: a row has four accesses, and sixteen rows are read at one K.  Access x of row r lies at x ^ key(r), with key in bits
-//     2 and 3 of r, or, where a lane's results are runs of neighbouring rows (the matrix instruction's row i of sixteen is row
-//     8 (i / 4) + i % 4 of the wavefront's then), in bits 3 and 4.
+//   wide: a row has four accesses.  Lanes 16 apart read neighbouring ones of a row, sixteen lanes their own rows; together go
+//     lanes 0 to 3, 12 to 15, 20 to 27 and such.  Access x of row r lies at x ^ key(q), q in bits 2 and 3 of r, or, where a lane's
+//     results are runs of neighbouring rows (the matrix instruction's row i of sixteen is row 8 (i / 4) + i % 4 of the
+//     wavefront's then), in bits 3 and 4.
 //   tall: sixteen neighbouring elements of a row are read from four rows by sixteen lanes, which hand them round (the read
 //     turns them).  Such a block b of row k lies at b ^ (k % 4 + 4 (k / 8 % 2)).
 template <bool TALL, uint32_t ROWS, uint32_t THREADS, bool RUNS>
@@ -244,7 +275,10 @@ struct Tile {
   static constexpr uint32_t kAcross = ROWS / 8;   // tall: accesses of a row
   uint32_t off[kLoads];
 
-  static __device__ __forceinline__ uint32_t key(uint32_t r) { return r >> (RUNS ? 3 : 2) & 3; }
+  static __device__ __forceinline__ uint32_t key(uint32_t r) {
+    const uint32_t q = r >> (RUNS ? 3 : 2) & 3;
+    return (q ^ q >> 1) % 2 * 2 + q / 2;   // 0, 2, 3, 1
+  }
   // Byte offsets from the tile's first row on; tall: inside a row.  Rows that are not there are read as the last one.
   __device__ __forceinline__ void place(const Operand& o, uint32_t first) {
 #pragma unroll
@@ -269,18 +303,23 @@ struct Tile {
                                        (__attribute__((address_space(3))) void*)(to + j * THREADS * 16), 16, 0, 0);
     }
   }
-  // What a lane takes to COUNT matrix instructions: its rows, of the sixteens from `rows` on, at 8 values of K.
+  // Where a lane reads what it takes to COUNT matrix instructions: its rows, of the sixteens from `rows` on, at 8 values of K.
+  template <uint32_t COUNT, uint32_t ALL>
+  static __device__ __forceinline__ void turned_at(const uint8_t* tile, uint32_t rows, uint32_t from, uint32_t (&at)[ALL]) {
+    const uint32_t lane = lane_id(), row = lane & 15, k = (lane >> 4) * 8 + (row >> 2);   // and four rows on: the same bits of the order
+    const uint32_t first = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const uint8_t*)tile + k * (ROWS * 2) +
+                           (rows / 16 ^ ((k & 3) | (k >> 3 & 1) << 2)) * 32 + (row & 3) * 8;
+#pragma unroll
+    for (uint32_t i = 0; i < COUNT; ++i) at[from + i] = first ^ i * 32;
+  }
   template <uint32_t COUNT>
   static __device__ __forceinline__ void read(const uint8_t* tile, uint32_t rows, Quad (&out)[COUNT]) {
-    const uint32_t lane = lane_id(), row = lane & 15, part = lane >> 4;
     if constexpr (TALL) {
-      const uint32_t at = part * 8 + (row >> 2);             // and four rows on: the same bits of the order
-      const uint32_t first = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const uint8_t*)tile + at * (ROWS * 2) +
-                             (rows / 16 ^ ((at & 3) | (at >> 3 & 1) << 2)) * 32 + (row & 3) * 8;
-      static_assert(COUNT % 4 == 0, "fours");
-#pragma unroll
-      for (uint32_t i = 0; i < COUNT; i += 4) turned<4 * ROWS * 2>(first ^ i * 32, first ^ (i + 1) * 32, first ^ (i + 2) * 32, first ^ (i + 3) * 32, out + i);
+      uint32_t at[COUNT];
+      turned_at<COUNT>(tile, rows, 0, at);
+      turned<4 * ROWS * 2>(at, out);
     } else {
+      const uint32_t lane = lane_id(), row = lane & 15, part = lane >> 4;
 #pragma unroll
       for (uint32_t i = 0; i < COUNT; ++i) {
         const uint32_t r = rows + (RUNS ? (row >> 2) * 8 + (row & 3) + run_of(i) : i * 16 + row);
@@ -372,8 +411,21 @@ __global__ __launch_bounds__(S::kThreads) void product_kernel(Product g, E epilo
   uint32_t take = 0;                                                  // the stage that is read next
   auto read = [&]() {
     const uint8_t* l = lds + take * S::kStage;
-    TileB::read(l + S::TM * kDepth * 2, s.wn * S::NT * 16, b);
-    TileA::read(l, s.wm * S::MT * 16, a);
+    if constexpr (TALL_A && TALL_B) {
+      static_assert(S::TM == S::TN, "rows equally far apart");
+      uint32_t at[S::MT + S::NT];
+      Quad both[S::MT + S::NT];
+      TileA::template turned_at<S::MT>(l, s.wm * S::MT * 16, 0, at);
+      TileB::template turned_at<S::NT>(l + S::TM * kDepth * 2, s.wn * S::NT * 16, S::MT, at);
+      turned<8 * S::TM>(at, both);
+#pragma unroll
+      for (uint32_t i = 0; i < S::MT; ++i) a[i] = both[i];
+#pragma unroll
+      for (uint32_t j = 0; j < S::NT; ++j) b[j] = both[S::MT + j];
+    } else {
+      TileB::read(l + S::TM * kDepth * 2, s.wn * S::NT * 16, b);
+      TileA::read(l, s.wm * S::MT * 16, a);
+    }
     take = take + 1 == S::kStages ? 0 : take + 1;
   };
   auto multiply = [&]() {
