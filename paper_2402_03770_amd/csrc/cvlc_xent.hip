@@ -71,7 +71,7 @@ struct Factors {
   float up[2], down[2];     // the same of hidden rows and table, powers of two
 };
 
-constexpr uint32_t kSurveyBlock = 256, kSurveyGrid = 1024, kSurveyAlone = 1u << 17;
+constexpr uint32_t kSurveyBlock = 256, kSurveyGrid = 1024, kSurveyEach = 4096, kSurveyAlone = 1u << 14;
 struct Matrix {
   const void* p;
   uint64_t stride;
@@ -209,6 +209,7 @@ template <uint32_t WM_, uint32_t WN_, uint32_t MT_, uint32_t NT_, uint32_t STAGE
 struct Shape {
   static constexpr uint32_t WM = WM_, WN = WN_, MT = MT_, NT = NT_, TM = WM * MT * 16, TN = WN * NT * 16, kThreads = WM * WN * kWave;
   static constexpr uint32_t kStages = STAGES, kStage = (TM + TN) * kDepth * 2;   // bytes of both operands' tiles
+  static constexpr bool kPairs = WM * WN == 8;   // wavefronts that share a SIMD
 };
 // Where a lane's rows are that belong to the i-th matrix instruction: eight neighbouring ones to two of them.
 constexpr __host__ __device__ uint32_t run_of(uint32_t i) { return i / 2 * 32 + i % 2 * 4; }
@@ -402,14 +403,13 @@ __global__ __launch_bounds__(S::kThreads) void product_kernel(Product g, E epilo
   for (uint32_t i = 0; i < S::MT; ++i)
 #pragma unroll
     for (uint32_t j = 0; j < S::NT; ++j) acc[i][j] = Four{0.0f, 0.0f, 0.0f, 0.0f};
-  // Every wavefront reads a tile from LDS, meets the others, multiplies it, meets them again; of the two that share a SIMD one is
-  // half a turn behind, so that one reads while the other multiplies.  The tiles behind are on their way into LDS: a stage is
-  // fetched into when the tile after the one it held is read, which the later ones have read too by then; what is read next has
-  // arrived, everybody's share of it, when all meet after reading.
+  // The tiles behind the one that is multiplied are on their way into LDS: a stage is fetched into as soon as all have read the
+  // tile it held, and what is read next has arrived, everybody's share of it, when all have met.
   constexpr uint32_t kLoads = TileA::kLoads + TileB::kLoads;
-  Quad a[S::MT], b[S::NT];
+  constexpr uint32_t kSets = S::kPairs ? 1 : 2;
+  Quad a[kSets][S::MT], b[kSets][S::NT];
   uint32_t take = 0;                                                  // the stage that is read next
-  auto read = [&]() {
+  auto read = [&](uint32_t o) {
     const uint8_t* l = lds + take * S::kStage;
     if constexpr (TALL_A && TALL_B) {
       static_assert(S::TM == S::TN, "rows equally far apart");
@@ -419,41 +419,69 @@ __global__ __launch_bounds__(S::kThreads) void product_kernel(Product g, E epilo
       TileB::template turned_at<S::NT>(l + S::TM * kDepth * 2, s.wn * S::NT * 16, S::MT, at);
       turned<8 * S::TM>(at, both);
 #pragma unroll
-      for (uint32_t i = 0; i < S::MT; ++i) a[i] = both[i];
+      for (uint32_t i = 0; i < S::MT; ++i) a[o][i] = both[i];
 #pragma unroll
-      for (uint32_t j = 0; j < S::NT; ++j) b[j] = both[S::MT + j];
+      for (uint32_t j = 0; j < S::NT; ++j) b[o][j] = both[S::MT + j];
     } else {
-      TileB::read(l + S::TM * kDepth * 2, s.wn * S::NT * 16, b);
-      TileA::read(l, s.wm * S::MT * 16, a);
+      TileB::read(l + S::TM * kDepth * 2, s.wn * S::NT * 16, b[o]);
+      TileA::read(l, s.wm * S::MT * 16, a[o]);
     }
     take = take + 1 == S::kStages ? 0 : take + 1;
   };
-  auto multiply = [&]() {
+  auto multiply = [&](uint32_t o) {
 #pragma unroll
     for (uint32_t i = 0; i < S::MT; ++i)
 #pragma unroll
-      for (uint32_t j = 0; j < S::NT; ++j) acc[i][j] = mfma<H>(a[i], b[j], acc[i][j]);
+      for (uint32_t j = 0; j < S::NT; ++j) acc[i][j] = mfma<H>(a[o][i], b[o][j], acc[i][j]);
   };
   if (count) {
-    const bool behind = wave & 4;
     for (uint32_t t = 0; t + 1 < S::kStages && t < count; ++t) fetch();
     arrive<0>();
-    if (behind) meet();
     uint32_t t = 0;
-    for (; t + S::kStages <= count; ++t) {
-      fetch();
-      read();
-      arrive<(S::kStages - 2) * kLoads>();
-      multiply();
-      meet();
+    if constexpr (S::kPairs) {
+      // Two wavefronts share a SIMD, one half a turn behind the other: one reads while the other multiplies.
+      const bool behind = wave & 4;
+      if (behind) meet();
+      for (; t + S::kStages <= count; ++t) {
+        fetch();
+        read(0);
+        arrive<(S::kStages - 2) * kLoads>();
+        multiply(0);
+        meet();
+      }
+      for (; t < count; ++t) {
+        read(0);
+        arrive<0>();
+        multiply(0);
+        meet();
+      }
+      if (!behind) meet();
+    } else {
+      // A wavefront has its SIMD to itself: it reads the next tile into other registers before it multiplies.
+      read(0);
+      if (S::kStages - 1 < count) fetch();
+      for (; t + S::kStages + 2 <= count; t += 2) {
+#pragma unroll
+        for (uint32_t o = 0; o < 2; ++o) {
+          arrive<(S::kStages - 2) * kLoads>();
+          fetch();
+          read(o ^ 1);
+          multiply(o);
+        }
+      }
+      for (; t < count; t += 2) {
+        arrive<0>();
+        if (t + S::kStages < count) fetch();
+        if (t + 1 < count) read(1);
+        multiply(0);
+        if (t + 1 < count) {
+          arrive<0>();
+          if (t + 1 + S::kStages < count) fetch();
+          if (t + 2 < count) read(0);
+          multiply(1);
+        }
+      }
     }
-    for (; t < count; ++t) {
-      read();
-      arrive<0>();
-      multiply();
-      meet();
-    }
-    if (!behind) meet();
   }
   __syncthreads();
   epilogue.template operator()<S>(acc, s, lds);
@@ -530,12 +558,14 @@ struct StatsEnd {
   }
 };
 
-// The tiles' statistics joined, and the losses.
-constexpr uint32_t kJoinTokens = 16, kJoinRows = 16;
-__global__ __launch_bounds__(kJoinTokens * kJoinRows) void loss_kernel(Rows who, uint32_t tiles, const float2* partial, const float* answer,
-                                                                       float* loss, float2* stats, uint32_t* status) {
-  __shared__ float2 shared[kJoinRows][kJoinTokens];
-  const uint32_t x = threadIdx.x % kJoinTokens, y = threadIdx.x / kJoinTokens, token = blockIdx.x * kJoinTokens + x;
+// The tiles' statistics joined, and the losses: a workgroup has 2^tokens_log2 tokens, fewer where there are few.
+constexpr uint32_t kJoinBlock = 256;
+uint32_t join_tokens_log2(uint32_t n) { return n >= 16384 ? 4 : n >= 2048 ? 2 : 0; }
+__global__ __launch_bounds__(kJoinBlock) void loss_kernel(Rows who, uint32_t tiles, uint32_t tokens_log2, const float2* partial,
+                                                          const float* answer, float* loss, float2* stats, uint32_t* status) {
+  __shared__ float2 shared[kJoinBlock];
+  const uint32_t tokens = 1u << tokens_log2, rows = kJoinBlock >> tokens_log2;
+  const uint32_t x = threadIdx.x & (tokens - 1), y = threadIdx.x >> tokens_log2, token = (blockIdx.x << tokens_log2) + x;
   float2 all = {-INFINITY, 0.0f};
   auto add = [](float2 a, float2 b) {
     const float top = fmaxf(a.x, b.x);
@@ -543,11 +573,14 @@ __global__ __launch_bounds__(kJoinTokens * kJoinRows) void loss_kernel(Rows who,
     return float2{top, a.y * expf(a.x - top) + b.y * expf(b.x - top)};
   };
   if (token < who.n)
-    for (uint32_t t = y; t < tiles; t += kJoinRows) all = add(all, partial[(uint64_t)t * who.n + token]);
-  shared[y][x] = all;
-  __syncthreads();
+#pragma unroll 4
+    for (uint32_t t = y; t < tiles; t += rows) all = add(all, partial[(uint64_t)t * who.n + token]);
+  shared[threadIdx.x] = all;
+  for (uint32_t half = rows / 2; half; half /= 2) {
+    __syncthreads();
+    if (y < half) shared[threadIdx.x] = all = add(all, shared[threadIdx.x + (half << tokens_log2)]);
+  }
   if (y || token >= who.n) return;
-  for (uint32_t r = 1; r < kJoinRows; ++r) all = add(all, shared[r][x]);
   if (status && who.label(token) >= (int64_t)who.vocab) atomicOr(status, CVLC_DEV_INDEX);
   const bool live = who.live(token);
   if (loss) loss[token] = live ? who.weight(token) * (logf(all.y) + (all.x - answer[token])) : 0.0f;
@@ -726,19 +759,22 @@ void set_pairs(Product& g, uint32_t pa, uint32_t pb) {
       }
 }
 
-template <class S>
-uint64_t tiles_of(const Product& g) {
-  return (uint64_t)((g.m + S::TM - 1) / S::TM) * ((g.n + S::TN - 1) / S::TN);
-}
 constexpr uint32_t kCus = 256;
-// Large tiles take four times as long as small ones would each, but half of that a value, one to a CU where two small ones are.
-bool large_goes(const Product& g) {
-  const uint64_t large = (tiles_of<Large>(g) * g.slices + kCus - 1) / kCus * 4, small = (tiles_of<Small>(g) * g.slices + 2 * kCus - 1) / (2 * kCus) * 2;
-  return large * 3 <= small * 4;
+uint64_t tiles(uint64_t m, uint64_t n, uint64_t tm, uint64_t tn) { return ((m + tm - 1) / tm) * ((n + tn - 1) / tn); }
+// What a product of m x n takes for each value of K, in hundredths of what 256 large tiles do (32 ns: 4096 x 16384 x 2048 262 us),
+// one to a CU.  Of small tiles a CU has two, which together are half as large and take 88, or one, which takes 72.
+uint64_t cost_large(uint64_t m, uint64_t n, uint64_t slices) { return (tiles(m, n, Large::TM, Large::TN) * slices + kCus - 1) / kCus * 100; }
+uint64_t cost_small(uint64_t m, uint64_t n, uint64_t slices) {
+  const uint64_t all = tiles(m, n, Small::TM, Small::TN) * slices, rest = all % (2 * kCus);
+  return all / (2 * kCus) * 88 + (rest > kCus ? 88 : rest ? 72 : 0);
 }
+bool large_goes(const Product& g) { return cost_large(g.m, g.n, g.slices) <= cost_small(g.m, g.n, g.slices); }
+uint64_t cost(uint64_t m, uint64_t n, uint64_t slices) { return std::min(cost_large(m, n, slices), cost_small(m, n, slices)); }
+
 template <class H, bool TALL_A, bool TALL_B, class S, class E>
 void run_as(const Product& g, const E& end, hipStream_t stream) {
-  hipLaunchKernelGGL((product_kernel<H, S, TALL_A, TALL_B, E>), dim3((uint32_t)(tiles_of<S>(g) * g.slices)), dim3(S::kThreads), 0, stream, g, end);
+  hipLaunchKernelGGL((product_kernel<H, S, TALL_A, TALL_B, E>), dim3((uint32_t)(tiles(g.m, g.n, S::TM, S::TN) * g.slices)), dim3(S::kThreads), 0,
+                     stream, g, end);
 }
 template <class H, bool TALL_A, bool TALL_B, class E>
 void run(const Product& g, const E& end, hipStream_t stream) {
@@ -752,18 +788,45 @@ struct Sizes {
   uint64_t depth, tokens, piece;      // dim and n in whole tiles of K; tokens of the vocabulary at a time
   uint32_t planes, g_planes, slices;
 };
-constexpr uint64_t kBudget = 256ull << 20;   // bytes of a piece's G and table
+constexpr uint64_t kBudget = 320ull << 20;   // bytes of a piece's G and table, about; less would end dh's sums too often
+constexpr uint64_t kSlicesMost = 16, kSliceMin = 128;   // parts of a piece that dh's product is cut into, and tokens of each at least
+constexpr uint64_t kLaunchCost = 30000;                 // a launch's own time, about 10 us
 Sizes sizes_for(uint32_t n, uint32_t vocab, uint32_t dim, uint32_t type, uint32_t dtable_type, bool grad) {
   Sizes z{};
   z.depth = pad_to(dim, kDepth);
   z.tokens = pad_to(n, kDepth);
   z.planes = type == CVLC_F32 ? 2 : 1;
   z.g_planes = dtable_type == CVLC_F32 ? 2 : 1;
+  z.slices = 1;
   const uint64_t each = z.depth * z.planes * 2 + (grad ? z.tokens * z.g_planes * 2 : 0);
-  z.piece = std::min(pad_to(vocab, kPadTo), std::max<uint64_t>(kPadTo, kBudget / each / kPadTo * kPadTo));
-  // dh has few tiles where tokens and columns are few: K, a piece of the vocabulary, is cut then
-  const uint64_t tiles = ((z.depth + 255) / 256) * ((z.tokens + 255) / 256);
-  z.slices = (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>(kCus / std::max<uint64_t>(tiles, 1), z.piece / 512));
+  const uint64_t whole = pad_to(vocab, kPadTo) / kPadTo, most = std::min(whole, std::max<uint64_t>(1, kBudget / each / kPadTo));
+  z.piece = most * kPadTo;
+  if (!grad) return z;
+  // A launch lasts as long as its fullest CU: of the pieces' sizes the one whose launches take least together.  A slice of dh's
+  // product is written and read again, 8 bytes a value at 5 TB/s.
+  auto of_piece = [&](uint64_t t, uint32_t* slices) {
+    const uint64_t rows = t * kPadTo;
+    uint64_t best = ~0ull;
+    for (uint64_t s = 1; s <= kSlicesMost && (s == 1 || rows / s >= kSliceMin); ++s) {
+      const uint64_t c = cost(dim, n, s) * (rows / s) * (z.planes == 1 ? 1 : 3) + s * n * (uint64_t)dim / 200;
+      if (c < best) {
+        best = c;
+        *slices = (uint32_t)s;
+      }
+    }
+    return best + cost(rows, n, 1) * z.depth * (z.planes == 1 ? 1 : 3) + cost(dim, rows, 1) * z.tokens * (z.planes == 1 ? z.g_planes : 3) + 3 * kLaunchCost;
+  };
+  uint64_t best = ~0ull;
+  const uint64_t step = std::max<uint64_t>(1, most / 128);
+  for (uint64_t t = most; t >= std::max<uint64_t>(1, most / 2); t -= std::min(step, t)) {
+    uint32_t slices = 1, other;
+    const uint64_t rest = whole % t, c = of_piece(t, &slices) * (whole / t) + (rest ? of_piece(rest, &other) : 0);
+    if (c < best) {
+      best = c;
+      z.piece = t * kPadTo;
+      z.slices = slices;
+    }
+  }
   return z;
 }
 
@@ -838,9 +901,10 @@ void find_factors(const Call& c, const Sizes& z, const Parts& parts, uint32_t* s
   } else if ((uint64_t)(c.n + (uint64_t)c.vocab) * c.dim <= kSurveyAlone) {
     hipLaunchKernelGGL(factors_kernel, dim3(1), dim3(1024), 0, stream, c.who, c.scale, nullptr, 0, hidden, table, c.dim, parts.factors, status);
   } else {
-    hipLaunchKernelGGL(survey_kernel, dim3(kSurveyGrid, 2), dim3(kSurveyBlock), 0, stream, hidden, table, c.dim, c.who, parts.tops);
-    hipLaunchKernelGGL(factors_kernel, dim3(1), dim3(1024), 0, stream, c.who, c.scale, parts.tops, kSurveyGrid, none, none, c.dim,
-                       parts.factors, status);
+    const uint32_t grid = (uint32_t)std::min<uint64_t>(((uint64_t)std::max(c.n, c.vocab) * c.dim + kSurveyEach - 1) / kSurveyEach, kSurveyGrid);
+    hipLaunchKernelGGL(survey_kernel, dim3(grid, 2), dim3(kSurveyBlock), 0, stream, hidden, table, c.dim, c.who, parts.tops);
+    hipLaunchKernelGGL(factors_kernel, dim3(1), dim3(1024), 0, stream, c.who, c.scale, parts.tops, grid, none, none, c.dim, parts.factors,
+                       status);
   }
 }
 
@@ -890,8 +954,9 @@ void loss_of(const Call& c, const Sizes& z, const LossParts& parts, float* loss,
     else
       go(Small{});
   }
-  hipLaunchKernelGGL(loss_kernel, dim3((c.n + kJoinTokens - 1) / kJoinTokens), dim3(kJoinTokens * kJoinRows), 0, stream, c.who, tile,
-                     parts.partial, parts.answer, loss, stats, status);
+  const uint32_t log2 = join_tokens_log2(c.n);
+  hipLaunchKernelGGL(loss_kernel, dim3((c.n + (1u << log2) - 1) >> log2), dim3(kJoinBlock), 0, stream, c.who, tile, log2, parts.partial,
+                     parts.answer, loss, stats, status);
 }
 
 template <class T, class TO>
