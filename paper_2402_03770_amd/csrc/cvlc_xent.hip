@@ -31,7 +31,8 @@ typedef __bf16 EightB __attribute__((ext_vector_type(8)));
 typedef _Float16 EightH __attribute__((ext_vector_type(8)));
 typedef uint16_t Half;  // 16 bits of either type
 
-constexpr uint32_t kDepth = 32;    // K of a tile: what one matrix instruction takes
+constexpr uint32_t kDepth = 64;    // K is padded to whole ones of the deepest tiles
+constexpr uint32_t kStep = 32;     // K of a matrix instruction
 constexpr uint32_t kPadTo = 256;   // vocabulary pieces are whole tiles
 constexpr float kLift = 0x1p13f;   // G's largest entries
 
@@ -191,9 +192,9 @@ struct Operand {
 struct Product {
   Operand a, b;
   uint32_t m, n;            // rows of a and of b
-  uint32_t k_tiles;         // K in tiles of kDepth
+  uint32_t k;               // K, whole kDepths
   uint32_t pairs, a_planes, b_planes;  // which planes are multiplied: four bits a pair
-  uint32_t slices;          // parts that all tiles of K are cut into
+  uint32_t slices;          // parts that all planes' K is cut into
 };
 
 template <class H>
@@ -204,12 +205,15 @@ __device__ __forceinline__ Four mfma(Quad a, Quad b, Four c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(EightH, a), __builtin_bit_cast(EightH, b), c, 0, 0, 0);
 }
 
-// A tile's shape: WM x WN wavefronts of MT x NT matrix instructions (16 x 16) each; STAGES tiles of K are in LDS.
+// A tile's shape: WM x WN wavefronts of MT x NT matrix instructions (16 x 16) each.  Two wavefronts share a SIMD (kPairs), and
+// operands' tiles of kDepth are in LDS, or they do not, and there are STAGES of both operands' tiles of kStep.
 template <uint32_t WM_, uint32_t WN_, uint32_t MT_, uint32_t NT_, uint32_t STAGES>
 struct Shape {
   static constexpr uint32_t WM = WM_, WN = WN_, MT = MT_, NT = NT_, TM = WM * MT * 16, TN = WN * NT * 16, kThreads = WM * WN * kWave;
-  static constexpr uint32_t kStages = STAGES, kStage = (TM + TN) * kDepth * 2;   // bytes of both operands' tiles
-  static constexpr bool kPairs = WM * WN == 8;   // wavefronts that share a SIMD
+  static constexpr bool kPairs = WM * WN == 8;
+  static constexpr uint32_t kK = kPairs ? kDepth : kStep, kStages = STAGES;
+  static constexpr uint32_t kStage = (kPairs ? TM : TM + TN) * kK * 2;   // bytes of an operand's tile, or of both
+  static_assert(!kPairs || TM == TN, "operands' tiles in one ring");
 };
 // Where a lane's rows are that belong to the i-th matrix instruction: eight neighbouring ones to two of them.
 constexpr __host__ __device__ uint32_t run_of(uint32_t i) { return i / 2 * 32 + i % 2 * 4; }
@@ -263,20 +267,21 @@ __device__ __forceinline__ void turned(const uint32_t (&at)[N], Quad (&out)[N]) 
 // One operand's tile in LDS: how it is fetched and read.  Tiles go straight to LDS, 16 bytes a lane in the order of the
 // lanes; where in memory a lane reads decides what lies where, and it is so that the lanes that read LDS together find
 // different banks:
-//   wide: a row has four accesses.  Lanes 16 apart read neighbouring ones of a row, sixteen lanes their own rows; together go
-//     lanes 0 to 3, 12 to 15, 20 to 27 and such.  Access x of row r lies at x ^ key(q), q in bits 2 and 3 of r, or, where a lane's
-//     results are runs of neighbouring rows (the matrix instruction's row i of sixteen is row 8 (i / 4) + i % 4 of the
-//     wavefront's then), in bits 3 and 4.
+//   wide: lanes 16 apart read neighbouring accesses of a row, sixteen lanes their own rows; together go lanes 0 to 3, 12 to 15,
+//     20 to 27 and such.  Access x of row r lies at x ^ key(r).  The sixteen rows follow each other, or, where a lane's results
+//     are runs of neighbouring rows (RUNS), the matrix instruction's row i is row 8 (i / 4) + i % 4.
 //   tall: sixteen neighbouring elements of a row are read from four rows by sixteen lanes, which hand them round (the read
 //     turns them).  Such a block b of row k lies at b ^ (k % 4 + 4 (k / 8 % 2)).
-template <bool TALL, uint32_t ROWS, uint32_t THREADS, bool RUNS>
+// Tiles of half a row's 128 bytes ask the caches for every line twice, which a large tile's rate shows: it takes kDepth.
+template <bool TALL, uint32_t ROWS, uint32_t THREADS, bool RUNS, uint32_t K>
 struct Tile {
-  static constexpr uint32_t kLoads = ROWS * 4 / THREADS;
-  static_assert(kLoads * THREADS == ROWS * 4, "whole loads");
-  static constexpr uint32_t kAcross = ROWS / 8;   // tall: accesses of a row
+  static constexpr uint32_t kLoads = ROWS * K / 8 / THREADS;
+  static_assert(kLoads * THREADS == ROWS * K / 8, "whole loads");
+  static constexpr uint32_t kAcross = (TALL ? ROWS : K) / 8;   // accesses of a row
   uint32_t off[kLoads];
 
   static __device__ __forceinline__ uint32_t key(uint32_t r) {
+    if (K == 64) return RUNS ? (r >> 1 & 1) | (r >> 3 & 3) << 1 : r >> 1 & 7;
     const uint32_t q = r >> (RUNS ? 3 : 2) & 3;
     return (q ^ q >> 1) % 2 * 2 + q / 2;   // 0, 2, 3, 1
   }
@@ -284,49 +289,67 @@ struct Tile {
   __device__ __forceinline__ void place(const Operand& o, uint32_t first) {
 #pragma unroll
     for (uint32_t j = 0; j < kLoads; ++j) {
-      const uint32_t slot = j * THREADS + threadIdx.x;
-      if constexpr (TALL) {
-        const uint32_t k = slot / kAcross, at = (slot % kAcross ^ ((k & 3) | (k >> 3 & 1) << 2) << 1) * 8;
-        off[j] = min(at, o.along - first - 8) * 2;
-      } else {
-        const uint32_t r = slot / 4;
-        off[j] = min(r, o.rows - first - 1) * (uint32_t)(o.stride * 2) + ((slot & 3) ^ key(r)) * 16;
-      }
+      const uint32_t slot = j * THREADS + threadIdx.x, r = slot / kAcross, x = slot % kAcross;
+      if constexpr (TALL)
+        off[j] = min((x ^ ((r & 3) | (r >> 3 & 1) << 2) << 1) * 8, o.along - first - 8) * 2;
+      else
+        off[j] = min(r, o.rows - first - 1) * (uint32_t)(o.stride * 2) + (x ^ key(r)) * 16;
     }
   }
   __device__ __forceinline__ void fetch(const Operand& o, uint32_t plane, uint32_t first, uint32_t k, uint8_t* to) const {
-    const uint8_t* p = reinterpret_cast<const uint8_t*>(o.p + plane * o.plane + (TALL ? k * o.stride + first : first * o.stride + k));
+    const uint32_t row = TALL ? min(k, o.rows - 1) : first;   // a piece's K is padded, its last tile may begin behind its rows
+    const uint8_t* p = reinterpret_cast<const uint8_t*>(o.p + plane * o.plane + row * o.stride + (TALL ? first : k));
 #pragma unroll
     for (uint32_t j = 0; j < kLoads; ++j) {
       uint32_t at = off[j];
-      if constexpr (TALL) at += min((j * THREADS + threadIdx.x) / kAcross, o.rows - 1 - k) * (uint32_t)(o.stride * 2);
+      if constexpr (TALL) at += min((j * THREADS + threadIdx.x) / kAcross, o.rows - 1 - row) * (uint32_t)(o.stride * 2);
       __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(p + at),
                                        (__attribute__((address_space(3))) void*)(to + j * THREADS * 16), 16, 0, 0);
     }
   }
-  // Where a lane reads what it takes to COUNT matrix instructions: its rows, of the sixteens from `rows` on, at 8 values of K.
+  // Where a lane reads what it takes to COUNT matrix instructions: its rows, of the sixteens from `rows` on, at 8 values of K, of
+  // the tile's step-th kStep.
   template <uint32_t COUNT, uint32_t ALL>
-  static __device__ __forceinline__ void turned_at(const uint8_t* tile, uint32_t rows, uint32_t from, uint32_t (&at)[ALL]) {
+  static __device__ __forceinline__ void turned_at(const uint8_t* tile, uint32_t rows, uint32_t step, uint32_t from, uint32_t (&at)[ALL]) {
     const uint32_t lane = lane_id(), row = lane & 15, k = (lane >> 4) * 8 + (row >> 2);   // and four rows on: the same bits of the order
-    const uint32_t first = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const uint8_t*)tile + k * (ROWS * 2) +
+    const uint32_t first = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const uint8_t*)tile + (step * kStep + k) * (ROWS * 2) +
                            (rows / 16 ^ ((k & 3) | (k >> 3 & 1) << 2)) * 32 + (row & 3) * 8;
 #pragma unroll
     for (uint32_t i = 0; i < COUNT; ++i) at[from + i] = first ^ i * 32;
   }
   template <uint32_t COUNT>
-  static __device__ __forceinline__ void read(const uint8_t* tile, uint32_t rows, Quad (&out)[COUNT]) {
+  static __device__ __forceinline__ void read(const uint8_t* tile, uint32_t rows, uint32_t step, Quad (&out)[COUNT]) {
     if constexpr (TALL) {
       uint32_t at[COUNT];
-      turned_at<COUNT>(tile, rows, 0, at);
+      turned_at<COUNT>(tile, rows, step, 0, at);
       turned<4 * ROWS * 2>(at, out);
     } else {
       const uint32_t lane = lane_id(), row = lane & 15, part = lane >> 4;
 #pragma unroll
       for (uint32_t i = 0; i < COUNT; ++i) {
         const uint32_t r = rows + (RUNS ? (row >> 2) * 8 + (row & 3) + run_of(i) : i * 16 + row);
-        out[i] = *reinterpret_cast<const Quad*>(tile + r * (kDepth * 2) + (part ^ key(r)) * 16);
+        out[i] = *reinterpret_cast<const Quad*>(tile + r * (K * 2) + ((step * 4 + part) ^ key(r)) * 16);
       }
     }
+  }
+};
+
+// The tiles of one operand in the order in which they are multiplied: all of K for every plane in turn.
+template <class T>
+struct Walk {
+  T tile;
+  uint32_t pair, k;
+  __device__ __forceinline__ void start(const Operand& o, uint32_t first, uint32_t at, uint32_t all_k) {
+    tile.place(o, first);
+    pair = at / all_k;
+    k = at % all_k;
+  }
+  __device__ __forceinline__ void fetch(const Operand& o, uint32_t planes, uint32_t first, uint32_t step, uint32_t all_k, uint8_t* to) {
+    tile.fetch(o, planes >> 4 * pair & 15, first, k, to);
+    k += step;
+    const bool over = k == all_k;
+    k = over ? 0 : k;
+    pair += over;
   }
 };
 
@@ -362,9 +385,13 @@ __device__ __forceinline__ void arrive() {
   asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LOADS) : "memory");
   __builtin_amdgcn_sched_barrier(0);
 }
+template <bool READS = false>
 __device__ __forceinline__ void meet() {
   __builtin_amdgcn_sched_barrier(0);
-  asm volatile("s_barrier" ::: "memory");
+  if (READS)
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+  else
+    asm volatile("s_barrier" ::: "memory");
   __builtin_amdgcn_sched_barrier(0);
 }
 
@@ -380,53 +407,39 @@ __global__ __launch_bounds__(S::kThreads) void product_kernel(Product g, E epilo
   s.wn = wave % S::WN;
   s.m = s.m0 + s.wm * S::MT * 16 + (lane >> 4) * (TALL_A ? 4 : 8);
   s.n = s.n0 + s.wn * S::NT * 16 + (lane & 15);
-  const uint32_t all = g.pairs * g.k_tiles, per = (all + g.slices - 1) / g.slices;
+  const uint32_t all = g.pairs * (g.k / S::kK), per = (all + g.slices - 1) / g.slices;
   const uint32_t from = min(s.slice * per, all), count = min(from + per, all) - from;
-  using TileA = Tile<TALL_A, S::TM, S::kThreads, !TALL_A>;
-  using TileB = Tile<TALL_B, S::TN, S::kThreads, false>;
-  TileA ta;
-  TileB tb;
-  ta.place(g.a, s.m0);
-  tb.place(g.b, s.n0);
-  uint32_t pair = from / g.k_tiles, k = from % g.k_tiles, fill = 0;   // of the next tile that is fetched, and its stage
-  auto fetch = [&]() {
-    uint8_t* l = lds + fill * S::kStage + wave * kWave * 16;
-    ta.fetch(g.a, g.a_planes >> 4 * pair & 15, s.m0, k * kDepth, l);
-    tb.fetch(g.b, g.b_planes >> 4 * pair & 15, s.n0, k * kDepth, l + S::TM * kDepth * 2);
-    const bool over = ++k == g.k_tiles;
-    k = over ? 0 : k;
-    pair += over;
-    fill = fill + 1 == S::kStages ? 0 : fill + 1;
-  };
+  using TileA = Tile<TALL_A, S::TM, S::kThreads, !TALL_A, S::kK>;
+  using TileB = Tile<TALL_B, S::TN, S::kThreads, false, S::kK>;
+  Walk<TileA> wa;
+  Walk<TileB> wb;
+  wa.start(g.a, s.m0, from * S::kK, g.k);
+  wb.start(g.b, s.n0, from * S::kK, g.k);
+  auto fetch_a = [&](uint8_t* to) { wa.fetch(g.a, g.a_planes, s.m0, S::kK, g.k, to + wave * kWave * 16); };
+  auto fetch_b = [&](uint8_t* to) { wb.fetch(g.b, g.b_planes, s.n0, S::kK, g.k, to + wave * kWave * 16); };
   Four acc[S::MT][S::NT];
 #pragma unroll
   for (uint32_t i = 0; i < S::MT; ++i)
 #pragma unroll
     for (uint32_t j = 0; j < S::NT; ++j) acc[i][j] = Four{0.0f, 0.0f, 0.0f, 0.0f};
-  // The tiles behind the one that is multiplied are on their way into LDS: a stage is fetched into as soon as all have read the
-  // tile it held, and what is read next has arrived, everybody's share of it, when all have met.
-  constexpr uint32_t kLoads = TileA::kLoads + TileB::kLoads;
   constexpr uint32_t kSets = S::kPairs ? 1 : 2;
   Quad a[kSets][S::MT], b[kSets][S::NT];
-  uint32_t take = 0;                                                  // the stage that is read next
-  auto read = [&](uint32_t o) {
-    const uint8_t* l = lds + take * S::kStage;
+  auto read = [&](const uint8_t* la, const uint8_t* lb, uint32_t step, uint32_t o) {
     if constexpr (TALL_A && TALL_B) {
       static_assert(S::TM == S::TN, "rows equally far apart");
       uint32_t at[S::MT + S::NT];
       Quad both[S::MT + S::NT];
-      TileA::template turned_at<S::MT>(l, s.wm * S::MT * 16, 0, at);
-      TileB::template turned_at<S::NT>(l + S::TM * kDepth * 2, s.wn * S::NT * 16, S::MT, at);
+      TileA::template turned_at<S::MT>(la, s.wm * S::MT * 16, step, 0, at);
+      TileB::template turned_at<S::NT>(lb, s.wn * S::NT * 16, step, S::MT, at);
       turned<8 * S::TM>(at, both);
 #pragma unroll
       for (uint32_t i = 0; i < S::MT; ++i) a[o][i] = both[i];
 #pragma unroll
       for (uint32_t j = 0; j < S::NT; ++j) b[o][j] = both[S::MT + j];
     } else {
-      TileB::read(l + S::TM * kDepth * 2, s.wn * S::NT * 16, b[o]);
-      TileA::read(l, s.wm * S::MT * 16, a[o]);
+      TileB::read(lb, s.wn * S::NT * 16, step, b[o]);
+      TileA::read(la, s.wm * S::MT * 16, step, a[o]);
     }
-    take = take + 1 == S::kStages ? 0 : take + 1;
   };
   auto multiply = [&](uint32_t o) {
 #pragma unroll
@@ -434,52 +447,82 @@ __global__ __launch_bounds__(S::kThreads) void product_kernel(Product g, E epilo
 #pragma unroll
       for (uint32_t j = 0; j < S::NT; ++j) acc[i][j] = mfma<H>(a[o][i], b[o][j], acc[i][j]);
   };
-  if (count) {
+  auto next = [&](uint32_t at) { return at + 1 == S::kStages ? 0 : at + 1; };
+  uint32_t take = 0, fill = 0;                                        // places in the ring: read next, fetched into next
+  if constexpr (S::kPairs) if (count) {
+    // Two wavefronts share a SIMD, one half a turn behind the other: one reads a step's values from LDS while the other
+    // multiplies; they meet after each.  The operands' tiles go round a ring, a, b, a, b: a place is fetched into when the tile
+    // after the one it held is read, which those behind have read too by then; tiles have arrived, everybody's share of them, when
+    // all meet after the reads before.
+    const bool behind = wave & 4;
+    auto to = [&]() {
+      uint8_t* l = lds + fill * S::kStage;
+      fill = next(fill);
+      return l;
+    };
+    fetch_a(to());
+    fetch_b(to());
+    if (count > 1) fetch_a(to());
+    arrive<0>();
+    if (behind) meet<>();
+    auto tile = [&](auto more_b, auto more_a) {   // loads of the next tile's b and of the a after it
+      const uint8_t *la = lds + take * S::kStage, *lb = lds + next(take) * S::kStage;
+      take = next(next(take));
+      if (decltype(more_b)::value) fetch_b(to());
+      read(la, lb, 0, 0);
+      meet<true>();
+      multiply(0);
+      meet<>();
+      if (decltype(more_a)::value) fetch_a(to());
+      read(la, lb, 1, 0);
+      arrive<decltype(more_a)::value ? TileA::kLoads : 0>();
+      multiply(0);
+      meet<>();
+    };
+    for (uint32_t t = 0; t + 2 < count; ++t) tile(std::true_type{}, std::true_type{});
+    if (count > 1) tile(std::true_type{}, std::false_type{});
+    tile(std::false_type{}, std::false_type{});
+    if (!behind) meet<>();
+  }
+  if constexpr (!S::kPairs) if (count) {
+    // A wavefront has its SIMD to itself: it reads the next tile into other registers before it multiplies.  A stage is
+    // fetched into as soon as all have read the tile that it held.
+    constexpr uint32_t kLoads = TileA::kLoads + TileB::kLoads;
+    auto fetch = [&]() {
+      uint8_t* l = lds + fill * S::kStage;
+      fill = next(fill);
+      fetch_a(l);
+      fetch_b(l + S::TM * S::kK * 2);
+    };
+    auto read_next = [&](uint32_t o) {
+      const uint8_t* l = lds + take * S::kStage;
+      take = next(take);
+      read(l, l + S::TM * S::kK * 2, 0, o);
+    };
     for (uint32_t t = 0; t + 1 < S::kStages && t < count; ++t) fetch();
     arrive<0>();
+    read_next(0);
+    if (S::kStages - 1 < count) fetch();
     uint32_t t = 0;
-    if constexpr (S::kPairs) {
-      // Two wavefronts share a SIMD, one half a turn behind the other: one reads while the other multiplies.
-      const bool behind = wave & 4;
-      if (behind) meet();
-      for (; t + S::kStages <= count; ++t) {
-        fetch();
-        read(0);
-        arrive<(S::kStages - 2) * kLoads>();
-        multiply(0);
-        meet();
-      }
-      for (; t < count; ++t) {
-        read(0);
-        arrive<0>();
-        multiply(0);
-        meet();
-      }
-      if (!behind) meet();
-    } else {
-      // A wavefront has its SIMD to itself: it reads the next tile into other registers before it multiplies.
-      read(0);
-      if (S::kStages - 1 < count) fetch();
-      for (; t + S::kStages + 2 <= count; t += 2) {
+    for (; t + S::kStages + 2 <= count; t += 2) {
 #pragma unroll
-        for (uint32_t o = 0; o < 2; ++o) {
-          arrive<(S::kStages - 2) * kLoads>();
-          fetch();
-          read(o ^ 1);
-          multiply(o);
-        }
+      for (uint32_t o = 0; o < 2; ++o) {
+        arrive<(S::kStages - 2) * kLoads>();
+        fetch();
+        read_next(o ^ 1);
+        multiply(o);
       }
-      for (; t < count; t += 2) {
+    }
+    for (; t < count; t += 2) {
+      arrive<0>();
+      if (t + S::kStages < count) fetch();
+      if (t + 1 < count) read_next(kSets - 1);
+      multiply(0);
+      if (t + 1 < count) {
         arrive<0>();
-        if (t + S::kStages < count) fetch();
-        if (t + 1 < count) read(1);
-        multiply(0);
-        if (t + 1 < count) {
-          arrive<0>();
-          if (t + 1 + S::kStages < count) fetch();
-          if (t + 2 < count) read(0);
-          multiply(1);
-        }
+        if (t + 1 + S::kStages < count) fetch();
+        if (t + 2 < count) read_next(0);
+        multiply(kSets - 1);
       }
     }
   }
@@ -737,7 +780,7 @@ __global__ __launch_bounds__(256) void zero_rows_kernel(uint64_t rows, uint32_t 
 }
 
 // ------------------------------------------------------------------------------ host
-using Large = Shape<2, 4, 8, 4, 5>;   // 256 x 256, all of a CU's LDS
+using Large = Shape<2, 4, 8, 4, 5>;   // 256 x 256, all of a CU's LDS: five operands' tiles
 using Small = Shape<2, 2, 4, 4, 5>;   // 128 x 128, half of it
 using Thin = Shape<4, 1, 4, 4, 4>;    // 256 x 64, half of it: few tokens
 
@@ -929,7 +972,7 @@ void loss_of(const Call& c, const Sizes& z, const LossParts& parts, float* loss,
   Product g{};
   g.b = hidden_goes ? Operand{static_cast<const Half*>(c.hidden), c.hidden_stride, 0, 0, c.n} : Operand{parts.hidden, z.depth, z.tokens * z.depth, 0, c.n};
   g.n = c.n;
-  g.k_tiles = (uint32_t)(z.depth / kDepth);
+  g.k = (uint32_t)z.depth;
   g.slices = 1;
   set_pairs(g, P, P);
   uint32_t tile = 0;
@@ -979,7 +1022,7 @@ void grad_of(const Call& c, const Sizes& z, const GradParts& parts, const float2
     g.b = Operand{parts.hidden, z.depth, z.tokens * z.depth, (uint32_t)z.depth, (uint32_t)z.tokens};
     g.m = count;
     g.n = c.n;
-    g.k_tiles = (uint32_t)(z.depth / kDepth);
+    g.k = (uint32_t)z.depth;
     set_pairs(g, P, P);
     const Operand of_g{parts.g, z.piece, z.tokens * z.piece, (uint32_t)z.piece, (uint32_t)z.tokens};
     run<H, false, false>(g, GradEnd<H, PG>{c.who, (uint32_t)first, c.scale, stats, parts.factors, P > 1, parts.g, parts.rests, z.piece,
@@ -990,7 +1033,7 @@ void grad_of(const Call& c, const Sizes& z, const GradParts& parts, const float2
       y.b = of_g;
       y.m = c.dim;
       y.n = c.n;
-      y.k_tiles = (uint32_t)(pad_to(count, kDepth) / kDepth);
+      y.k = (uint32_t)pad_to(count, kDepth);
       y.slices = z.slices;
       set_pairs(y, P, P);   // 16-bit results: G's first plane alone
       run<H, true, false>(y, HiddenEnd{parts.sums, z.depth, c.n, first > 0}, stream);
@@ -1001,7 +1044,7 @@ void grad_of(const Call& c, const Sizes& z, const GradParts& parts, const float2
       t.b = of_g;
       t.m = c.dim;
       t.n = count;
-      t.k_tiles = (uint32_t)(z.tokens / kDepth);
+      t.k = (uint32_t)z.tokens;
       t.slices = 1;
       set_pairs(t, P, PG);
       run<H, true, true>(t, TableEnd<TO>{dtable + first * dtable_stride, dtable_stride, c.dim, count, accumulate, parts.factors, P > 1}, stream);
