@@ -39,12 +39,12 @@ constexpr float kLift = 0x1p13f;   // G's largest entries
 uint64_t pad_to(uint64_t x, uint64_t to) { return (x + to - 1) / to * to; }
 
 // ------------------------------------------------------------------------------ planes
-// x as a sum of P values of a 16-bit type.
+// x as a sum of P values of a 16-bit type.  Three cut bits off, which leaves the rest exact; one or two round.
 template <class H, uint32_t P>
 __device__ __forceinline__ void split(float x, Half (&out)[P]) {
 #pragma unroll
   for (uint32_t p = 0; p < P; ++p) {
-    const H h = (H)x;
+    const H h = P == 3 ? __builtin_bit_cast(H, (Half)(__float_as_uint(x) >> 16)) : (H)x;
     out[p] = __builtin_bit_cast(Half, h);
     x -= (float)h;
   }
@@ -163,14 +163,14 @@ __global__ __launch_bounds__(kPackBlock) void pack_kernel(PackArgs first, PackAr
   const uint32_t block = blockIdx.x < grid ? blockIdx.x : blockIdx.x - grid, blocks = blockIdx.x < grid ? grid : gridDim.x - grid;
   const uint32_t across = (uint32_t)(a.stride / 8);
   const uint64_t all = (uint64_t)a.rows_to * across;
-  const float up = P > 1 ? *a.up : 1.0f;
+  const float up = P == 2 ? *a.up : 1.0f;
   for (uint64_t k = (uint64_t)block * kPackBlock + threadIdx.x; k < all; k += (uint64_t)blocks * kPackBlock) {
     const uint32_t row = (uint32_t)(k / across), c = (uint32_t)(k % across) * 8;
     float x[8] = {};
     if (row < a.from.rows && !(a.masked && !who.live(row))) load_row<8>(static_cast<const T*>(a.from.p) + row * a.from.stride, c, a.cols, 0.0f, x);
     Half h[8][P];
 #pragma unroll
-    for (uint32_t i = 0; i < 8; ++i) split<H, P>(P > 1 ? x[i] * up : x[i], h[i]);
+    for (uint32_t i = 0; i < 8; ++i) split<H, P>(P == 2 ? x[i] * up : x[i], h[i]);
 #pragma unroll
     for (uint32_t p = 0; p < P; ++p) {
       Quad q;
@@ -680,10 +680,11 @@ struct GradEnd {
   }
 };
 
-// Rows are dh's columns, columns are tokens: fp32 sums, a matrix for every slice of K.
-struct HiddenEnd {
+// Rows are the result's columns, columns its rows (tokens for dh, the vocabulary's for dT): fp32 sums, a matrix for every slice
+// of K.
+struct SumsEnd {
   float* sums;
-  uint64_t stride;          // of a token; whole fours
+  uint64_t stride;          // of a row; whole fours
   uint32_t n, add;
 
   template <class S>
@@ -743,35 +744,199 @@ struct TableEnd {
   }
 };
 
-// dh: the slices added up, and what the rounding of the label's entry of G, its largest, has left.
-template <class T>
-__global__ __launch_bounds__(256) void hidden_kernel(Rows who, uint32_t dim, const float* sums, uint64_t stride, uint32_t slices,
-                                                     const Factors* factors, uint32_t scaled, const float* rests, Matrix table, T* out,
-                                                     uint64_t out_stride) {
-  const uint32_t blocks = (dim + 1023) / 1024;
+// The slices added up.  dh, of rows that count: and what the rounding of the label's entry of G, its largest, has left.
+struct JoinArgs {
+  uint32_t rows, dim;
+  const float* sums;
+  uint64_t stride;
+  uint32_t slices;
+  const Factors* factors;
+  uint32_t side;            // of Factors::down; 2: none
+  uint32_t of_hidden, add;
+  Rows who;
+  const float* rests;
+  Matrix table;
+  uint64_t out_stride;
+};
+template <class T, class TO>
+__global__ __launch_bounds__(256) void join_kernel(JoinArgs a, TO* out) {
+  const uint32_t blocks = (a.dim + 1023) / 1024;
   const uint32_t c = blockIdx.x % blocks * 1024 + threadIdx.x * 4;
-  if (c >= dim) return;
-  const float f = scaled ? factors->back * factors->down[1] : factors->back;
-  for (uint32_t i = blockIdx.x / blocks; i < who.n; i += gridDim.x / blocks) {
+  if (c >= a.dim) return;
+  const float f = a.side < 2 ? a.factors->back * a.factors->down[a.side] : a.factors->back;
+  for (uint32_t i = blockIdx.x / blocks; i < a.rows; i += gridDim.x / blocks) {
     float x[4] = {};
-    if (who.live(i)) {
-      for (uint32_t k = 0; k < slices; ++k) {
-        const Four p = *reinterpret_cast<const Four*>(sums + ((uint64_t)k * who.n + i) * stride + c);
+    if (!a.of_hidden || a.who.live(i)) {
+#pragma unroll 4
+      for (uint32_t k = 0; k < a.slices; ++k) {
+        const Four p = *reinterpret_cast<const Four*>(a.sums + ((uint64_t)k * a.rows + i) * a.stride + c);
 #pragma unroll
         for (uint32_t r = 0; r < 4; ++r) x[r] += p[r];
       }
-      if (rests) {
+      if (a.rests) {
         float t[4];
-        load_row<4>(static_cast<const T*>(table.p) + (uint64_t)who.label(i) * table.stride, c, dim, 0.0f, t);
+        load_row<4>(static_cast<const T*>(a.table.p) + (uint64_t)a.who.label(i) * a.table.stride, c, a.dim, 0.0f, t);
 #pragma unroll
-        for (uint32_t r = 0; r < 4; ++r) x[r] = fmaf(rests[i], t[r], x[r]);
+        for (uint32_t r = 0; r < 4; ++r) x[r] = fmaf(a.rests[i], t[r], x[r]);
       }
     }
+    float old[4] = {};
+    if (a.add) load_row<4>(out + i * a.out_stride, c, a.dim, 0.0f, old);
 #pragma unroll
-    for (uint32_t r = 0; r < 4; ++r) x[r] *= f;
-    store_row<4>(out + i * out_stride, c, dim, x);
+    for (uint32_t r = 0; r < 4; ++r) x[r] = fmaf(x[r], f, old[r]);
+    store_row<4>(out + i * a.out_stride, c, a.dim, x);
   }
 }
+
+// ------------------------------------------------------------------------------ few tokens
+// z of up to 16 NT tokens and 64 rows of the table, which are read as they lie in memory, once, straight into the registers of
+// the four wavefronts that share K out among them.  Bound by HBM where the vocabulary is large, by the latency of a fourth of K
+// where it is not; 24 x 2048 x 200 003 bf16 would take a launch before it, and half as long again, from LDS.  fp32 rows are cut
+// into three planes of bfloat16 (8 + 8 + 8 bits are its 24) on the way, of which the six largest products are added: no
+// row needs to be known before it is multiplied.
+constexpr uint32_t kFewRows = 64, kFewBlock = 256, kFewWaves = kFewBlock / kWave, kFewTokens = 64, kFewGap = 4;
+struct FewArgs {
+  Matrix table;
+  uint32_t dim;
+  const Half* hidden;       // planes of tokens, rows and K padded with zeros
+  uint64_t stride, plane;
+};
+
+template <class T>
+constexpr uint32_t kFewPlanes = sizeof(T) == 4 ? 3 : 1;
+
+// Eight values of a row as operands.
+template <class T>
+__device__ __forceinline__ void operands(const float (&x)[8], Quad (&q)[kFewPlanes<T>]) {
+  if constexpr (sizeof(T) == 4) {
+    float rest[8];
+#pragma unroll
+    for (uint32_t i = 0; i < 8; ++i) rest[i] = x[i];
+#pragma unroll
+    for (uint32_t p = 0; p < 3; ++p) {
+#pragma unroll
+      for (uint32_t i = 0; i < 4; ++i) {
+        const uint32_t low = __float_as_uint(rest[2 * i]), high = __float_as_uint(rest[2 * i + 1]);
+        q[p][i] = low >> 16 | (high & 0xFFFF0000u);
+        rest[2 * i] -= __uint_as_float(low & 0xFFFF0000u);
+        rest[2 * i + 1] -= __uint_as_float(high & 0xFFFF0000u);
+      }
+    }
+  } else {
+#pragma unroll
+    for (uint32_t i = 0; i < 4; ++i)
+      q[0][i] = (uint32_t)__builtin_bit_cast(Half, (T)x[2 * i]) | (uint32_t)__builtin_bit_cast(Half, (T)x[2 * i + 1]) << 16;
+  }
+}
+
+template <class T, uint32_t NT, class E>
+__global__ __launch_bounds__(kFewBlock) void few_kernel(FewArgs a, E epilogue) {
+  using H = std::conditional_t<std::is_same_v<T, f16_t>, f16_t, bf16_t>;
+  constexpr uint32_t P = kFewPlanes<T>, MT = kFewRows / 16, kWide = kFewRows + kFewGap;
+  __shared__ __attribute__((aligned(16))) float z[kFewWaves][NT * 16][kWide];
+  const uint32_t lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(wave_id()), first = blockIdx.x * kFewRows, part = (lane >> 4) * 8;
+  const T* rows[MT];
+#pragma unroll
+  for (uint32_t i = 0; i < MT; ++i) rows[i] = static_cast<const T*>(a.table.p) + min(first + i * 16 + (lane & 15), a.table.rows - 1) * a.table.stride;
+  const Half* tokens = a.hidden + (lane & 15) * a.stride;
+  Four acc[MT][NT];
+#pragma unroll
+  for (uint32_t i = 0; i < MT; ++i)
+#pragma unroll
+    for (uint32_t j = 0; j < NT; ++j) acc[i][j] = Four{0.0f, 0.0f, 0.0f, 0.0f};
+  auto step = [&](uint32_t k, auto whole) {
+    Quad b[NT][P];
+#pragma unroll
+    for (uint32_t j = 0; j < NT; ++j)
+#pragma unroll
+      for (uint32_t p = 0; p < P; ++p) b[j][p] = *reinterpret_cast<const Quad*>(tokens + p * a.plane + j * 16 * a.stride + k + part);
+#pragma unroll
+    for (uint32_t i = 0; i < MT; ++i) {
+      Quad q[P];
+      if constexpr (decltype(whole)::value && P == 1) {
+        q[0] = *reinterpret_cast<const UnalignedQuad*>(rows[i] + k + part);
+      } else {
+        float x[8];
+        if (decltype(whole)::value)
+          load_values<8>(rows[i] + k + part, x);
+        else
+          load_row<8>(rows[i], k + part, a.dim, 0.0f, x);
+        operands<T>(x, q);
+      }
+#pragma unroll
+      for (uint32_t order = P; order-- > 0;)
+#pragma unroll
+        for (uint32_t p = 0; p <= order; ++p)
+#pragma unroll
+          for (uint32_t j = 0; j < NT; ++j) acc[i][j] = mfma<H>(q[p], b[j][order - p], acc[i][j]);
+    }
+  };
+  const uint32_t whole = a.dim / kStep;
+  uint32_t t = wave;
+  for (; t + 3 * kFewWaves < whole; t += 4 * kFewWaves) {
+#pragma unroll
+    for (uint32_t u = 0; u < 4; ++u) step((t + u * kFewWaves) * kStep, std::true_type{});
+  }
+  for (; t < whole; t += kFewWaves) step(t * kStep, std::true_type{});
+  if (a.dim % kStep && whole % kFewWaves == wave) step(whole * kStep, std::false_type{});
+#pragma unroll
+  for (uint32_t i = 0; i < MT; ++i)
+#pragma unroll
+    for (uint32_t j = 0; j < NT; ++j) *reinterpret_cast<Four*>(&z[wave][j * 16 + (lane & 15)][i * 16 + (lane >> 4) * 4]) = acc[i][j];
+  __syncthreads();
+  // a wavefront has a token's 64 rows at a time
+  for (uint32_t token = wave; token < max(NT * 16, epilogue.tokens); token += kFewWaves) {
+    float sum = 0.0f;
+    if (token < NT * 16)
+#pragma unroll
+      for (uint32_t w = 0; w < kFewWaves; ++w) sum += z[w][token][lane];
+    epilogue(token, first + lane, sum);
+  }
+}
+
+struct FewStats {
+  Rows who;
+  float scale;
+  float2* partial;
+  float* answer;
+  uint32_t tokens;
+  __device__ __forceinline__ void operator()(uint32_t token, uint32_t v, float product) const {
+    if (token >= who.n) return;
+    const bool there = v < who.vocab;
+    const float x = product * scale, top = wave_max(there ? x : -INFINITY), sum = wave_sum(there ? exp_of(x - top) : 0.0f);
+    if (lane_id() == 0) partial[(uint64_t)blockIdx.x * who.n + token] = float2{top, sum};
+    if ((int64_t)v == who.label(token) && there) answer[token] = x;
+  }
+};
+
+template <class H, uint32_t P>
+struct FewGrad {
+  Rows who;
+  uint32_t first;
+  float scale;
+  const float2* stats;
+  const Factors* factors;
+  Half* g;
+  float* rests;
+  uint64_t stride, plane;
+  uint32_t tokens;          // with the rows of zeros up to whole tiles of K
+  __device__ __forceinline__ void operator()(uint32_t token, uint32_t row, float product) const {
+    const bool live = token < who.n && who.live(token);
+    float x = 0.0f;
+    const int64_t v = (int64_t)first + row;
+    if (live && v < (int64_t)who.vocab) {
+      const float2 st = stats[token];
+      const float w = who.weight(token) * scale * factors->grad;
+      x = exp_of(product * scale - st.x) * (w / st.y);
+      if (v == who.label(token)) x -= w;
+    }
+    Half out[P];
+    split<H, P>(x, out);
+    if (live && v == who.label(token)) rests[token] = x - (float)__builtin_bit_cast(H, out[0]);
+#pragma unroll
+    for (uint32_t p = 0; p < P; ++p) g[p * plane + token * stride + row] = out[p];
+  }
+};
 
 template <class TO>
 __global__ __launch_bounds__(256) void zero_rows_kernel(uint64_t rows, uint32_t dim, TO* out, uint64_t stride) {
@@ -782,7 +947,6 @@ __global__ __launch_bounds__(256) void zero_rows_kernel(uint64_t rows, uint32_t 
 // ------------------------------------------------------------------------------ host
 using Large = Shape<2, 4, 8, 4, 5>;   // 256 x 256, all of a CU's LDS: five operands' tiles
 using Small = Shape<2, 2, 4, 4, 5>;   // 128 x 128, half of it
-using Thin = Shape<4, 1, 4, 4, 4>;    // 256 x 64, half of it: few tokens
 
 template <class T>
 struct Kind {                      // how matrices of a type are multiplied
@@ -832,8 +996,26 @@ struct Sizes {
   uint32_t planes, g_planes, slices;
 };
 constexpr uint64_t kBudget = 320ull << 20;   // bytes of a piece's G and table, about; less would end dh's sums too often
-constexpr uint64_t kSlicesMost = 16, kSliceMin = 128;   // parts of a piece that dh's product is cut into, and tokens of each at least
-constexpr uint64_t kLaunchCost = 30000;                 // a launch's own time, about 10 us
+constexpr uint64_t kSliceMin = 128;          // K that a product's slice has, at least ...
+constexpr uint32_t kSlicesMost = 64;         // ... and slices, at most ...
+constexpr uint64_t kSumsMost = 64ull << 20;  // ... and bytes of dT's slices
+constexpr uint64_t kLaunchCost = 30000;      // a launch's own time, about 10 us
+
+// Into how many slices K of a product is cut, and what it costs then.  A slice's results are written and read again, 8 bytes
+// a value at 5 TB/s, and added up in turn.
+struct Slices {
+  uint32_t count;
+  uint64_t cost;
+};
+Slices slices_for(uint64_t m, uint64_t n, uint64_t k, uint64_t products, uint64_t most) {
+  Slices best{1, cost(m, n, 1) * k * products};
+  for (uint32_t s = 2; s <= std::min<uint64_t>(kSlicesMost, most) && k / s >= kSliceMin; s *= 2) {
+    const uint64_t c = cost(m, n, s) * ((k + s - 1) / s) * products + s * (m * n / 200 + 300) + kLaunchCost / 2;
+    if (c < best.cost) best = Slices{s, c};
+  }
+  return best;
+}
+
 Sizes sizes_for(uint32_t n, uint32_t vocab, uint32_t dim, uint32_t type, uint32_t dtable_type, bool grad) {
   Sizes z{};
   z.depth = pad_to(dim, kDepth);
@@ -845,22 +1027,16 @@ Sizes sizes_for(uint32_t n, uint32_t vocab, uint32_t dim, uint32_t type, uint32_
   const uint64_t whole = pad_to(vocab, kPadTo) / kPadTo, most = std::min(whole, std::max<uint64_t>(1, kBudget / each / kPadTo));
   z.piece = most * kPadTo;
   if (!grad) return z;
-  // A launch lasts as long as its fullest CU: of the pieces' sizes the one whose launches take least together.  A slice of dh's
-  // product is written and read again, 8 bytes a value at 5 TB/s.
+  // A launch lasts as long as its fullest CU: of the pieces' sizes the one whose launches take least together.
+  const uint64_t of_z = z.planes == 1 ? 1 : 3, of_g = z.planes == 1 ? z.g_planes : 3;
   auto of_piece = [&](uint64_t t, uint32_t* slices) {
     const uint64_t rows = t * kPadTo;
-    uint64_t best = ~0ull;
-    for (uint64_t s = 1; s <= kSlicesMost && (s == 1 || rows / s >= kSliceMin); ++s) {
-      const uint64_t c = cost(dim, n, s) * (rows / s) * (z.planes == 1 ? 1 : 3) + s * n * (uint64_t)dim / 200;
-      if (c < best) {
-        best = c;
-        *slices = (uint32_t)s;
-      }
-    }
-    return best + cost(rows, n, 1) * z.depth * (z.planes == 1 ? 1 : 3) + cost(dim, rows, 1) * z.tokens * (z.planes == 1 ? z.g_planes : 3) + 3 * kLaunchCost;
+    const Slices h = slices_for(dim, n, rows, of_z, kSlicesMost);
+    *slices = h.count;
+    return h.cost + cost(rows, n, 1) * z.depth * of_z + slices_for(dim, rows, z.tokens, of_g, kSumsMost / (rows * z.depth * 4)).cost + 3 * kLaunchCost;
   };
   uint64_t best = ~0ull;
-  const uint64_t step = std::max<uint64_t>(1, most / 128);
+  const uint64_t step = std::max<uint64_t>(1, most / 32);
   for (uint64_t t = most; t >= std::max<uint64_t>(1, most / 2); t -= std::min(step, t)) {
     uint32_t slices = 1, other;
     const uint64_t rest = whole % t, c = of_piece(t, &slices) * (whole / t) + (rest ? of_piece(rest, &other) : 0);
@@ -906,31 +1082,33 @@ bool as_it_is(const void* p, uint64_t stride, uint32_t dim, uint32_t type) {
 struct Parts {
   Factors* factors;
   float* tops;
-  Half *hidden, *table;
-  explicit Parts(Room& r, const Sizes& z) {
+  Half *hidden, *table, *few;   // few: hidden rows beside a table that is read as it is
+  Parts(Room& r, const Sizes& z, uint32_t n) {
     factors = r.take<Factors>(1);
     tops = r.take<float>(z.planes > 1 ? 2 * kSurveyGrid : 0);
     hidden = r.take<Half>(z.planes * z.tokens * z.depth);
     table = r.take<Half>(z.planes * z.piece * z.depth);
+    few = r.take<Half>(n <= kFewTokens ? 3 * kFewTokens * z.depth : 0);
   }
 };
 struct LossParts : Parts {
   float2* partial;
   float* answer;
   uint64_t bytes;
-  LossParts(Room r, const Sizes& z, uint32_t n, uint32_t vocab) : Parts(r, z) {
-    partial = r.take<float2>((vocab / 128 + vocab / z.piece + 2) * n);
+  LossParts(Room r, const Sizes& z, uint32_t n, uint32_t vocab) : Parts(r, z, n) {
+    partial = r.take<float2>((vocab / (n <= kFewTokens ? kFewRows : Small::TM) + vocab / z.piece + 2) * n);
     answer = r.take<float>(n);
     bytes = r.used;
   }
 };
 struct GradParts : Parts {
   Half* g;
-  float *sums, *rests;
+  float *sums, *table_sums, *rests;
   uint64_t bytes;
-  GradParts(Room r, const Sizes& z, uint32_t n) : Parts(r, z) {
+  GradParts(Room r, const Sizes& z, uint32_t n) : Parts(r, z, n) {
     g = r.take<Half>(z.g_planes * z.tokens * z.piece);
     sums = r.take<float>(z.slices * n * z.depth);
+    table_sums = r.take<float>(std::min(kSumsMost / 4, kSlicesMost * z.piece * z.depth));
     rests = r.take<float>(n);
     bytes = r.used;
   }
@@ -951,51 +1129,65 @@ void find_factors(const Call& c, const Sizes& z, const Parts& parts, uint32_t* s
   }
 }
 
-template <class T>
+template <class T, class H = typename Kind<T>::H, uint32_t P = Kind<T>::P>
 void pack(const Call& c, const PackArgs& first, const PackArgs& second, hipStream_t stream) {
   auto grid = [](const PackArgs& a) {
     return (uint32_t)std::min<uint64_t>(((uint64_t)a.rows_to * (a.stride / 8) + kPackBlock - 1) / kPackBlock, 1u << 16);
   };
   const uint32_t one = grid(first), two = grid(second);
   if (one + two)
-    hipLaunchKernelGGL((pack_kernel<T, typename Kind<T>::H, Kind<T>::P>), dim3(one + two), dim3(kPackBlock), 0, stream, first, second, one, c.who);
+    hipLaunchKernelGGL((pack_kernel<T, H, P>), dim3(one + two), dim3(kPackBlock), 0, stream, first, second, one, c.who);
+}
+
+// z of few tokens, from the table's rows [first, first + rows) as they are; the tokens' planes are made with the first.
+template <class T, class E>
+void run_few(const Call& c, const Sizes& z, const Parts& parts, uint64_t first, uint32_t rows, const E& end, hipStream_t stream) {
+  constexpr uint32_t P = kFewPlanes<T>;
+  using H = std::conditional_t<std::is_same_v<T, f16_t>, f16_t, bf16_t>;
+  const uint64_t plane = kFewTokens * z.depth;
+  if (first == 0) pack<T, H, P>(c, PackArgs{c.hidden_matrix(), c.dim, kFewTokens, parts.few, z.depth, plane, nullptr, 1}, PackArgs{}, stream);
+  const FewArgs a{c.table_matrix(first, rows), c.dim, parts.few, z.depth, plane};
+  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((rows + kFewRows - 1) / kFewRows), dim3(kFewBlock), 0, stream, a, end); };
+  if (c.n <= 16)
+    go(few_kernel<T, 1, E>);
+  else if (c.n <= 32)
+    go(few_kernel<T, 2, E>);
+  else
+    go(few_kernel<T, 4, E>);
 }
 
 template <class T>
 void loss_of(const Call& c, const Sizes& z, const LossParts& parts, float* loss, float2* stats, uint32_t* status, hipStream_t stream) {
   using H = typename Kind<T>::H;
   constexpr uint32_t P = Kind<T>::P;
-  const bool hidden_goes = as_it_is(c.hidden, c.hidden_stride, c.dim, c.type), table_goes = as_it_is(c.table, c.table_stride, c.dim, c.type);
-  if (P > 1) find_factors(c, z, parts, nullptr, stream);
-  PackArgs hidden{c.hidden_matrix(), c.dim, c.n, parts.hidden, z.depth, z.tokens * z.depth, parts.factors->up, 0};
-  if (hidden_goes) hidden.rows_to = 0;
-  Product g{};
-  g.b = hidden_goes ? Operand{static_cast<const Half*>(c.hidden), c.hidden_stride, 0, 0, c.n} : Operand{parts.hidden, z.depth, z.tokens * z.depth, 0, c.n};
-  g.n = c.n;
-  g.k = (uint32_t)z.depth;
-  g.slices = 1;
-  set_pairs(g, P, P);
   uint32_t tile = 0;
-  const uint64_t step = table_goes ? pad_to(c.vocab, kPadTo) : z.piece;
-  for (uint64_t first = 0; first < c.vocab; first += step) {
-    g.m = (uint32_t)std::min<uint64_t>(step, c.vocab - first);
-    PackArgs table{c.table_matrix(first, g.m), c.dim, table_goes ? 0 : g.m, parts.table, z.depth, z.piece * z.depth, parts.factors->up + 1, 0};
-    pack<T>(c, hidden, table, stream);
-    hidden.rows_to = 0;
-    g.a = table_goes ? Operand{static_cast<const Half*>(c.table) + first * c.table_stride, c.table_stride, 0, 0, g.m}
-                     : Operand{parts.table, z.depth, z.piece * z.depth, 0, g.m};
-    const StatsEnd end{c.who, (uint32_t)first, tile, c.scale, P > 1 ? parts.factors : nullptr, parts.partial, parts.answer};
-    auto go = [&](auto shape) {
-      using S = decltype(shape);
-      run_as<H, false, false, S>(g, end, stream);
-      tile += (g.m + S::TM - 1) / S::TM;
-    };
-    if (c.n <= Thin::TN)
-      go(Thin{});
-    else if (large_goes(g))
-      go(Large{});
-    else
-      go(Small{});
+  if (c.n <= kFewTokens) {
+    run_few<T>(c, z, parts, 0, c.vocab, FewStats{c.who, c.scale, parts.partial, parts.answer, 0}, stream);
+    tile = (c.vocab + kFewRows - 1) / kFewRows;
+  } else {
+    const bool hidden_goes = as_it_is(c.hidden, c.hidden_stride, c.dim, c.type), table_goes = as_it_is(c.table, c.table_stride, c.dim, c.type);
+    if (P > 1) find_factors(c, z, parts, nullptr, stream);
+    PackArgs hidden{c.hidden_matrix(), c.dim, c.n, parts.hidden, z.depth, z.tokens * z.depth, parts.factors->up, 0};
+    if (hidden_goes) hidden.rows_to = 0;
+    Product g{};
+    g.b = hidden_goes ? Operand{static_cast<const Half*>(c.hidden), c.hidden_stride, 0, 0, c.n} : Operand{parts.hidden, z.depth, z.tokens * z.depth, 0, c.n};
+    g.n = c.n;
+    g.k = (uint32_t)z.depth;
+    g.slices = 1;
+    set_pairs(g, P, P);
+    const uint64_t step = table_goes ? pad_to(c.vocab, kPadTo) : z.piece;
+    for (uint64_t first = 0; first < c.vocab; first += step) {
+      g.m = (uint32_t)std::min<uint64_t>(step, c.vocab - first);
+      PackArgs table{c.table_matrix(first, g.m), c.dim, table_goes ? 0 : g.m, parts.table, z.depth, z.piece * z.depth, parts.factors->up + 1, 0};
+      pack<T>(c, hidden, table, stream);
+      hidden.rows_to = 0;
+      g.a = table_goes ? Operand{static_cast<const Half*>(c.table) + first * c.table_stride, c.table_stride, 0, 0, g.m}
+                       : Operand{parts.table, z.depth, z.piece * z.depth, 0, g.m};
+      const StatsEnd end{c.who, (uint32_t)first, tile, c.scale, P > 1 ? parts.factors : nullptr, parts.partial, parts.answer};
+      run<H, false, false>(g, end, stream);
+      const uint32_t rows = large_goes(g) ? Large::TM : Small::TM;
+      tile += (g.m + rows - 1) / rows;
+    }
   }
   const uint32_t log2 = join_tokens_log2(c.n);
   hipLaunchKernelGGL(loss_kernel, dim3((c.n + (1u << log2) - 1) >> log2), dim3(kJoinBlock), 0, stream, c.who, tile, log2, parts.partial,
@@ -1003,16 +1195,23 @@ void loss_of(const Call& c, const Sizes& z, const LossParts& parts, float* loss,
 }
 
 template <class T, class TO>
+void join(const JoinArgs& a, TO* out, hipStream_t stream) {
+  const uint32_t blocks = (a.dim + 1023) / 1024;
+  hipLaunchKernelGGL((join_kernel<T, TO>), dim3(std::min(a.rows, std::max(1u, 8192u / blocks)) * blocks), dim3(256), 0, stream, a, out);
+}
+
+template <class T, class TO>
 void grad_of(const Call& c, const Sizes& z, const GradParts& parts, const float2* stats, T* dhidden, uint64_t dhidden_stride, TO* dtable,
              uint64_t dtable_stride, bool accumulate, uint32_t* status, hipStream_t stream) {
   using H = typename Kind<T>::H;
   constexpr uint32_t P = Kind<T>::P, PG = sizeof(TO) == 4 ? 2 : 1;
-  const bool table_goes = as_it_is(c.table, c.table_stride, c.dim, c.type);
+  const bool table_goes = as_it_is(c.table, c.table_stride, c.dim, c.type), few = c.n <= kFewTokens;
   find_factors(c, z, parts, status, stream);
   PackArgs hidden{c.hidden_matrix(), c.dim, (uint32_t)z.tokens, parts.hidden, z.depth, z.tokens * z.depth, parts.factors->up, 1};
   for (uint64_t first = 0; first < c.vocab; first += z.piece) {
     const uint32_t count = (uint32_t)std::min<uint64_t>(z.piece, c.vocab - first);
-    PackArgs table{c.table_matrix(first, count), c.dim, table_goes ? 0 : count, parts.table, z.depth, z.piece * z.depth, parts.factors->up + 1, 0};
+    PackArgs table{c.table_matrix(first, count), c.dim, table_goes || (few && !dhidden) ? 0 : count, parts.table, z.depth, z.piece * z.depth,
+                   parts.factors->up + 1, 0};
     pack<T>(c, hidden, table, stream);
     hidden.rows_to = 0;
     Product g{};
@@ -1025,8 +1224,12 @@ void grad_of(const Call& c, const Sizes& z, const GradParts& parts, const float2
     g.k = (uint32_t)z.depth;
     set_pairs(g, P, P);
     const Operand of_g{parts.g, z.piece, z.tokens * z.piece, (uint32_t)z.piece, (uint32_t)z.tokens};
-    run<H, false, false>(g, GradEnd<H, PG>{c.who, (uint32_t)first, c.scale, stats, parts.factors, P > 1, parts.g, parts.rests, z.piece,
-                                           z.tokens * z.piece, z.tokens}, stream);
+    if (few)
+      run_few<T>(c, z, parts, first, count, FewGrad<H, PG>{c.who, (uint32_t)first, c.scale, stats, parts.factors, parts.g, parts.rests, z.piece,
+                                                           z.tokens * z.piece, (uint32_t)z.tokens}, stream);
+    else
+      run<H, false, false>(g, GradEnd<H, PG>{c.who, (uint32_t)first, c.scale, stats, parts.factors, P > 1, parts.g, parts.rests, z.piece,
+                                             z.tokens * z.piece, z.tokens}, stream);
     if (dhidden) {
       Product y{};
       y.a = g.a;
@@ -1036,7 +1239,7 @@ void grad_of(const Call& c, const Sizes& z, const GradParts& parts, const float2
       y.k = (uint32_t)pad_to(count, kDepth);
       y.slices = z.slices;
       set_pairs(y, P, P);   // 16-bit results: G's first plane alone
-      run<H, true, false>(y, HiddenEnd{parts.sums, z.depth, c.n, first > 0}, stream);
+      run<H, true, false>(y, SumsEnd{parts.sums, z.depth, c.n, first > 0}, stream);
     }
     if (dtable) {
       Product t{};
@@ -1045,16 +1248,21 @@ void grad_of(const Call& c, const Sizes& z, const GradParts& parts, const float2
       t.m = c.dim;
       t.n = count;
       t.k = (uint32_t)z.tokens;
-      t.slices = 1;
       set_pairs(t, P, PG);
-      run<H, true, true>(t, TableEnd<TO>{dtable + first * dtable_stride, dtable_stride, c.dim, count, accumulate, parts.factors, P > 1}, stream);
+      t.slices = slices_for(c.dim, count, z.tokens, t.pairs, kSumsMost / (count * z.depth * 4)).count;
+      TO* out = dtable + first * dtable_stride;
+      if (t.slices == 1) {
+        run<H, true, true>(t, TableEnd<TO>{out, dtable_stride, c.dim, count, accumulate, parts.factors, P > 1}, stream);
+      } else {
+        run<H, true, true>(t, SumsEnd{parts.table_sums, z.depth, count, 0}, stream);
+        join<T>(JoinArgs{count, c.dim, parts.table_sums, z.depth, t.slices, parts.factors, P > 1 ? 0u : 2u, 0, accumulate, c.who, nullptr, Matrix{},
+                         dtable_stride}, out, stream);
+      }
     }
   }
-  if (dhidden) {
-    const uint32_t blocks = (c.dim + 1023) / 1024;
-    hipLaunchKernelGGL(hidden_kernel<T>, dim3(std::min(c.n, std::max(1u, 8192u / blocks)) * blocks), dim3(256), 0, stream, c.who, c.dim, parts.sums,
-                       z.depth, z.slices, parts.factors, P > 1, P == 1 ? parts.rests : nullptr, c.table_matrix(0, c.vocab), dhidden, dhidden_stride);
-  }
+  if (dhidden)
+    join<T>(JoinArgs{c.n, c.dim, parts.sums, z.depth, z.slices, parts.factors, P > 1 ? 1u : 2u, 1, 0, c.who, P == 1 ? parts.rests : nullptr,
+                     c.table_matrix(0, c.vocab), dhidden_stride}, dhidden, stream);
 }
 
 constexpr uint32_t kMostRows = 1u << 22;   // offsets inside a tile of tokens' columns have 32 bits
