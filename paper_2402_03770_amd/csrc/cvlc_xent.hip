@@ -794,7 +794,9 @@ __global__ __launch_bounds__(256) void join_kernel(JoinArgs a, TO* out) {
 // where it is not; 24 x 2048 x 200 003 bf16 would take a launch before it, and half as long again, from LDS.  fp32 rows are cut
 // into three planes of bfloat16 (8 + 8 + 8 bits are its 24) on the way, of which the six largest products are added: no
 // row needs to be known before it is multiplied.
-constexpr uint32_t kFewRows = 64, kFewBlock = 256, kFewWaves = kFewBlock / kWave, kFewTokens = 64, kFewGap = 4;
+constexpr uint32_t kFewRows = 64, kFewTokens = 64, kFewGap = 4;
+template <uint32_t NT>
+constexpr uint32_t kFewWaves = NT == 4 ? 4 : 8;
 struct FewArgs {
   Matrix table;
   uint32_t dim;
@@ -830,10 +832,10 @@ __device__ __forceinline__ void operands(const float (&x)[8], Quad (&q)[kFewPlan
 }
 
 template <class T, uint32_t NT, class E>
-__global__ __launch_bounds__(kFewBlock) void few_kernel(FewArgs a, E epilogue) {
+__global__ __launch_bounds__(kFewWaves<NT>* kWave) void few_kernel(FewArgs a, E epilogue) {
   using H = std::conditional_t<std::is_same_v<T, f16_t>, f16_t, bf16_t>;
-  constexpr uint32_t P = kFewPlanes<T>, MT = kFewRows / 16, kWide = kFewRows + kFewGap;
-  __shared__ __attribute__((aligned(16))) float z[kFewWaves][NT * 16][kWide];
+  constexpr uint32_t P = kFewPlanes<T>, MT = kFewRows / 16, kWide = kFewRows + kFewGap, kWaves = kFewWaves<NT>;
+  __shared__ __attribute__((aligned(16))) float z[kWaves][NT * 16][kWide];
   const uint32_t lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(wave_id()), first = blockIdx.x * kFewRows, part = (lane >> 4) * 8;
   const T* rows[MT];
 #pragma unroll
@@ -844,52 +846,75 @@ __global__ __launch_bounds__(kFewBlock) void few_kernel(FewArgs a, E epilogue) {
   for (uint32_t i = 0; i < MT; ++i)
 #pragma unroll
     for (uint32_t j = 0; j < NT; ++j) acc[i][j] = Four{0.0f, 0.0f, 0.0f, 0.0f};
-  auto step = [&](uint32_t k, auto whole) {
-    Quad b[NT][P];
+  auto add = [&](uint32_t i, const Quad (&q)[P], const Quad (&b)[NT][P]) {
+#pragma unroll
+    for (uint32_t order = P; order-- > 0;)
+#pragma unroll
+      for (uint32_t p = 0; p <= order; ++p)
+#pragma unroll
+        for (uint32_t j = 0; j < NT; ++j) acc[i][j] = mfma<H>(q[p], b[j][order - p], acc[i][j]);
+  };
+  auto take = [&](uint32_t k, Quad (&b)[NT][P]) {
 #pragma unroll
     for (uint32_t j = 0; j < NT; ++j)
 #pragma unroll
       for (uint32_t p = 0; p < P; ++p) b[j][p] = *reinterpret_cast<const Quad*>(tokens + p * a.plane + j * 16 * a.stride + k + part);
-#pragma unroll
-    for (uint32_t i = 0; i < MT; ++i) {
-      Quad q[P];
-      if constexpr (decltype(whole)::value && P == 1) {
-        q[0] = *reinterpret_cast<const UnalignedQuad*>(rows[i] + k + part);
-      } else {
-        float x[8];
-        if (decltype(whole)::value)
-          load_values<8>(rows[i] + k + part, x);
-        else
-          load_row<8>(rows[i], k + part, a.dim, 0.0f, x);
-        operands<T>(x, q);
-      }
-#pragma unroll
-      for (uint32_t order = P; order-- > 0;)
-#pragma unroll
-        for (uint32_t p = 0; p <= order; ++p)
-#pragma unroll
-          for (uint32_t j = 0; j < NT; ++j) acc[i][j] = mfma<H>(q[p], b[j][order - p], acc[i][j]);
-    }
   };
-  const uint32_t whole = a.dim / kStep;
-  uint32_t t = wave;
-  for (; t + 3 * kFewWaves < whole; t += 4 * kFewWaves) {
+  constexpr uint32_t kLine = 128 / sizeof(T), kSteps = kLine / kStep, kQuads = sizeof(T) / 2;
+  const uint32_t lines = a.dim / kLine;
+  for (uint32_t l = wave; l < lines; l += kWaves) {
+    Quad raw[kSteps][MT][kQuads], b[kSteps][NT][P];
 #pragma unroll
-    for (uint32_t u = 0; u < 4; ++u) step((t + u * kFewWaves) * kStep, std::true_type{});
+    for (uint32_t s = 0; s < kSteps; ++s) {
+      const uint32_t k = l * kLine + s * kStep;
+#pragma unroll
+      for (uint32_t i = 0; i < MT; ++i)
+#pragma unroll
+        for (uint32_t c = 0; c < kQuads; ++c) raw[s][i][c] = *reinterpret_cast<const UnalignedQuad*>(rows[i] + k + part + c * 16 / sizeof(T));
+      take(k, b[s]);
+    }
+    // all of them on their way before the first is waited for: left to itself the compiler asks for each where it is used
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (uint32_t s = 0; s < kSteps; ++s)
+#pragma unroll
+      for (uint32_t i = 0; i < MT; ++i) {
+        if constexpr (P == 1) {
+          add(i, raw[s][i], b[s]);
+        } else {
+          float x[8];
+          Quad q[P];
+#pragma unroll
+          for (uint32_t c = 0; c < 8; ++c) x[c] = __uint_as_float(raw[s][i][c / 4][c % 4]);
+          operands<T>(x, q);
+          add(i, q, b[s]);
+        }
+      }
   }
-  for (; t < whole; t += kFewWaves) step(t * kStep, std::true_type{});
-  if (a.dim % kStep && whole % kFewWaves == wave) step(whole * kStep, std::false_type{});
+  if (wave == lines % kWaves)
+    for (uint32_t k = lines * kLine; k < a.dim; k += kStep) {
+      Quad b[NT][P];
+      take(k, b);
+#pragma unroll
+      for (uint32_t i = 0; i < MT; ++i) {
+        float x[8];
+        Quad q[P];
+        load_row<8>(rows[i], k + part, a.dim, 0.0f, x);
+        operands<T>(x, q);
+        add(i, q, b);
+      }
+    }
 #pragma unroll
   for (uint32_t i = 0; i < MT; ++i)
 #pragma unroll
     for (uint32_t j = 0; j < NT; ++j) *reinterpret_cast<Four*>(&z[wave][j * 16 + (lane & 15)][i * 16 + (lane >> 4) * 4]) = acc[i][j];
   __syncthreads();
   // a wavefront has a token's 64 rows at a time
-  for (uint32_t token = wave; token < max(NT * 16, epilogue.tokens); token += kFewWaves) {
+  for (uint32_t token = wave; token < max(NT * 16, epilogue.tokens); token += kWaves) {
     float sum = 0.0f;
     if (token < NT * 16)
 #pragma unroll
-      for (uint32_t w = 0; w < kFewWaves; ++w) sum += z[w][token][lane];
+      for (uint32_t w = 0; w < kFewWaves<NT>; ++w) sum += z[w][token][lane];
     epilogue(token, first + lane, sum);
   }
 }
@@ -1147,13 +1172,17 @@ void run_few(const Call& c, const Sizes& z, const Parts& parts, uint64_t first, 
   const uint64_t plane = kFewTokens * z.depth;
   if (first == 0) pack<T, H, P>(c, PackArgs{c.hidden_matrix(), c.dim, kFewTokens, parts.few, z.depth, plane, nullptr, 1}, PackArgs{}, stream);
   const FewArgs a{c.table_matrix(first, rows), c.dim, parts.few, z.depth, plane};
-  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((rows + kFewRows - 1) / kFewRows), dim3(kFewBlock), 0, stream, a, end); };
+  auto go = [&](auto tokens) {
+    constexpr uint32_t NT = decltype(tokens)::value;
+    hipLaunchKernelGGL((few_kernel<T, NT, E>), dim3((rows + kFewRows - 1) / kFewRows),
+                       dim3(kFewWaves<NT> * kWave), 0, stream, a, end);
+  };
   if (c.n <= 16)
-    go(few_kernel<T, 1, E>);
+    go(std::integral_constant<uint32_t, 1>{});
   else if (c.n <= 32)
-    go(few_kernel<T, 2, E>);
+    go(std::integral_constant<uint32_t, 2>{});
   else
-    go(few_kernel<T, 4, E>);
+    go(std::integral_constant<uint32_t, 4>{});
 }
 
 template <class T>
