@@ -1023,7 +1023,8 @@ struct Sizes {
 constexpr uint64_t kBudget = 320ull << 20;   // bytes of a piece's G and table, about; less would end dh's sums too often
 constexpr uint64_t kSliceMin = 128;          // K that a product's slice has, at least ...
 constexpr uint32_t kSlicesMost = 64;         // ... and slices, at most ...
-constexpr uint64_t kSumsMost = 64ull << 20;  // ... and bytes of dT's slices
+constexpr uint64_t kSumsMost = 64ull << 20;  // ... and bytes of dT's slices; of which there is one where it has more small tiles than
+constexpr uint64_t kTilesFew = kCus / 2;     // this: 2048 x 768 x 32 000 fp32 takes 1190 us so, 1310 with slices of a last piece's dT
 constexpr uint64_t kLaunchCost = 30000;      // a launch's own time, about 10 us
 
 // Into how many slices K of a product is cut, and what it costs then.  A slice's results are written and read again, 8 bytes
@@ -1034,13 +1035,20 @@ struct Slices {
 };
 Slices slices_for(uint64_t m, uint64_t n, uint64_t k, uint64_t products, uint64_t most) {
   Slices best{1, cost(m, n, 1) * k * products};
-  for (uint32_t s = 2; s <= std::min<uint64_t>(kSlicesMost, most) && k / s >= kSliceMin; s *= 2) {
+  const uint64_t large = tiles(m, n, Large::TM, Large::TN), small = tiles(m, n, Small::TM, Small::TN);
+  // as many as fill the CUs one to three times over with large tiles, or half, once and twice with small ones
+  for (uint64_t s : {kCus / large, 2 * kCus / large, 3 * kCus / large, kCus / small, 2 * kCus / small, 4 * kCus / small}) {
+    s = std::min({s, (uint64_t)kSlicesMost, most, k / kSliceMin});
+    if (s < 2) continue;
     const uint64_t c = cost(m, n, s) * ((k + s - 1) / s) * products + s * (m * n / 200 + 300) + kLaunchCost / 2;
-    if (c < best.cost) best = Slices{s, c};
+    if (c < best.cost) best = Slices{(uint32_t)s, c};
   }
   return best;
 }
-
+Slices table_slices(uint64_t rows, uint64_t dim, uint64_t depth, uint64_t tokens, uint64_t products) {
+  const bool few = tiles(dim, rows, Small::TM, Small::TN) <= kTilesFew;
+  return slices_for(dim, rows, tokens, products, few ? kSumsMost / (rows * depth * 4) : 1);
+}
 Sizes sizes_for(uint32_t n, uint32_t vocab, uint32_t dim, uint32_t type, uint32_t dtable_type, bool grad) {
   Sizes z{};
   z.depth = pad_to(dim, kDepth);
@@ -1058,10 +1066,10 @@ Sizes sizes_for(uint32_t n, uint32_t vocab, uint32_t dim, uint32_t type, uint32_
     const uint64_t rows = t * kPadTo;
     const Slices h = slices_for(dim, n, rows, of_z, kSlicesMost);
     *slices = h.count;
-    return h.cost + cost(rows, n, 1) * z.depth * of_z + slices_for(dim, rows, z.tokens, of_g, kSumsMost / (rows * z.depth * 4)).cost + 3 * kLaunchCost;
+    return h.cost + cost(rows, n, 1) * z.depth * of_z + table_slices(rows, dim, z.depth, z.tokens, of_g).cost + 3 * kLaunchCost;
   };
   uint64_t best = ~0ull;
-  const uint64_t step = std::max<uint64_t>(1, most / 32);
+  const uint64_t step = std::max<uint64_t>(1, most / 64);
   for (uint64_t t = most; t >= std::max<uint64_t>(1, most / 2); t -= std::min(step, t)) {
     uint32_t slices = 1, other;
     const uint64_t rest = whole % t, c = of_piece(t, &slices) * (whole / t) + (rest ? of_piece(rest, &other) : 0);
@@ -1278,7 +1286,7 @@ void grad_of(const Call& c, const Sizes& z, const GradParts& parts, const float2
       t.n = count;
       t.k = (uint32_t)z.tokens;
       set_pairs(t, P, PG);
-      t.slices = slices_for(c.dim, count, z.tokens, t.pairs, kSumsMost / (count * z.depth * 4)).count;
+      t.slices = table_slices(count, c.dim, z.depth, z.tokens, t.pairs).count;
       TO* out = dtable + first * dtable_stride;
       if (t.slices == 1) {
         run<H, true, true>(t, TableEnd<TO>{out, dtable_stride, c.dim, count, accumulate, parts.factors, P > 1}, stream);
@@ -1309,8 +1317,8 @@ int check(const Call& c, const float* d_stats, const void* d_workspace, const ui
   if (c.who.weights && !buffer_ok(c.who.weights, 4)) return CVLC_ERR_ARG;
   if (d_stats && !buffer_ok(d_stats, 8)) return CVLC_ERR_ARG;
   // tiles of a launch, and threads of one: fewer than 2^32
-  const uint64_t tiles = ((uint64_t)c.n / 32 + 1) * (pad_to(c.vocab, kPadTo) / 128), packs = ((uint64_t)std::max(c.n, c.vocab) / 64 + 1) * (c.dim / 64 + 1);
-  if (tiles >= 1ull << 23 || packs >= 1ull << 24) return CVLC_ERR_ARG;
+  const uint64_t tiles = ((uint64_t)c.n / 128 + 1) * (pad_to(c.vocab, kPadTo) / 128), packs = ((uint64_t)std::max(c.n, c.vocab) / 64 + 1) * (c.dim / 64 + 1);
+  if (tiles >= 1ull << 23 || packs >= 1ull << 24 || (c.n <= kFewTokens && c.vocab / kFewRows >= 1u << 22)) return CVLC_ERR_ARG;
   return CVLC_OK;
 }
 
