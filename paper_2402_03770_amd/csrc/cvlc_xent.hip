@@ -789,14 +789,16 @@ __global__ __launch_bounds__(256) void join_kernel(JoinArgs a, TO* out) {
 }
 
 // ------------------------------------------------------------------------------ few tokens
-// z of up to 16 NT tokens and 64 rows of the table, which are read as they lie in memory, once, straight into the registers of
-// the four wavefronts that share K out among them.  Bound by HBM where the vocabulary is large, by the latency of a fourth of K
-// where it is not; 24 x 2048 x 200 003 bf16 would take a launch before it, and half as long again, from LDS.  fp32 rows are cut
-// into three planes of bfloat16 (8 + 8 + 8 bits are its 24) on the way, of which the six largest products are added: no
-// row needs to be known before it is multiplied.
+// z of up to 16 NT tokens and 64 rows of the table, which are read as they lie in memory, whatever their stride and alignment,
+// once, straight into registers.  Bound by HBM: 24 x 2048 x 200 003 bf16 takes 166 us (4.95 TB/s), where tiles of 256 rows through
+// LDS took 181 and wanted an aligned table.  For that a wavefront asks for 64 lines of 128 bytes, and the tokens' part, before it
+// waits for the first, and eight share K out among them line by line (four 176 us, two 214, sixteen 198; loads past the caches'
+// order 194).  Where the vocabulary is small it is K that takes the time, an eighth of it here: 4 x 4096 x 1472 15 us, which
+// a workgroup to a tile and all of K takes 57 for.  fp32 rows are cut into three planes of bfloat16 on the way, which hold
+// 8 + 8 + 8 bits, all there are, so that no row needs to be known before it is multiplied.
 constexpr uint32_t kFewRows = 64, kFewTokens = 64, kFewGap = 4;
 template <uint32_t NT>
-constexpr uint32_t kFewWaves = NT == 4 ? 4 : 8;
+constexpr uint32_t kFewWaves = NT == 4 ? 4 : 8;                  // what LDS has room for
 struct FewArgs {
   Matrix table;
   uint32_t dim;
@@ -848,9 +850,9 @@ __global__ __launch_bounds__(kFewWaves<NT>* kWave) void few_kernel(FewArgs a, E 
     for (uint32_t j = 0; j < NT; ++j) acc[i][j] = Four{0.0f, 0.0f, 0.0f, 0.0f};
   auto add = [&](uint32_t i, const Quad (&q)[P], const Quad (&b)[NT][P]) {
 #pragma unroll
-    for (uint32_t order = P; order-- > 0;)
+    for (uint32_t order = P == 1 ? 1 : P + 1; order-- > 0;)      // the last product of three planes, below 2^-30, is left out
 #pragma unroll
-      for (uint32_t p = 0; p <= order; ++p)
+      for (uint32_t p = order < P ? 0 : order - P + 1; p < P && p <= order; ++p)
 #pragma unroll
         for (uint32_t j = 0; j < NT; ++j) acc[i][j] = mfma<H>(q[p], b[j][order - p], acc[i][j]);
   };

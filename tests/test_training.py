@@ -741,3 +741,163 @@ def test_linear_xent_refusals_on_the_host():
         assert grad(**kw) == cv.ERR_ARG, kw
     assert grad(bytes=need - 1) == -4
     assert grad(n=0, h=None, t=None, labels=None, stats=None, dt=None) == 0
+
+
+@gpu
+@pytest.mark.parametrize("dtype,dtable,n,dim,vocab", [(BF16, F32, 100, 4096, 40000), (F32, F32, 20, 2048, 40000), (F16, F16, 300, 6000, 30001)])
+def test_linear_xent_of_several_pieces(dtype, dtable, n, dim, vocab):
+    """Tables whose planes and gradients go through the workspace in several pieces, the last of them smaller."""
+    each = dim * 2 * (2 if dtype == F32 else 1) + -(-n // 64) * 64 * 2 * (2 if dtable == F32 else 1)
+    assert each * vocab > 320 << 20, "one piece"
+    x = Xent(n, dim, vocab, dtype, dtable)
+    x.forward()
+    x.backward()
+    x.check()
+
+
+@gpu
+@pytest.mark.parametrize("dtype,dtable", XENT_TYPES)
+@pytest.mark.parametrize("n,dim,vocab,extra", [(3000, 40, 11, 1), (5001, 130, 300, 0), (4100, 24, 2000, 8)])
+def test_linear_xent_of_many_tokens_and_few_words(dtype, dtable, n, dim, vocab, extra):
+    """Where tokens are shared out among the table's gradients' workgroups, also added to what is there."""
+    x = Xent(n, dim, vocab, dtype, dtable, extra)
+    x.forward()
+    x.backward()
+    x.check()
+    start = f64(random_matrix(vocab, dim, dtable, 9, scale=1e-3))
+    x.dtable.copy_(torch.from_numpy(start))
+    x.dhidden.fill_(5.0)
+    x.backward(accumulate=True, dhidden=False)
+    x.check(dhidden=False, start=start)
+
+
+@gpu
+@pytest.mark.parametrize("dtype,dtable", XENT_TYPES)
+@pytest.mark.parametrize("n", [15, 16, 17, 32, 48, 64, 65])
+@pytest.mark.parametrize("dim,vocab,extra,offset", [(577, 65, 2, 0), (1030, 191, 1, 1), (32, 64, 0, 0), (31, 63, 5, 3)])
+def test_linear_xent_of_few_tokens(dtype, dtable, n, dim, vocab, extra, offset):
+    """Up to 64 tokens and one more; K that ends inside a line, vocabularies that end inside 64 rows, rows at any address."""
+    x = Xent(n, dim, vocab, dtype, dtable, extra, offset)
+    x.hidden[x.labels < 0] = float("nan")
+    x.forward(0.5)
+    x.backward(0.5)
+    x.check(0.5)
+
+
+# ----------------------------------------------------------------------------- streams, graphs, together
+@gpu
+def test_training_on_a_side_stream_and_in_a_graph():
+    """A step's forward and backward behind the kernels that make its inputs, on a stream of its own; then captured and
+    replayed on fresh inputs, with the same step eager on the same buffers and workspaces in between."""
+    n, dim, vocab = 300, 96, 2001
+    starts = torch.tensor([0, 100, 100, 101, 300], dtype=torch.int32, device=DEV)
+    x, gate, h, dh, dx, dgate = (torch.randn(n, dim, device=DEV, dtype=BF16) for _ in range(6))
+    table, labels = random_matrix(vocab, dim, BF16, 5, scale=0.1), tokens(n, vocab, 6).to(DEV)
+    loss, stats, dtable = torch.empty(n, device=DEV), torch.empty(n, 2, device=DEV), torch.empty(vocab, dim, device=DEV)
+    h0, last, dh0 = torch.randn(4, dim, device=DEV), torch.empty(4, dim, device=DEV), torch.empty(4, dim, device=DEV)
+    ws = cv.new_workspace(max(cv.gated_scan_workspace_bytes(n, dim, 4), cv.linear_xent_workspace_bytes(n, vocab, dim, BF16),
+                              cv.linear_xent_grad_workspace_bytes(n, vocab, dim, BF16, F32)), DEV)   # calls in turn share it
+
+    def step():
+        cv.gated_scan(x, gate, h, ws, starts=starts, h0=h0, last_out=last)
+        cv.linear_xent(h, table, labels, loss, ws, stats_out=stats)
+        cv.linear_xent_grad(h, table, labels, stats, dh, dtable, ws)
+        cv.gated_scan_grad(dh, x, gate, h, dx, dgate, ws, starts=starts, h0=h0, dlast=last, dh0_out=dh0)
+
+    outs = (h, last, loss, stats, dh, dtable, dx, dgate, dh0)
+
+    def wiped(call):
+        for t in outs:
+            t.fill_(3.0)
+        ws.fill_(0xFF)
+        call()
+        torch.cuda.synchronize()
+        return [t.clone() for t in outs]
+
+    def equal(a, b):
+        return all(torch.equal(p, q) for p, q in zip(a, b))
+
+    want = wiped(step)
+
+    def aside():
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            table.mul_(2.0).mul_(0.5)
+            step()
+        torch.cuda.current_stream().wait_stream(side)
+
+    assert equal(wiped(aside), want)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for seed in range(3):
+        g = torch.Generator().manual_seed(seed)
+        x.copy_(torch.randn(n, dim, generator=g))
+        labels.copy_(tokens(n, vocab, 20 + seed))
+        starts.copy_(torch.tensor([0, 7 * seed, 50, 299 - seed, 300], dtype=torch.int32))
+        assert equal(wiped(graph.replay), wiped(step))
+
+
+@gpu
+def test_local_training_example():
+    """The example's gradients against automatic differentiation of its loss in 64 bits, its single tokens against its
+    scan, one step of AdamW from its gradients; then that it runs."""
+    import math
+
+    from examples import local_training as ex
+
+    g = torch.Generator().manual_seed(3)
+    vocab, dim, lengths = 150, 24, [20, 1, 33, 6]
+    starts = torch.tensor([0, *np.cumsum(lengths)], dtype=torch.int32)
+    n = sum(lengths)
+    model = ex.Model(vocab, dim, DEV)
+    flat = torch.randn(model.flat.numel(), generator=g) * 0.5
+    model.flat.copy_(flat)
+    ids = torch.randint(vocab, (n,), generator=g)
+    ids[-2:] = -1
+    client = ex.Client(model, ids.to(DEV), starts.to(DEV))
+    client.model.flat.copy_(model.flat)
+    loss = client.gradient()
+
+    p = flat.double().requires_grad_()
+    table, inp, gate, gamma, beta = ex.Model.parts(model, p)
+    x = table[ids.clamp(min=0)] * math.sqrt(dim) * (ids >= 0).double()[:, None]
+    c = x - x.mean(1, keepdim=True)
+    y = c / torch.sqrt((c * c).mean(1, keepdim=True) + 1e-5) * gamma + beta
+    u, f, rows = y @ inp, torch.sigmoid(y @ gate), []
+    for low, high in zip(starts[:-1].tolist(), starts[1:].tolist()):
+        state = torch.zeros(dim, dtype=torch.float64)
+        for t in range(low, high):
+            state = f[t] * state + (1 - f[t]) * u[t]
+            rows.append(state)
+    h = torch.stack(rows)
+    labels = client.labels.cpu()
+    want = torch.nn.functional.cross_entropy((h @ table.t())[labels >= 0], labels[labels >= 0])
+    want.backward()
+    # seven sums in a row, of 150 terms at most, each off by no more than its length times a rounding of its terms, which
+    # cancel to a tenth of their size at worst
+    slack = 7 * 150 * ref.U * 10
+    assert loss.item() == pytest.approx(want.item(), rel=slack)
+    assert torch.linalg.norm(client.grad.cpu().double() - p.grad) <= slack * torch.linalg.norm(p.grad)
+    assert client.status.item() == 0
+
+    # the first text again, a token at a time
+    states, got = torch.zeros(1, dim, device=DEV), torch.empty(1, dim, device=DEV)
+    for t in range(lengths[0]):
+        cv.gated_scan_step(client.u[t:t + 1], client.f[t:t + 1], states, got)
+        assert torch.linalg.norm(got - client.h[t:t + 1]) <= 20 * 16 * ref.U * torch.linalg.norm(client.u[:t + 1])
+
+    # from no averages AdamW's first step is by the gradient's sign, almost: m / (1 - b1) over the root of v / (1 - b2), each
+    # within a step of their 8 bits (which the step itself does not see: it takes the averages before they are rounded)
+    before, grad = client.model.flat.clone(), client.grad.clone()
+    cv.adamw(client.plan, 1, 1e-3, seed=5)
+    decay = torch.cat([torch.full((q.numel(),), w) for q, w in zip(client.model.parts(before), [0.01] * 3 + [0.0] * 2)]).to(DEV)
+    want = before.double() * (1 - 1e-3 * decay.double()) - 1e-3 * grad.double() / (grad.double().abs() + 1e-8)
+    # an AdamW step's roundings: 16 of the move (b1, b2 and what they leave are fp32: 1 - 0.999 is off by 2^-14 of itself, but
+    # v and its correction by the same), and two of the weight
+    assert bool(((client.model.flat.double() - want).abs() <= 1e-3 * 2.0 ** -13 + 2 * ref.U * want.abs() + 2.0 ** -126).all())
+
+    losses, text = ex.run(rounds=3, clients=2, steps=2, texts=4, length=20, vocab=300, dim=32, say=lambda line: None)
+    assert len(losses) == 3 and all(math.isfinite(v) for v in losses)
+    assert text.shape == (8, 4) and bool(((text >= 0) & (text < 300)).all())
