@@ -793,12 +793,10 @@ __global__ __launch_bounds__(256) void join_kernel(JoinArgs a, TO* out) {
 // once, straight into registers.  Bound by HBM: 24 x 2048 x 200 003 bf16 takes 166 us (4.95 TB/s), where tiles of 256 rows through
 // LDS took 181 and wanted an aligned table.  For that a wavefront asks for 64 lines of 128 bytes, and the tokens' part, before it
 // waits for the first, and eight share K out among them line by line (four 176 us, two 214, sixteen 198; loads past the caches'
-// order 194).  Where the vocabulary is small it is K that takes the time, an eighth of it here: 4 x 4096 x 1472 15 us, which
-// a workgroup to a tile and all of K takes 57 for.  fp32 rows are cut into three planes of bfloat16 on the way, which hold
+// order 194).  Where the vocabulary is small it is what a CU has on its way: 4 x 4096 x 1472 takes 7.4 us, 57 as
+// tiles with all of K.  fp32 rows are cut into three planes of bfloat16 on the way, which hold
 // 8 + 8 + 8 bits, all there are, so that no row needs to be known before it is multiplied.
-constexpr uint32_t kFewRows = 64, kFewTokens = 64, kFewGap = 4;
-template <uint32_t NT>
-constexpr uint32_t kFewWaves = NT == 4 ? 4 : 8;                  // what LDS has room for
+constexpr uint32_t kFewTokens = 64, kFewGap = 4, kFewWaves = 8, kNoRow = 0xFFFFFFFFu;
 struct FewArgs {
   Matrix table;
   uint32_t dim;
@@ -833,12 +831,12 @@ __device__ __forceinline__ void operands(const float (&x)[8], Quad (&q)[kFewPlan
   }
 }
 
-template <class T, uint32_t NT, class E>
-__global__ __launch_bounds__(kFewWaves<NT>* kWave) void few_kernel(FewArgs a, E epilogue) {
+template <class T, uint32_t NT, uint32_t MT, class E>
+__global__ __launch_bounds__(kFewWaves* kWave) void few_kernel(FewArgs a, E epilogue) {
   using H = std::conditional_t<std::is_same_v<T, f16_t>, f16_t, bf16_t>;
-  constexpr uint32_t P = kFewPlanes<T>, MT = kFewRows / 16, kWide = kFewRows + kFewGap, kWaves = kFewWaves<NT>;
+  constexpr uint32_t P = kFewPlanes<T>, kRows = MT * 16, kWide = kRows + kFewGap, kWaves = kFewWaves;
   __shared__ __attribute__((aligned(16))) float z[kWaves][NT * 16][kWide];
-  const uint32_t lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(wave_id()), first = blockIdx.x * kFewRows, part = (lane >> 4) * 8;
+  const uint32_t lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(wave_id()), first = blockIdx.x * kRows, part = (lane >> 4) * 8;
   const T* rows[MT];
 #pragma unroll
   for (uint32_t i = 0; i < MT; ++i) rows[i] = static_cast<const T*>(a.table.p) + min(first + i * 16 + (lane & 15), a.table.rows - 1) * a.table.stride;
@@ -911,13 +909,14 @@ __global__ __launch_bounds__(kFewWaves<NT>* kWave) void few_kernel(FewArgs a, E 
 #pragma unroll
     for (uint32_t j = 0; j < NT; ++j) *reinterpret_cast<Four*>(&z[wave][j * 16 + (lane & 15)][i * 16 + (lane >> 4) * 4]) = acc[i][j];
   __syncthreads();
-  // a wavefront has a token's 64 rows at a time
+  // a wavefront has a token's rows at a time
+  const bool mine = lane < kRows;
   for (uint32_t token = wave; token < max(NT * 16, epilogue.tokens); token += kWaves) {
     float sum = 0.0f;
-    if (token < NT * 16)
+    if (token < NT * 16 && mine)
 #pragma unroll
-      for (uint32_t w = 0; w < kFewWaves<NT>; ++w) sum += z[w][token][lane];
-    epilogue(token, first + lane, sum);
+      for (uint32_t w = 0; w < kWaves; ++w) sum += z[w][token][lane];
+    epilogue(token, mine ? first + lane : kNoRow, sum);
   }
 }
 
@@ -948,6 +947,7 @@ struct FewGrad {
   uint64_t stride, plane;
   uint32_t tokens;          // with the rows of zeros up to whole tiles of K
   __device__ __forceinline__ void operator()(uint32_t token, uint32_t row, float product) const {
+    if (row == kNoRow) return;
     const bool live = token < who.n && who.live(token);
     float x = 0.0f;
     const int64_t v = (int64_t)first + row;
@@ -1017,6 +1017,11 @@ void run(const Product& g, const E& end, hipStream_t stream) {
   else
     run_as<H, TALL_A, TALL_B, Small>(g, end, stream);
 }
+
+// Rows of a workgroup of few tokens: fewer where 64 to each would not give every CU one (4 x 4096 x 1472 bf16 7.4 us, 15.2 with 64;
+// 38 x 6205 x 1216 32, 49).
+uint64_t few_rows(uint64_t vocab) { return vocab <= 64 * kCus ? 16 : 64; }
+uint64_t few_blocks(uint64_t vocab) { return (vocab + 63) / 64 * (64 / few_rows(vocab)); }
 
 struct Sizes {
   uint64_t depth, tokens, piece;      // dim and n in whole tiles of K; tokens of the vocabulary at a time
@@ -1113,6 +1118,13 @@ bool as_it_is(const void* p, uint64_t stride, uint32_t dim, uint32_t type) {
   return type != CVLC_F32 && dim % kDepth == 0 && stride % 8 == 0 && stride < (1u << 22) && reinterpret_cast<uintptr_t>(p) % 16 == 0;
 }
 
+// Few tokens, that is whether logits come from the rows as they are.  Of more than 32, tiles that stay in LDS take less of a table
+// that they can read as it is and that fills them: 60 x 2048 x 200 003 bf16 227 us against 292 (3 values to a row more 583 against
+// 387, fp32 835 against 346 for half as many rows).
+bool few_tokens(const Call& c) {
+  return c.n <= kFewTokens / 2 || (c.n <= kFewTokens && (few_rows(c.vocab) == 16 || !as_it_is(c.table, c.table_stride, c.dim, c.type)));
+}
+
 // The parts of a workspace; with base = null only its size.
 struct Parts {
   Factors* factors;
@@ -1131,7 +1143,7 @@ struct LossParts : Parts {
   float* answer;
   uint64_t bytes;
   LossParts(Room r, const Sizes& z, uint32_t n, uint32_t vocab) : Parts(r, z, n) {
-    partial = r.take<float2>((vocab / (n <= kFewTokens ? kFewRows : Small::TM) + vocab / z.piece + 2) * n);
+    partial = r.take<float2>(std::max(n <= kFewTokens ? few_blocks(vocab) : 0, vocab / Small::TM + vocab / z.piece + 2) * n);
     answer = r.take<float>(n);
     bytes = r.used;
   }
@@ -1184,8 +1196,11 @@ void run_few(const Call& c, const Sizes& z, const Parts& parts, uint64_t first, 
   const FewArgs a{c.table_matrix(first, rows), c.dim, parts.few, z.depth, plane};
   auto go = [&](auto tokens) {
     constexpr uint32_t NT = decltype(tokens)::value;
-    hipLaunchKernelGGL((few_kernel<T, NT, E>), dim3((rows + kFewRows - 1) / kFewRows),
-                       dim3(kFewWaves<NT> * kWave), 0, stream, a, end);
+    const uint32_t blocks = few_blocks(rows);
+    if (few_rows(rows) == 16)
+      hipLaunchKernelGGL((few_kernel<T, NT, 1, E>), dim3(blocks), dim3(kFewWaves * kWave), 0, stream, a, end);
+    else
+      hipLaunchKernelGGL((few_kernel<T, NT, 4, E>), dim3(blocks), dim3(kFewWaves * kWave), 0, stream, a, end);
   };
   if (c.n <= 16)
     go(std::integral_constant<uint32_t, 1>{});
@@ -1200,9 +1215,9 @@ void loss_of(const Call& c, const Sizes& z, const LossParts& parts, float* loss,
   using H = typename Kind<T>::H;
   constexpr uint32_t P = Kind<T>::P;
   uint32_t tile = 0;
-  if (c.n <= kFewTokens) {
+  if (few_tokens(c)) {
     run_few<T>(c, z, parts, 0, c.vocab, FewStats{c.who, c.scale, parts.partial, parts.answer, 0}, stream);
-    tile = (c.vocab + kFewRows - 1) / kFewRows;
+    tile = few_blocks(c.vocab);
   } else {
     const bool hidden_goes = as_it_is(c.hidden, c.hidden_stride, c.dim, c.type), table_goes = as_it_is(c.table, c.table_stride, c.dim, c.type);
     if (P > 1) find_factors(c, z, parts, nullptr, stream);
@@ -1244,7 +1259,7 @@ void grad_of(const Call& c, const Sizes& z, const GradParts& parts, const float2
              uint64_t dtable_stride, bool accumulate, uint32_t* status, hipStream_t stream) {
   using H = typename Kind<T>::H;
   constexpr uint32_t P = Kind<T>::P, PG = sizeof(TO) == 4 ? 2 : 1;
-  const bool table_goes = as_it_is(c.table, c.table_stride, c.dim, c.type), few = c.n <= kFewTokens;
+  const bool table_goes = as_it_is(c.table, c.table_stride, c.dim, c.type), few = few_tokens(c);
   find_factors(c, z, parts, status, stream);
   PackArgs hidden{c.hidden_matrix(), c.dim, (uint32_t)z.tokens, parts.hidden, z.depth, z.tokens * z.depth, parts.factors->up, 1};
   for (uint64_t first = 0; first < c.vocab; first += z.piece) {
@@ -1320,7 +1335,7 @@ int check(const Call& c, const float* d_stats, const void* d_workspace, const ui
   if (d_stats && !buffer_ok(d_stats, 8)) return CVLC_ERR_ARG;
   // tiles of a launch, and threads of one: fewer than 2^32
   const uint64_t tiles = ((uint64_t)c.n / 128 + 1) * (pad_to(c.vocab, kPadTo) / 128), packs = ((uint64_t)std::max(c.n, c.vocab) / 64 + 1) * (c.dim / 64 + 1);
-  if (tiles >= 1ull << 23 || packs >= 1ull << 24 || (c.n <= kFewTokens && c.vocab / kFewRows >= 1u << 22)) return CVLC_ERR_ARG;
+  if (tiles >= 1ull << 23 || packs >= 1ull << 24 || (c.n <= kFewTokens && c.vocab >= 1u << 28)) return CVLC_ERR_ARG;
   return CVLC_OK;
 }
 

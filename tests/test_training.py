@@ -784,6 +784,18 @@ def test_linear_xent_of_few_tokens(dtype, dtable, n, dim, vocab, extra, offset):
     x.check(0.5)
 
 
+@gpu
+@pytest.mark.parametrize("dtype,dtable", XENT_TYPES)
+@pytest.mark.parametrize("n", [32, 33, 64])
+@pytest.mark.parametrize("dim,extra", [(128, 0), (128, 1)])
+def test_linear_xent_of_few_tokens_and_many_words(dtype, dtable, n, dim, extra):
+    """Where tables that tiles can read as they are, and others, go different ways."""
+    x = Xent(n, dim, 16500, dtype, dtable, extra)
+    x.forward()
+    x.backward()
+    x.check()
+
+
 # ----------------------------------------------------------------------------- streams, graphs, together
 @gpu
 def test_training_on_a_side_stream_and_in_a_graph():
