@@ -453,7 +453,7 @@ int cvlc_distill_grad(uint32_t n, uint32_t vocab, const void* d_logits, uint32_t
  *   d_labels   n tokens of id_bytes = 4 or 8 bytes, signed.  A negative one is
  *              padding; one at or beyond `vocab` sets CVLC_DEV_INDEX and counts as
  *              padding too
- *   d_weights  n fp32 w_i, or NULL (all 1)
+ *   d_weights  n fp32 w_i, finite, or NULL (all 1)
  *   d_loss     NULL, or n fp32
  *   d_stats    NULL, or n times {m, S}, fp32, 8-byte aligned, for
  *              cvlc_linear_xent_grad: the largest logit and the sum of exp(z - m)

@@ -601,13 +601,15 @@ struct StatsEnd {
   }
 };
 
-// The tiles' statistics joined, and the losses: a workgroup has 2^tokens_log2 tokens, fewer where there are few.
-constexpr uint32_t kJoinBlock = 256;
+// The tiles' statistics joined, and the losses: a workgroup has 2^tokens_log2 tokens, fewer where there are few, and more threads
+// where there are many tiles to each (24 tokens, 3126 tiles: 8.9 us, 11.4 with 256).
+constexpr uint32_t kJoinMost = 1024;
+uint32_t join_block(uint32_t n, uint32_t tiles) { return n < 2048 && tiles > 1024 ? kJoinMost : 256; }
 uint32_t join_tokens_log2(uint32_t n) { return n >= 16384 ? 4 : n >= 2048 ? 2 : 0; }
-__global__ __launch_bounds__(kJoinBlock) void loss_kernel(Rows who, uint32_t tiles, uint32_t tokens_log2, const float2* partial,
+__global__ __launch_bounds__(kJoinMost) void loss_kernel(Rows who, uint32_t tiles, uint32_t tokens_log2, const float2* partial,
                                                           const float* answer, float* loss, float2* stats, uint32_t* status) {
-  __shared__ float2 shared[kJoinBlock];
-  const uint32_t tokens = 1u << tokens_log2, rows = kJoinBlock >> tokens_log2;
+  __shared__ float2 shared[kJoinMost];
+  const uint32_t tokens = 1u << tokens_log2, rows = blockDim.x >> tokens_log2;
   const uint32_t x = threadIdx.x & (tokens - 1), y = threadIdx.x >> tokens_log2, token = (blockIdx.x << tokens_log2) + x;
   float2 all = {-INFINITY, 0.0f};
   auto add = [](float2 a, float2 b) {
@@ -1244,7 +1246,7 @@ void loss_of(const Call& c, const Sizes& z, const LossParts& parts, float* loss,
     }
   }
   const uint32_t log2 = join_tokens_log2(c.n);
-  hipLaunchKernelGGL(loss_kernel, dim3((c.n + (1u << log2) - 1) >> log2), dim3(kJoinBlock), 0, stream, c.who, tile, log2, parts.partial,
+  hipLaunchKernelGGL(loss_kernel, dim3((c.n + (1u << log2) - 1) >> log2), dim3(join_block(c.n, tile)), 0, stream, c.who, tile, log2, parts.partial,
                      parts.answer, loss, stats, status);
 }
 
