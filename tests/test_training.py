@@ -464,6 +464,31 @@ def test_gated_scan_step_of_slots_that_do_not_go():
 
 
 @gpu
+@pytest.mark.parametrize("dtype,n,dim", [(F32, 4097, 6), (BF16, 5003, 17), (F16, 70001, 3)])
+def test_gated_scan_step_of_many_slots(dtype, n, dim):
+    """Rows enough for their slots to be looked at several at a time; some named twice, near by and far off, some not there."""
+    x, gate = random_matrix(n, dim, dtype, 1, 1, 1), random_matrix(n, dim, dtype, 2, 1, 1)
+    at = torch.randperm(n, generator=torch.Generator().manual_seed(3))
+    wrong = [4, 17, 31, 33, n - 2, n - 1]
+    at[4], at[17], at[31], at[33], at[n - 2], at[n - 1], at[40] = at[3], at[16], n, at[0], at[n - 3], at[5], -1
+    g = torch.Generator().manual_seed(4)
+    states, status = torch.randn(n, dim, generator=g).to(DEV), torch.zeros(1, dtype=torch.int32, device=DEV)
+    before = f64(states)
+    h, flat = matrix(n, dim, dtype, 1, 1, fill=5.0)
+    cv.gated_scan_step(x, gate, states, h, slots=at.to(torch.int32 if dim == 6 else torch.int64).to(DEV), status=status)
+    live = np.array([i for i in range(n) if i not in (*wrong, 40)])
+    slots = at.numpy()[live]
+    f, rest = ref.sigmoid(f64(gate)[live])
+    want_h, off_h, want, off = np.zeros((n, dim)), np.zeros((n, dim)), before.copy(), np.zeros((n, dim))
+    want_h[live] = f * before[slots] + rest * f64(x)[live]
+    off_h[live] = 16 * ref.U * (f * np.abs(before[slots]) + rest * np.abs(f64(x)[live])) + 2.0 ** -126   # as a step of the scan
+    want[slots], off[slots] = want_h[live], off_h[live]
+    assert_near(h, want_h, off_h, dtype)
+    assert_near(states, want, off)
+    assert status.item() == cv.DEV_INDEX and untouched(flat, h, 5.0)
+
+
+@gpu
 def test_gated_scan_steps_walk_as_the_scan_does():
     n, dim = 40, 33
     s = Scan(3 * n, dim, F32, 3)
@@ -638,6 +663,34 @@ def test_linear_xent_of_far_weights(dtype, weight):
     x.forward()
     x.backward()
     x.check()
+
+
+@gpu
+@pytest.mark.parametrize("n", [20, 150])
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("what", ["no hidden", "no table", "scale 0", "scale -1.5", "no weight", "weights below 0", "far", "one label"])
+def test_linear_xent_at_the_ends_of_what_is_allowed(n, dtype, what):
+    x, scale = Xent(n, 64, 300, dtype, F32), {"scale 0": 0.0, "scale -1.5": -1.5}.get(what, 1.0)
+    if what == "no hidden":
+        x.hidden.zero_()
+    elif what == "no table":
+        x.table.zero_()
+    elif what == "no weight":
+        x.weights.zero_()
+    elif what == "weights below 0":
+        x.weights.neg_()
+    elif what == "far":                                                # powers of two, and what the types hold
+        far = 2.0 ** (10 if dtype == F16 else 90)
+        x.hidden.mul_(far)
+        x.table.mul_(1 / far if dtype != F16 else 2.0 ** -4)
+        scale = 1.0 if dtype != F16 else 2.0 ** -6
+    elif what == "one label":
+        x.labels.fill_(7)
+    x.forward(scale)
+    x.backward(scale)
+    if what == "no weight":
+        assert not x.loss.any() and not x.dhidden.any() and not x.dtable.any()
+    x.check(scale)
 
 
 @gpu
