@@ -797,7 +797,8 @@ __global__ __launch_bounds__(256) void join_kernel(JoinArgs a, TO* out) {
 // waits for the first, and eight share K out among them line by line (four 176 us, two 214, sixteen 198; loads past the caches'
 // order 194).  Where the vocabulary is small it is what a CU has on its way: 4 x 4096 x 1472 takes 7.4 us, 57 as
 // tiles with all of K.  fp32 rows are cut into three planes of bfloat16 on the way, which hold
-// 8 + 8 + 8 bits, all there are, so that no row needs to be known before it is multiplied.
+// 8 + 8 + 8 bits, all there are, so that no row needs to be known before it is multiplied (24 x 2048 x 100 003 228 us, 3.6 TB/s; with
+// K in an order that has four lanes read 64 bytes of a row at a time the same).
 constexpr uint32_t kFewTokens = 64, kFewGap = 4, kFewWaves = 8, kNoRow = 0xFFFFFFFFu;
 struct FewArgs {
   Matrix table;
@@ -842,7 +843,8 @@ __global__ __launch_bounds__(kFewWaves* kWave) void few_kernel(FewArgs a, E epil
   const T* rows[MT];
 #pragma unroll
   for (uint32_t i = 0; i < MT; ++i) rows[i] = static_cast<const T*>(a.table.p) + min(first + i * 16 + (lane & 15), a.table.rows - 1) * a.table.stride;
-  const Half* tokens = a.hidden + (lane & 15) * a.stride;
+  const uint32_t token0 = blockIdx.y * kFewTokens;
+  const Half* tokens = a.hidden + (token0 + (lane & 15)) * a.stride;
   Four acc[MT][NT];
 #pragma unroll
   for (uint32_t i = 0; i < MT; ++i)
@@ -913,12 +915,12 @@ __global__ __launch_bounds__(kFewWaves* kWave) void few_kernel(FewArgs a, E epil
   __syncthreads();
   // a wavefront has a token's rows at a time
   const bool mine = lane < kRows;
-  for (uint32_t token = wave; token < max(NT * 16, epilogue.tokens); token += kWaves) {
+  for (uint32_t token = wave; token < max(NT * 16, min(epilogue.tokens, kFewTokens)); token += kWaves) {
     float sum = 0.0f;
     if (token < NT * 16 && mine)
 #pragma unroll
       for (uint32_t w = 0; w < kWaves; ++w) sum += z[w][token][lane];
-    epilogue(token, mine ? first + lane : kNoRow, sum);
+    epilogue(token0 + token, mine ? first + lane : kNoRow, sum);
   }
 }
 
@@ -1120,11 +1122,20 @@ bool as_it_is(const void* p, uint64_t stride, uint32_t dim, uint32_t type) {
   return type != CVLC_F32 && dim % kDepth == 0 && stride % 8 == 0 && stride < (1u << 22) && reinterpret_cast<uintptr_t>(p) % 16 == 0;
 }
 
+// Of more than 64, 64 at a time, while a CU has no more than one of them: 96 x 2816 x 1983 fp32 43 us against 113 of 16 small tiles
+// (256 x 2816 x 4000, four to a CU, 152 against 115).
+constexpr uint32_t kFewMany = 256;
+bool few_of_many(uint32_t n, uint32_t vocab) {
+  return n <= kFewMany && few_rows(vocab) == 16 && (n + kFewTokens - 1) / kFewTokens * few_blocks(vocab) <= kCus;
+}
+bool may_be_few(uint32_t n, uint32_t vocab) { return n <= kFewTokens || few_of_many(n, vocab); }
+
 // Few tokens, that is whether logits come from the rows as they are.  Of more than 32, tiles that stay in LDS take less of a table
 // that they can read as it is and that fills them: 60 x 2048 x 200 003 bf16 227 us against 292 (3 values to a row more 583 against
 // 387, fp32 835 against 346 for half as many rows).
 bool few_tokens(const Call& c) {
-  return c.n <= kFewTokens / 2 || (c.n <= kFewTokens && (few_rows(c.vocab) == 16 || !as_it_is(c.table, c.table_stride, c.dim, c.type)));
+  if (c.n > kFewTokens) return few_of_many(c.n, c.vocab);
+  return c.n <= kFewTokens / 2 || few_rows(c.vocab) == 16 || !as_it_is(c.table, c.table_stride, c.dim, c.type);
 }
 
 // The parts of a workspace; with base = null only its size.
@@ -1132,20 +1143,20 @@ struct Parts {
   Factors* factors;
   float* tops;
   Half *hidden, *table, *few;   // few: hidden rows beside a table that is read as it is
-  Parts(Room& r, const Sizes& z, uint32_t n) {
+  Parts(Room& r, const Sizes& z, uint32_t n, uint32_t vocab) {
     factors = r.take<Factors>(1);
     tops = r.take<float>(z.planes > 1 ? 2 * kSurveyGrid : 0);
     hidden = r.take<Half>(z.planes * z.tokens * z.depth);
     table = r.take<Half>(z.planes * z.piece * z.depth);
-    few = r.take<Half>(n <= kFewTokens ? 3 * kFewTokens * z.depth : 0);
+    few = r.take<Half>(may_be_few(n, vocab) ? 3 * z.tokens * z.depth : 0);
   }
 };
 struct LossParts : Parts {
   float2* partial;
   float* answer;
   uint64_t bytes;
-  LossParts(Room r, const Sizes& z, uint32_t n, uint32_t vocab) : Parts(r, z, n) {
-    partial = r.take<float2>(std::max(n <= kFewTokens ? few_blocks(vocab) : 0, vocab / Small::TM + vocab / z.piece + 2) * n);
+  LossParts(Room r, const Sizes& z, uint32_t n, uint32_t vocab) : Parts(r, z, n, vocab) {
+    partial = r.take<float2>(std::max(may_be_few(n, vocab) ? few_blocks(vocab) : 0, vocab / Small::TM + vocab / z.piece + 2) * n);
     answer = r.take<float>(n);
     bytes = r.used;
   }
@@ -1154,7 +1165,7 @@ struct GradParts : Parts {
   Half* g;
   float *sums, *table_sums, *rests;
   uint64_t bytes;
-  GradParts(Room r, const Sizes& z, uint32_t n) : Parts(r, z, n) {
+  GradParts(Room r, const Sizes& z, uint32_t n, uint32_t vocab) : Parts(r, z, n, vocab) {
     g = r.take<Half>(z.g_planes * z.tokens * z.piece);
     sums = r.take<float>(z.slices * n * z.depth);
     table_sums = r.take<float>(std::min(kSumsMost / 4, kSlicesMost * z.piece * z.depth));
@@ -1193,16 +1204,17 @@ template <class T, class E>
 void run_few(const Call& c, const Sizes& z, const Parts& parts, uint64_t first, uint32_t rows, const E& end, hipStream_t stream) {
   constexpr uint32_t P = kFewPlanes<T>;
   using H = std::conditional_t<std::is_same_v<T, f16_t>, f16_t, bf16_t>;
-  const uint64_t plane = kFewTokens * z.depth;
-  if (first == 0) pack<T, H, P>(c, PackArgs{c.hidden_matrix(), c.dim, kFewTokens, parts.few, z.depth, plane, nullptr, 1}, PackArgs{}, stream);
+  const uint32_t groups = (c.n + kFewTokens - 1) / kFewTokens;
+  const uint64_t plane = groups * kFewTokens * z.depth;
+  if (first == 0) pack<T, H, P>(c, PackArgs{c.hidden_matrix(), c.dim, groups * kFewTokens, parts.few, z.depth, plane, nullptr, 1}, PackArgs{}, stream);
   const FewArgs a{c.table_matrix(first, rows), c.dim, parts.few, z.depth, plane};
   auto go = [&](auto tokens) {
     constexpr uint32_t NT = decltype(tokens)::value;
     const uint32_t blocks = few_blocks(rows);
     if (few_rows(rows) == 16)
-      hipLaunchKernelGGL((few_kernel<T, NT, 1, E>), dim3(blocks), dim3(kFewWaves * kWave), 0, stream, a, end);
+      hipLaunchKernelGGL((few_kernel<T, NT, 1, E>), dim3(blocks, groups), dim3(kFewWaves * kWave), 0, stream, a, end);
     else
-      hipLaunchKernelGGL((few_kernel<T, NT, 4, E>), dim3(blocks), dim3(kFewWaves * kWave), 0, stream, a, end);
+      hipLaunchKernelGGL((few_kernel<T, NT, 4, E>), dim3(blocks, groups), dim3(kFewWaves * kWave), 0, stream, a, end);
   };
   if (c.n <= 16)
     go(std::integral_constant<uint32_t, 1>{});
@@ -1373,7 +1385,7 @@ int cvlc_linear_xent(uint32_t n, uint32_t vocab, uint32_t dim, const void* d_hid
 size_t cvlc_linear_xent_grad_workspace_bytes(uint32_t n, uint32_t vocab, uint32_t dim, uint32_t type, uint32_t dtable_type) {
   using namespace cvlc;
   if (!n || !vocab || !dim) return 256;
-  return (size_t)GradParts(Room{}, sizes_for(n, vocab, dim, type, dtable_type, true), n).bytes;
+  return (size_t)GradParts(Room{}, sizes_for(n, vocab, dim, type, dtable_type, true), n, vocab).bytes;
 }
 
 int cvlc_linear_xent_grad(uint32_t n, uint32_t vocab, uint32_t dim, const void* d_hidden, uint64_t hidden_stride, const void* d_table,
@@ -1402,7 +1414,7 @@ int cvlc_linear_xent_grad(uint32_t n, uint32_t vocab, uint32_t dim, const void* 
     return hip_check(hipGetLastError());
   }
   const Sizes z = sizes_for(n, vocab, dim, type, out_type, true);
-  const GradParts room(Room{static_cast<uint8_t*>(d_workspace), 0}, z, n);
+  const GradParts room(Room{static_cast<uint8_t*>(d_workspace), 0}, z, n, vocab);
   by_type(type, [&](auto t) {
     using T = decltype(t);
     auto go = [&](auto to) {

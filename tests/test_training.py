@@ -839,6 +839,17 @@ def test_linear_xent_of_few_tokens(dtype, dtable, n, dim, vocab, extra, offset):
 
 @gpu
 @pytest.mark.parametrize("dtype,dtable", XENT_TYPES)
+@pytest.mark.parametrize("n,vocab", [(128, 700), (129, 63), (128, 2048), (200, 1025), (256, 1024), (256, 1025), (257, 200)])
+def test_linear_xent_of_a_few_times_64_tokens(dtype, dtable, n, vocab):
+    x = Xent(n, 300, vocab, dtype, dtable, 1, 1)
+    x.hidden[x.labels < 0] = float("nan")
+    x.forward()
+    x.backward()
+    x.check()
+
+
+@gpu
+@pytest.mark.parametrize("dtype,dtable", XENT_TYPES)
 @pytest.mark.parametrize("n", [32, 33, 64])
 @pytest.mark.parametrize("dim,extra", [(128, 0), (128, 1)])
 def test_linear_xent_of_few_tokens_and_many_words(dtype, dtable, n, dim, extra):
