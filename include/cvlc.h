@@ -509,6 +509,9 @@ int cvlc_linear_xent_grad(uint32_t n, uint32_t vocab, uint32_t dim, const void* 
  *              written.  Offsets that are not so set CVLC_DEV_INDEX; results are
  *              then unspecified.  NULL: n_seq sequences of n / n_seq rows each
  *              (n a multiple of n_seq).
+ * A NaN or an infinity reaches what the recurrence, forward or backward, comes to
+ * after it in its channel of its sequence, as one of the two; other sequences and
+ * channels come out as they would without it.
  *   d_status   as for cvlc_embed */
 
 /* GPU.  Forward.

@@ -5,7 +5,8 @@
 //   D_t = dy_t + c_(t+1),   c_t = f_t (dy_t + c_(t+1)),
 //   dx_t = (1 - f_t) D_t,   dgate_t = D_t (h_(t-1) - x_t) f_t (1 - f_t).
 // Both are one walk, u <- a u + b, that way and back: steps chain as (A, B), u <- A u + B,
-// so rows are cut into pieces whose (A, B) are found side by side and joined.
+// so rows are cut into pieces whose (A, B) are found side by side and joined.  A piece in which a sequence begins
+// forgets what comes before it: its A is kAnew, not 0, which would hand a NaN or an infinity on to the next sequence.
 //
 // Where sequences and channels fill the device (scan_rows), a workgroup has a block of channels of one
 // sequence and goes over its rows some hundred at a time: every thread has `L` rows of 16 bytes' worth of
@@ -84,6 +85,9 @@ __device__ __forceinline__ float blend(float g, float u, float x) {
   const float near = keeps(g) ? u : x, far = keeps(g) ? x : u;
   return fmaf(fabsf(g), far - near, near);
 }
+
+constexpr float kAnew = -1.0f;          // other A are products of gates: never negative, and 0 where they are too small
+__device__ __forceinline__ float chain(float A, float B, float u) { return A < 0.0f ? B : fmaf(A, u, B); }
 
 // Marks of an iteration's rows, by their place in it: the sequence that begins, or ends, with a row; -1: none.
 template <uint32_t W>
@@ -223,7 +227,7 @@ __device__ __forceinline__ void join(uint32_t mine, uint32_t width, uint32_t row
     for (uint32_t r = 0; r < rows; ++r) {
       const float x = sa[r * width + threadIdx.x], y = sb[r * width + threadIdx.x];
       sb[r * width + threadIdx.x] = u;
-      u = fmaf(x, u, y);
+      u = chain(x, y, u);
     }
     carry[threadIdx.x] = u;
   }
@@ -296,19 +300,22 @@ __global__ __launch_bounds__(kScanBlock, 4) void scan_rows_kernel(ScanArgs a, co
         float g[L][N], y[L][N];
 #pragma unroll
         for (uint32_t k = 0; k < N; ++k) A[k] = 1.0f, B[k] = 0.0f;
+        bool anew = false;
 #pragma unroll
         for (uint32_t i = 0; i < L; ++i)
           if (WHOLE || there(i)) {
             const int32_t seq = WHOLE ? -1 : mark(enters, i);
             if (seq >= 0) {
               load_state<N>(a.first, (uint32_t)seq, at, a.dim, B);
-#pragma unroll
-              for (uint32_t k = 0; k < N; ++k) A[k] = 0.0f;
+              anew = true;
             }
             rg[i].values(g[i]);
             rv[i].values(y[i]);
             first_walk<T, FORWARD>(g[i], y[i], A, B);
           }
+        if (!WHOLE && anew)
+#pragma unroll
+          for (uint32_t k = 0; k < N; ++k) A[k] = kAnew;
         join<N>(mine, width, rows, A, B, sa, sb, carry, in);
 #pragma unroll
         for (uint32_t i = 0; i < L; ++i)
@@ -394,6 +401,7 @@ __global__ __launch_bounds__(kRangeBlock, 4) void scan_range_kernel(ScanArgs a, 
     if (from < to) locate(a, FORWARD ? from : to - 1, seq, begin, end);
   }
   float A[N], u[N];
+  bool anew = false;
 #pragma unroll
   for (uint32_t k = 0; k < N; ++k) A[k] = 1.0f, u[k] = 0.0f;
   if (APPLY) {
@@ -424,8 +432,7 @@ __global__ __launch_bounds__(kRangeBlock, 4) void scan_range_kernel(ScanArgs a, 
           if (a.flat && (t < begin || t >= end)) locate(a, t, seq, begin, end);
           if (t == (FORWARD ? begin : end - 1)) {
             load_state<N>(a.first, seq, at, a.dim, u);
-#pragma unroll
-            for (uint32_t k = 0; k < N; ++k) A[k] = 0.0f;
+            anew = true;
           }
         }
         float g[N], y[N], none[N] = {};
@@ -466,7 +473,7 @@ __global__ __launch_bounds__(kRangeBlock, 4) void scan_range_kernel(ScanArgs a, 
     float2* p = a.partial + (uint64_t)part * a.dim + at;
 #pragma unroll
     for (uint32_t k = 0; k < N; ++k)
-      if (at + k < a.dim) p[k] = float2{A[k], u[k]};
+      if (at + k < a.dim) p[k] = float2{anew ? kAnew : A[k], u[k]};
   }
 }
 
@@ -483,20 +490,20 @@ __global__ __launch_bounds__(kCarryWide * kCarryRows) void scan_carry_kernel(Sca
 #pragma unroll 8
     for (uint32_t r = from; r < to; ++r) {
       const float2 s = p[(uint64_t)r * a.dim];
-      all = float2{all.x * s.x, fmaf(s.x, all.y, s.y)};
+      all = float2{all.x < 0.0f || s.x < 0.0f ? kAnew : all.x * s.x, chain(s.x, s.y, all.y)};
     }
   steps[y][x] = all;
   __syncthreads();
   if (c >= a.dim) return;
   float u = a.first && !a.flat ? a.first[(uint64_t)walk * a.dim + c] : 0.0f;
 #pragma unroll 8
-  for (uint32_t r = 0; r < y; ++r) u = fmaf(steps[r][x].x, u, steps[r][x].y);
+  for (uint32_t r = 0; r < y; ++r) u = chain(steps[r][x].x, steps[r][x].y, u);
   float* e = a.enter + (uint64_t)walk * a.ranges * a.dim + c;
 #pragma unroll 8
   for (uint32_t r = from; r < to; ++r) {
     const float2 s = p[(uint64_t)r * a.dim];
     e[(uint64_t)r * a.dim] = u;
-    u = fmaf(s.x, u, s.y);
+    u = chain(s.x, s.y, u);
   }
 }
 
