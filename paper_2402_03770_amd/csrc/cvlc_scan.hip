@@ -158,13 +158,44 @@ __device__ __forceinline__ uint32_t channel_of(uint32_t group, uint32_t dim) {
   return dim >= N ? min(group * N, dim - N) : 0u;
 }
 
-// Sequences without rows hand on what they start from; offsets that are out of order or out of the rows are told of.
-__device__ __forceinline__ void see_to_empty(const ScanArgs& a, uint32_t thread, uint32_t threads) {
-  for (uint32_t j = thread; j < a.n_seq; j += threads) {
-    const int64_t from = start_as_given(a, j), to = start_as_given(a, j + 1);
-    if (a.status && (from < 0 || to < from || to > (int64_t)a.n)) atomicOr(a.status, CVLC_DEV_INDEX);
-    if (a.last && start_of(a, j + 1) <= start_of(a, j))
-      for (uint32_t c = 0; c < a.dim; ++c) a.last[(uint64_t)j * a.dim + c] = a.first ? a.first[(uint64_t)j * a.dim + c] : 0.0f;
+// Sequences without rows hand on what they start from; offsets that are out of order or out of the rows are told of.  A wavefront
+// has some sequences and kSeeWide channels of their states, which its lanes copy side by side.
+constexpr uint32_t kSeeEach = 8, kSeeWide = kWave * kSeeEach, kSeeFew = 1u << 12;
+__host__ __device__ inline uint32_t see_per(uint32_t n_seq) { return n_seq <= kSeeFew ? 1 : kWave; }   // sequences of a wavefront
+__host__ __device__ inline uint64_t see_items(uint32_t n_seq, uint32_t dim) {
+  return ((uint64_t)n_seq + see_per(n_seq) - 1) / see_per(n_seq) * (((uint64_t)dim + kSeeWide - 1) / kSeeWide);
+}
+__device__ __forceinline__ void see_to_empty(const ScanArgs& a, uint32_t wave, uint32_t waves) {
+  const uint32_t dim = a.last ? a.dim : 1, per = see_per(a.n_seq), parts = (dim + kSeeWide - 1) / kSeeWide, lane = lane_id();
+  const uint64_t all = see_items(a.n_seq, dim);
+  for (uint64_t item = wave; item < all; item += waves) {
+    const uint32_t first = (uint32_t)(item / parts) * per, part = (uint32_t)(item % parts), low = part * kSeeWide, high = min(dim - low, kSeeWide) + low;
+    const uint32_t j = first + lane;
+    bool empty = false;
+    if (lane < per && j < a.n_seq) {
+      const int64_t from = start_as_given(a, j), to = start_as_given(a, j + 1);
+      if (part == 0 && a.status && (from < 0 || to < from || to > (int64_t)a.n)) atomicOr(a.status, CVLC_DEV_INDEX);
+      empty = a.last && start_of(a, j + 1) <= start_of(a, j);
+    }
+    const uint64_t which = __ballot(empty);
+    if (which == 0) continue;
+    uint32_t wide = kWave;              // lanes that share a state: fewer where it is narrower
+    while (wide > 1 && wide / 2 >= high - low) wide /= 2;
+    for (uint32_t k = lane / wide; k < per; k += kWave / wide) {
+      if (!(which >> k & 1)) continue;
+      const uint64_t row = (uint64_t)(first + k) * a.dim;
+      float u[kSeeEach];
+#pragma unroll
+      for (uint32_t i = 0; i < kSeeEach; ++i) {
+        const uint32_t c = low + lane % wide + i * wide;
+        u[i] = a.first && c < high ? a.first[row + c] : 0.0f;
+      }
+#pragma unroll
+      for (uint32_t i = 0; i < kSeeEach; ++i) {
+        const uint32_t c = low + lane % wide + i * wide;
+        if (c < high) a.last[row + c] = u[i];
+      }
+    }
   }
 }
 
@@ -245,7 +276,7 @@ __global__ __launch_bounds__(kScanBlock, 4) void scan_rows_kernel(ScanArgs a, co
   __shared__ float sa[kScanBlock * N], sb[kScanBlock * N], carry[kGroupsMost * N];
   __shared__ Marks<kMarks> marks;
   if (blockIdx.x >= a.main_grid) {
-    see_to_empty(a, (blockIdx.x - a.main_grid) * kScanBlock + threadIdx.x, (gridDim.x - a.main_grid) * kScanBlock);
+    see_to_empty(a, (blockIdx.x - a.main_grid) * (kScanBlock / kWave) + wave_id(), (gridDim.x - a.main_grid) * (kScanBlock / kWave));
     return;
   }
   const uint32_t groups = 1u << a.groups_log2, width = groups * N, rows = kScanBlock >> a.groups_log2, W = rows * L;
@@ -380,7 +411,7 @@ __global__ __launch_bounds__(kRangeBlock, 4) void scan_range_kernel(ScanArgs a, 
                                                                     T* dgate) {
   constexpr uint32_t N = kPerAccess<T>, P = kBatch<FORWARD, APPLY>;
   if (APPLY && blockIdx.x >= a.main_grid) {
-    see_to_empty(a, (blockIdx.x - a.main_grid) * kRangeBlock + threadIdx.x, (gridDim.x - a.main_grid) * kRangeBlock);
+    see_to_empty(a, (blockIdx.x - a.main_grid) * (kRangeBlock / kWave) + wave_id(), (gridDim.x - a.main_grid) * (kRangeBlock / kWave));
     return;
   }
   const uint32_t pieces = (a.dim + N - 1) / N;
@@ -508,6 +539,7 @@ __global__ __launch_bounds__(kCarryWide * kCarryRows) void scan_carry_kernel(Sca
 }
 
 constexpr uint32_t kMostGrid = 1u << 21;  // launches stay below 2^32 threads
+constexpr uint32_t kSeeGrid = 1u << 12;   // workgroups that see to sequences without rows, at most
 constexpr uint32_t kFull = 256;           // walks times blocks of channels from which on scan_rows fills the device
 constexpr uint32_t kFewIterations = 3;    // ... or that are over so soon that three launches are not worth it
 constexpr uint32_t kThreads = 1u << 18;   // threads that ranges are cut for: sixteen wavefronts to a CU
@@ -569,8 +601,8 @@ int launch(ScanArgs a, uint32_t type, const void* v, const void* gate, const voi
       a.ranges > 1 ? ((uint64_t)a.walks * a.ranges * pieces + kRangeBlock - 1) / kRangeBlock : (uint64_t)a.walks * a.blocks;
   if (main_blocks > 0xFFFFFFFFull) return CVLC_ERR_ARG;
   a.main_grid = (uint32_t)std::min<uint64_t>(main_blocks, kMostGrid);
-  const uint32_t more =
-      (a.starts || a.n == 0) && (a.last || a.status) ? std::min((a.n_seq + kRangeBlock - 1) / kRangeBlock, kMostGrid) : 0u;
+  const uint64_t seen = (a.starts || a.n == 0) && (a.last || a.status) ? see_items(a.n_seq, a.last ? a.dim : 1) : 0;
+  const uint32_t more = (uint32_t)std::min<uint64_t>((seen + kRangeBlock / kWave - 1) / (kRangeBlock / kWave), kSeeGrid);
   if (a.main_grid + more == 0) return CVLC_OK;
   by_type(type, [&](auto t) {
     using T = decltype(t);

@@ -4,7 +4,7 @@ import numpy as np
 import pytest
 import torch
 
-import paper_2402_03770_amd.cvlc as cv  # noqa: F401
+import paper_2402_03770_amd.cvlc as cv
 from test_local_step import BF16, DEV, F16, F32, f64
 from test_training import Scan, cuts
 
@@ -81,3 +81,31 @@ def test_gated_scan_whose_gates_forget_everything_keeps_a_nan(lengths, dim):
     s.forward(starts=at)
     bad = np.isnan(f64(s.h))
     assert bad[low + 2:high].all() and bad.sum() == (high - low - 2) * dim and bool(torch.isnan(s.last[j]).all())
+
+
+@gpu
+@pytest.mark.parametrize("dim", [1, 3, 33, 64, 65, 512, 513, 2304, 8192])
+@pytest.mark.parametrize("sequences,every,rows", [(43, 3, 2), (4096, 50, 1), (4097, 50, 1), (9001, 400, 30), (70, 1000, 0)])
+def test_gated_scan_states_of_sequences_without_rows(sequences, every, rows, dim):
+    """Of `sequences` one in `every` has `rows` rows; the others hand their states on, forward and back, at any width."""
+    if sequences * dim > 1 << 23:
+        dim = (1 << 23) // sequences
+    lengths = [rows if j % every == every - 1 else 0 for j in range(sequences)]
+    starts, _ = cuts(lengths)
+    n, at = int(starts[-1]), torch.from_numpy(starts).to(DEV)
+    empty = torch.tensor([k == 0 for k in lengths], device=DEV)
+    s, status = Scan(n, dim, F32, sequences), torch.zeros(1, dtype=torch.int32, device=DEV)
+    s.forward(starts=at, status=status)
+    s.backward(starts=at, status=status)
+    assert status.item() == 0
+    assert torch.equal(s.last[empty], s.h0[empty]) and torch.equal(s.dh0[empty], s.dlast[empty])
+    full = [k for k, x in enumerate(lengths) if x]
+    assert torch.equal(s.last[full], s.h[starts[1:][full] - 1])
+    s.h0 = s.dlast = None
+    s.forward(starts=at)
+    s.backward(starts=at)
+    assert not bool(s.last[empty].any()) and not bool(s.dh0[empty].any())
+    if n:                                                              # without states that are handed on, offsets are looked at all the same
+        at[sequences // 2] = n + 1
+        cv.gated_scan(s.x, s.gate, s.h, s.ws, starts=at, status=status)
+        assert status.item() == cv.DEV_INDEX
