@@ -242,9 +242,9 @@ __device__ __forceinline__ void step_back(const float (&g)[N], const float (&dy)
 
 // ------------------------------------------------------------------------------ every byte once
 // A workgroup's joined steps: `in` is what comes before the thread's rows then.  carry[ch]: what comes before all rows, then
-// what comes after them.
+// what comes after them.  `anew`: whether some A may be kAnew; asking each lengthens the chain, by which 512 x 500 bf16 takes a tenth longer.
 template <uint32_t N>
-__device__ __forceinline__ void join(uint32_t mine, uint32_t width, uint32_t rows, const float (&A)[N], const float (&B)[N], float* sa,
+__device__ __forceinline__ void join(uint32_t mine, uint32_t width, uint32_t rows, bool anew, const float (&A)[N], const float (&B)[N], float* sa,
                                      float* sb, float* carry, float (&in)[N]) {
 #pragma unroll
   for (uint32_t k = 0; k < N; ++k) {
@@ -254,12 +254,18 @@ __device__ __forceinline__ void join(uint32_t mine, uint32_t width, uint32_t row
   __syncthreads();
   if (threadIdx.x < width) {
     float u = carry[threadIdx.x];
+    auto walk = [&](auto asks) {
 #pragma unroll 8
-    for (uint32_t r = 0; r < rows; ++r) {
-      const float x = sa[r * width + threadIdx.x], y = sb[r * width + threadIdx.x];
-      sb[r * width + threadIdx.x] = u;
-      u = chain(x, y, u);
-    }
+      for (uint32_t r = 0; r < rows; ++r) {
+        const float x = sa[r * width + threadIdx.x], y = sb[r * width + threadIdx.x];
+        sb[r * width + threadIdx.x] = u;
+        u = decltype(asks)::value ? chain(x, y, u) : fmaf(x, u, y);
+      }
+    };
+    if (anew)
+      walk(std::true_type{});
+    else
+      walk(std::false_type{});
     carry[threadIdx.x] = u;
   }
   __syncthreads();
@@ -275,7 +281,7 @@ __global__ __launch_bounds__(kScanBlock, 4) void scan_rows_kernel(ScanArgs a, co
   constexpr uint32_t kMarks = kScanBlock * L;
   __shared__ float sa[kScanBlock * N], sb[kScanBlock * N], carry[kGroupsMost * N];
   __shared__ Marks<kMarks> marks;
-  if (blockIdx.x >= a.main_grid) {
+  if (__builtin_expect(blockIdx.x >= a.main_grid, 0)) {
     see_to_empty(a, (blockIdx.x - a.main_grid) * (kScanBlock / kWave) + wave_id(), (gridDim.x - a.main_grid) * (kScanBlock / kWave));
     return;
   }
@@ -347,7 +353,7 @@ __global__ __launch_bounds__(kScanBlock, 4) void scan_rows_kernel(ScanArgs a, co
         if (!WHOLE && anew)
 #pragma unroll
           for (uint32_t k = 0; k < N; ++k) A[k] = kAnew;
-        join<N>(mine, width, rows, A, B, sa, sb, carry, in);
+        join<N>(mine, width, rows, !WHOLE && marked, A, B, sa, sb, carry, in);
 #pragma unroll
         for (uint32_t i = 0; i < L; ++i)
           if (WHOLE || there(i)) {
@@ -410,7 +416,7 @@ template <class T, bool FORWARD, bool APPLY, bool ONCE>
 __global__ __launch_bounds__(kRangeBlock, 4) void scan_range_kernel(ScanArgs a, const T* v, const T* gate, const T* x, const T* h, T* out,
                                                                     T* dgate) {
   constexpr uint32_t N = kPerAccess<T>, P = kBatch<FORWARD, APPLY>;
-  if (APPLY && blockIdx.x >= a.main_grid) {
+  if (APPLY && __builtin_expect(blockIdx.x >= a.main_grid, 0)) {
     see_to_empty(a, (blockIdx.x - a.main_grid) * (kRangeBlock / kWave) + wave_id(), (gridDim.x - a.main_grid) * (kRangeBlock / kWave));
     return;
   }
@@ -501,15 +507,17 @@ __global__ __launch_bounds__(kRangeBlock, 4) void scan_range_kernel(ScanArgs a, 
       some(first, rows, std::false_type{});
   }
   if (!APPLY) {
+    const float mark = a.flat ? kAnew : 0.0f;   // before a sequence that is walked by itself there is nothing to forget
     float2* p = a.partial + (uint64_t)part * a.dim + at;
 #pragma unroll
     for (uint32_t k = 0; k < N; ++k)
-      if (at + k < a.dim) p[k] = float2{anew ? kAnew : A[k], u[k]};
+      if (at + k < a.dim) p[k] = float2{anew ? mark : A[k], u[k]};
   }
 }
 
 // What every range starts from: a workgroup has 16 channels of a walk, its threads 64 pieces of the ranges each.
 constexpr uint32_t kCarryWide = 16, kCarryRows = 64;
+template <bool FLAT>
 __global__ __launch_bounds__(kCarryWide * kCarryRows) void scan_carry_kernel(ScanArgs a) {
   __shared__ float2 steps[kCarryRows][kCarryWide];
   const uint32_t blocks = (a.dim + kCarryWide - 1) / kCarryWide, x = threadIdx.x % kCarryWide, y = threadIdx.x / kCarryWide;
@@ -517,24 +525,25 @@ __global__ __launch_bounds__(kCarryWide * kCarryRows) void scan_carry_kernel(Sca
   const uint32_t per = (a.ranges + kCarryRows - 1) / kCarryRows, from = min(y * per, a.ranges), to = min(from + per, a.ranges);
   const float2* p = a.partial + (uint64_t)walk * a.ranges * a.dim + c;
   float2 all = {1.0f, 0.0f};
+  auto next = [](float2 s, float u) { return FLAT ? chain(s.x, s.y, u) : fmaf(s.x, u, s.y); };
   if (c < a.dim)
 #pragma unroll 8
     for (uint32_t r = from; r < to; ++r) {
       const float2 s = p[(uint64_t)r * a.dim];
-      all = float2{all.x < 0.0f || s.x < 0.0f ? kAnew : all.x * s.x, chain(s.x, s.y, all.y)};
+      all = float2{FLAT && fminf(all.x, s.x) < 0.0f ? kAnew : all.x * s.x, next(s, all.y)};
     }
   steps[y][x] = all;
   __syncthreads();
   if (c >= a.dim) return;
   float u = a.first && !a.flat ? a.first[(uint64_t)walk * a.dim + c] : 0.0f;
 #pragma unroll 8
-  for (uint32_t r = 0; r < y; ++r) u = chain(steps[r][x].x, steps[r][x].y, u);
+  for (uint32_t r = 0; r < y; ++r) u = next(steps[r][x], u);
   float* e = a.enter + (uint64_t)walk * a.ranges * a.dim + c;
 #pragma unroll 8
   for (uint32_t r = from; r < to; ++r) {
     const float2 s = p[(uint64_t)r * a.dim];
     e[(uint64_t)r * a.dim] = u;
-    u = chain(s.x, s.y, u);
+    u = next(s, u);
   }
 }
 
@@ -617,7 +626,7 @@ int launch(ScanArgs a, uint32_t type, const void* v, const void* gate, const voi
       go(past ? scan_rows_kernel<T, FORWARD, true> : scan_rows_kernel<T, FORWARD, false>, a.main_grid + more, kScanBlock);
     } else {
       go(scan_range_kernel<T, FORWARD, false, false>, a.main_grid, kRangeBlock);
-      hipLaunchKernelGGL(scan_carry_kernel, dim3(a.walks * ((a.dim + kCarryWide - 1) / kCarryWide)), dim3(kCarryWide * kCarryRows), 0,
+      hipLaunchKernelGGL(a.flat ? scan_carry_kernel<true> : scan_carry_kernel<false>, dim3(a.walks * ((a.dim + kCarryWide - 1) / kCarryWide)), dim3(kCarryWide * kCarryRows), 0,
                          stream, a);
       go(past ? scan_range_kernel<T, FORWARD, true, true> : scan_range_kernel<T, FORWARD, true, false>, a.main_grid + more, kRangeBlock);
     }
