@@ -55,7 +55,8 @@ class Client:
         self.m, self.v = (torch.zeros(server.flat.numel(), dtype=torch.uint8, device=dev) for _ in range(2))
         params, grads, ms, vs = (self.model.parts(t) for t in (self.model.flat, self.grad, self.m, self.v))
         scales = [torch.zeros(-(-p.numel() // cv.ADAMW_BLOCK), 2, device=dev) for p in params]
-        self.plan = cv.AdamwPlan(params, grads, ms, vs, scales=scales, weight_decays=[decay] * 3 + [0.0] * 2)
+        self.plan = cv.AdamwPlan(params, grads, ms, vs, scales=scales, weight_decays=[decay] * 3 + [0.0] * 2,
+                                 m_by_chance=True)
         self.ws_table = cv.new_workspace(cv.embed_grad_workspace_bytes(n, vocab, dim), dev)
         self.ws_norm = cv.new_workspace(cv.layer_norm_grad_workspace_bytes(n, dim), dev)
         self.ws_scan = cv.new_workspace(cv.gated_scan_workspace_bytes(n, dim, starts.numel() - 1), dev)

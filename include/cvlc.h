@@ -561,14 +561,20 @@ int cvlc_gated_scan_step(uint32_t n, uint32_t dim, const void* d_x, uint64_t x_s
  * Averages of 8 bits are codes of e4m3 (bias 7, largest value 448, no infinity),
  * of m and of sqrt(v), times a scale for each per CVLC_ADAMW_BLOCK values of the
  * tensor: {largest |m| / 448, largest sqrt(v) / 448}, zeros where the largest is
- * below 2^-100.  The weights move by the averages before they are held.  m is
- * rounded to nearest.  sqrt(v) goes to one of the two codes around it, up with
- * the probability of its distance from the lower one in steps of 2^-16 (a step
- * changes it by less than a code, so to nearest it would never move), and to
- * zero only from zero.  Its 16 random bits are those of Philox4x32-10 with key
- * seed and counter (i / 8, 0, t, tensor) for element i: halves of the four words
- * in ascending order, low ones first.  All zeros is where training starts. */
+ * below 2^-100.  The weights move by the averages before they are held.
+ * sqrt(v) goes to one of the two codes around it, up with the probability of its
+ * distance from the lower one in steps of 2^-16 (a step changes it by less than a
+ * code, so to nearest it would never move), and to zero only from zero.  Its 16
+ * random bits are those of Philox4x32-10 with key seed and counter
+ * (i / 8, 0, t, tensor) for element i: halves of the four words in ascending
+ * order, low ones first.  With CVLC_ADAMW_M_BY_CHANCE m does the same by the bits
+ * of counter (i / 8, 1, t, tensor), and goes to zero too: this is what training
+ * for more than some dozens of steps takes.  Without the flag m is rounded to
+ * nearest: it then stays at a code that a step does not take it away from, and a
+ * weight whose gradient has become small beside that moves on at every step, for
+ * good.  All zeros is where training starts. */
 #define CVLC_ADAMW_BLOCK 256u
+#define CVLC_ADAMW_M_BY_CHANCE 1u
 typedef struct cvlc_adamw_tensor_t {
   uint64_t n;           /* elements, 0 allowed, at most 2^35                          */
   float* d_param;       /* n fp32, as a slice of the model's flat vector is           */
@@ -580,6 +586,7 @@ typedef struct cvlc_adamw_tensor_t {
   uint32_t copy_type;   /* CVLC_BF16, CVLC_F16                                        */
   uint32_t state_bits;  /* 32 or 8                                                    */
   float weight_decay;
+  uint32_t flags;       /* 8 bits: 0 or CVLC_ADAMW_M_BY_CHANCE                        */
 } cvlc_adamw_tensor_t;
 
 /* What cvlc_adamw_plan leaves for the steps; the caller keeps it with its workspace. */

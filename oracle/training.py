@@ -24,10 +24,10 @@ def spread(scales, n):
     return np.repeat(np.asarray(scales, np.float64), BLOCK, 0)[:n]
 
 
-def chances(n, seed, step, tensor):
-    """Element i's 16 bits: Philox4x32-10 of (i / 8, 0, step, tensor), the halves of its words, low ones first."""
+def chances(n, seed, step, tensor, word=0):
+    """Element i's 16 bits: Philox4x32-10 of (i / 8, word, step, tensor), the halves of its words, low ones first; word 1 is m's."""
     low = np.uint64(0xFFFFFFFF)
-    c = [np.arange((n + 7) // 8, dtype=np.uint64)] + [np.full((n + 7) // 8, x, np.uint64) for x in (0, step, tensor)]
+    c = [np.arange((n + 7) // 8, dtype=np.uint64)] + [np.full((n + 7) // 8, x, np.uint64) for x in (word, step, tensor)]
     k = [seed & 0xFFFFFFFF, seed >> 32]
     for _ in range(10):
         p, q = c[0] * np.uint64(0xD2511F53), c[2] * np.uint64(0xCD9E8D57)
@@ -44,12 +44,12 @@ def nearest(y):
     return np.where((below < above) | ((below == above) & ((at - 1) % 2 == 0)), at - 1, at)
 
 
-def by_chance(y, chance):
-    """The codes below y >= 0 or above it, above where the chance carries over; none but zeros become zeros."""
+def by_chance(y, chance, least=1):
+    """The codes below y >= 0 or above it, above where the chance carries over; at least `least` unless y is 0 (m's: 0)."""
     at = np.clip(np.searchsorted(CODES, y, side="right") - 1, 0, 126)
     step = np.where(at < 126, CODES[np.minimum(at + 1, 126)] - CODES[at], 1.0)
     up = (y - CODES[at]) / step + chance * 2.0 ** -16 >= 1.0
-    return np.where(y > 0, np.clip(at + up, 1, 126), 0)
+    return np.where(y > 0, np.clip(at + up, least, 126), 0)
 
 
 def adamw(param, grad, m, v, step, lr, betas, eps, decay, grad_scale=1.0, held=False):

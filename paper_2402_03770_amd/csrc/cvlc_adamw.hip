@@ -9,6 +9,9 @@
 // rounding to nearest would hold it where it is for good: it goes up or down by 16
 // random bits, right on average; the codes' relative step of 1/8 at most then is
 // noise, not drift.  It never goes down to zero, where the next step would divide by eps.
+// The same holds for m: to nearest, codes of 1 to 4 never decay at b1 = 0.9 and none does at
+// 0.99, while r does, so a weight whose gradient has ended moves by the same amount
+// at every step.  CVLC_ADAMW_M_BY_CHANCE rounds m as r is, by bits of its own, and down to zero too.
 //
 // Everything is read and written once and nothing is shared between workgroups but
 // the tensors' table: bound by HBM (28 bytes a weight with fp32 gradients and
@@ -43,7 +46,7 @@ struct Entry {
   float* scales;
   void* copy;
   uint32_t first_chunk;
-  uint8_t grad_type, copy_type, bits, spare;
+  uint8_t grad_type, copy_type, bits, flags;
   float decay;
 };
 static_assert(sizeof(Entry) % 8 == 0, "entries are 8-byte granular");
@@ -83,8 +86,8 @@ __host__ __device__ inline void with_step(Rates& r, float lr, double step) {
 }
 
 // The eight 16-bit halves of Philox4x32-10's words (Salmon et al., 2011), low ones first.
-__device__ __forceinline__ void chances(uint32_t c0, uint32_t c2, uint32_t c3, uint32_t k0, uint32_t k1, uint32_t (&out)[kEach]) {
-  uint32_t c1 = 0;
+__device__ __forceinline__ void chances(uint32_t c0, uint32_t c1, uint32_t c2, uint32_t c3, uint32_t k0, uint32_t k1,
+                                        uint32_t (&out)[kEach]) {
 #pragma unroll
   for (uint32_t round = 0; round < 10; ++round) {
     const uint64_t p0 = (uint64_t)0xD2511F53u * c0, p1 = (uint64_t)0xCD9E8D57u * c2;
@@ -131,10 +134,10 @@ __device__ __forceinline__ Pair encode(const float (&y)[kEach]) {
 }
 
 // y >= 0 to one of the two codes around it: up with the probability of its distance from the lower one, in steps of 2^-16,
-// and never to zero unless it is zero.  From 2^-6 on eight codes to an octave, steps of 2^-9 below.
-__device__ __forceinline__ float by_chance(float y, uint32_t chance) {
+// and never below `least` unless it is zero.  From 2^-6 on eight codes to an octave, steps of 2^-9 below.
+__device__ __forceinline__ float by_chance(float y, uint32_t chance, float least) {
   const float normal = __uint_as_float((__float_as_uint(y) + (chance << 4)) & 0xFFF00000u);
-  const float small = fmaxf(floorf(y * 512.0f + (float)chance * 0x1p-16f) * 0x1p-9f, 0x1p-9f);
+  const float small = fmaxf(floorf(y * 512.0f + (float)chance * 0x1p-16f) * 0x1p-9f, least);
   const float z = y >= 0x1p-6f ? normal : small;
   return y > 0.0f ? fminf(z, kTop) : 0.0f;
 }
@@ -250,11 +253,16 @@ __device__ __forceinline__ void step_each(const Entry& e, uint32_t tensor, const
     top_q = top_q >= kTiny ? top_q : 0.0f;
     const float inv_m = top_m > 0.0f ? 1.0f / top_m * kTop : 0.0f, inv_q = top_q > 0.0f ? 1.0f / top_q * kTop : 0.0f;
     uint32_t chance[kEach];
-    chances((uint32_t)(at / kEach), r.step, tensor, r.k0, r.k1, chance);
+    chances((uint32_t)(at / kEach), 0, r.step, tensor, r.k0, r.k1, chance);
 #pragma unroll
     for (uint32_t i = 0; i < kEach; ++i) {
       m[i] = fminf(fmaxf(m[i] * inv_m, -kTop), kTop);
-      q[i] = by_chance(fminf(q[i] * inv_q, kTop), chance[i]);
+      q[i] = by_chance(fminf(q[i] * inv_q, kTop), chance[i], 0x1p-9f);
+    }
+    if (e.flags & CVLC_ADAMW_M_BY_CHANCE) {
+      chances((uint32_t)(at / kEach), 1, r.step, tensor, r.k0, r.k1, chance);
+#pragma unroll
+      for (uint32_t i = 0; i < kEach; ++i) m[i] = copysignf(by_chance(fabsf(m[i]), chance[i], 0.0f), m[i]);
     }
     const Pair cm = encode(m), cv = encode(q);
     if (count == kEach) {
@@ -329,7 +337,7 @@ bool buffers_meet(uint32_t count, const cvlc_adamw_tensor_t* tensors) {
 
 bool tensor_ok(const cvlc_adamw_tensor_t& t) {
   if (t.state_bits != 8 && t.state_bits != 32) return false;
-  if (!type_known(t.grad_type) || !std::isfinite(t.weight_decay)) return false;
+  if (!type_known(t.grad_type) || !std::isfinite(t.weight_decay) || (t.flags & ~CVLC_ADAMW_M_BY_CHANCE)) return false;
   if (t.d_copy && t.copy_type != CVLC_BF16 && t.copy_type != CVLC_F16) return false;
   if (t.n == 0) return true;
   if (t.n > 1ull << 35) return false;  // its eighths are counted in 32 bits
@@ -388,7 +396,7 @@ int cvlc_adamw_plan(uint32_t count, const cvlc_adamw_tensor_t* tensors, void* d_
     for (uint32_t i = 0; i < u.count; ++i) {
       const cvlc_adamw_tensor_t& t = tensors[first + i];
       u.entry[i] = Entry{t.n, t.d_param, t.d_grad, t.d_m, t.d_v, t.d_scales, t.d_copy, at, (uint8_t)t.grad_type,
-                         (uint8_t)t.copy_type, (uint8_t)t.state_bits, 0, t.weight_decay};
+                         (uint8_t)t.copy_type, (uint8_t)t.state_bits, (uint8_t)t.flags, t.weight_decay};
       at += (uint32_t)chunks_of(t.n);
       most = std::max(most, chunks_of(t.n));
       moved += t.n * (4u + type_bytes(t.grad_type) + (t.d_copy ? 2u : 0u) + (t.state_bits == 32 ? 8u : 2u));

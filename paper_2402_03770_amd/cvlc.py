@@ -6,6 +6,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import warnings
 from typing import List, Optional, Sequence
 
 import torch
@@ -23,6 +24,7 @@ GRAD_ACCUMULATE = 1
 DISTILL_LOGPROBS = 1
 DISTILL_MAX_K = 1024
 ADAMW_BLOCK = 256
+ADAMW_M_BY_CHANCE = 1
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libcvlc.so")
@@ -61,7 +63,7 @@ class AdamwTensor(C.Structure):
     """cvlc_adamw_tensor_t"""
     _fields_ = [("n", C.c_uint64), ("param", C.c_void_p), ("grad", C.c_void_p), ("m", C.c_void_p), ("v", C.c_void_p),
                 ("scales", C.c_void_p), ("copy", C.c_void_p), ("grad_type", C.c_uint32), ("copy_type", C.c_uint32),
-                ("state_bits", C.c_uint32), ("weight_decay", C.c_float)]
+                ("state_bits", C.c_uint32), ("weight_decay", C.c_float), ("flags", C.c_uint32)]
 
 
 class AdamwPlanData(C.Structure):
@@ -763,12 +765,14 @@ class AdamwPlan:
     """cvlc_adamw_plan: what adamw() steps over.  Lists of one entry per tensor, contiguous, of equal numbers of elements:
     `params` float32, `grads` of any type, `m` and `v` both float32 or, for averages in 8 bits, both float8_e4m3fn or
     uint8, with `scales` float32 (ceil(n / ADAMW_BLOCK), 2).  `copies`: None, or per tensor None or bfloat16 or float16.
-    Keeps the tensors, which must stay where they are, and a workspace of its own; waits until it is laid out."""
+    `m_by_chance`: averages in 8 bits have m rounded by chance, as sqrt(v) always is, which is right on average; False: to nearest,
+    where it stands still while changes are small, so that weights whose gradient has ended go on moving (None: the same, with
+    a warning).  Keeps the tensors, which must stay where they are, and a workspace of its own; waits until it is laid out."""
 
     def __init__(self, params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], m: Sequence[torch.Tensor],
                  v: Sequence[torch.Tensor], scales: Optional[Sequence[Optional[torch.Tensor]]] = None,
                  copies: Optional[Sequence[Optional[torch.Tensor]]] = None,
-                 weight_decays: Optional[Sequence[float]] = None):
+                 weight_decays: Optional[Sequence[float]] = None, m_by_chance: Optional[bool] = None):
         what, count = "cvlc_adamw_plan", len(params)
         scales = scales if scales is not None else [None] * count
         copies = copies if copies is not None else [None] * count
@@ -793,12 +797,16 @@ class AdamwPlan:
                 _refuse(what, f"tensor {i}: scales go with averages of 8 bits")
             table[i] = AdamwTensor(n, p.data_ptr(), g.data_ptr(), a.data_ptr(), b.data_ptr(),
                                    _vector(what, "scales", s, (-(-n // ADAMW_BLOCK), 2)), c.data_ptr() if c is not None else None,
-                                   _TYPES[g.dtype], _TYPES[c.dtype] if c is not None else 0, bits, decay)
+                                   _TYPES[g.dtype], _TYPES[c.dtype] if c is not None else 0, bits, decay,
+                                   ADAMW_M_BY_CHANCE if m_by_chance and bits == 8 else 0)
         self.tensors = (list(params), *(list(x) for x in lists[:-1]))
         every = [t for x in self.tensors for t in x if t is not None]
         stream = _stream_of(what, *every)
         if torch.cuda.is_current_stream_capturing():
             _refuse(what, "a plan is made before a graph is captured")
+        if m_by_chance is None and any(t.state_bits == 8 for t in table):
+            warnings.warn("AdamwPlan: m in 8 bits is rounded to nearest, so weights whose gradient has ended go on moving; "
+                          "m_by_chance=True rounds it by chance", stacklevel=2)
         self.device, self.data = params[0].get_device(), AdamwPlanData()
         self.workspace = new_workspace(lib().cvlc_adamw_workspace_bytes(count, table), params[0].device)
         _check(lib().cvlc_adamw_plan(count, table, self.workspace.data_ptr(), self.workspace.numel(), C.byref(self.data), stream), what)

@@ -1,12 +1,16 @@
 """What a client trains with, on inputs and sizes beside the ordinary: values that are not finite, sequences without rows, averages
 over thousands of steps, calls that the caches do not hold.  Oracles as in test_training.py."""
+import ctypes as C
+import warnings
+
 import numpy as np
 import pytest
 import torch
 
 import paper_2402_03770_amd.cvlc as cv
+from oracle import training as ref
 from test_local_step import BF16, DEV, F16, F32, f64
-from test_training import Scan, cuts
+from test_training import Scan, Tensors, check_adamw, cuts
 
 gpu = pytest.mark.gpu
 
@@ -109,3 +113,115 @@ def test_gated_scan_states_of_sequences_without_rows(sequences, every, rows, dim
         at[sequences // 2] = n + 1
         cv.gated_scan(s.x, s.gate, s.h, s.ws, starts=at, status=status)
         assert status.item() == cv.DEV_INDEX
+
+
+# ----------------------------------------------------------------------------- AdamW
+@gpu
+@pytest.mark.parametrize("grad,copy", [(F32, None), (BF16, BF16), (F16, F16)])
+@pytest.mark.parametrize("sizes", [[1], [255, 256, 257], [7, 0, 513, 1, 2048, 30], [8193, 20000]], ids=str)
+def test_adamw_m_by_chance(grad, copy, sizes):
+    """m's codes are those that its chances say; everything else is, bit by bit, what it is without."""
+    t, same = (Tensors(sizes, 8, grad, copy, offset=3, seed=len(sizes)) for _ in range(2))
+    decays, seed, betas = [0.1 * (i % 3) for i in range(len(sizes))], 2 ** 40 + 5, (0.9, 0.999)
+    plans = [cv.AdamwPlan(x.param, x.grad, x.m, x.v, scales=x.scales, copies=x.copy, weight_decays=decays, m_by_chance=on)
+             for x, on in ((t, True), (same, False))]
+    for step in (1, 2, 1000):
+        for a, b in zip(same.m, t.m):
+            a.copy_(b)
+        before = [t.read(i) for i in range(len(sizes))]
+        for plan in plans:
+            cv.adamw(plan, step, 1e-2, betas=betas, grad_scale=0.7, seed=seed)
+        check_adamw(same, before, decays, step, 1e-2, betas, 1e-8, 0.7, seed, copy)
+        for a, b in zip((*t.param, *t.v, *t.scales, *(t.copy or [])), (*same.param, *same.v, *same.scales, *(same.copy or []))):
+            assert torch.equal(a, b)
+        for i, (old, decay) in enumerate(zip(before, decays)):
+            _, _, m, off, *_ = ref.adamw(*old, step, 1e-2, betas, 1e-8, decay, 0.7, True)
+            top = ref.spread(f64(t.scales[i])[:, :1], m.size)[:, 0]
+            rel = np.where(m != 0, off / np.maximum(np.abs(m), 1e-300), 0.0) + 6 * ref.U
+            with np.errstate(divide="ignore", invalid="ignore"):
+                y = np.where(top > 0, np.abs(m) / top, 0.0)
+            # beyond the values' own error a step of 2^-9 and its chance have a rounding in the sum of up to 8
+            chance = ref.chances(m.size, seed, step, i, word=1)
+            low, high = (ref.by_chance(np.minimum(y * (1 + s * rel), 448.0), np.clip(chance + s * 2.0 ** -4, 0, 65535.9375), least=0) for s in (-1, 1))
+            codes = t.m[i].cpu().numpy().astype(np.int64)
+            assert np.all((low <= codes & 127) & (codes & 127 <= high)) and np.sum(low != high) <= 1 + 0.02 * m.size
+            assert np.all((codes & 127 == 0) | ((codes >= 128) == (m < 0)))
+
+
+@gpu
+@pytest.mark.parametrize("betas", [(0.9, 0.95), (0.95, 0.99), (0.99, 0.999)], ids=str)
+@pytest.mark.parametrize("dim", [64, 251])
+def test_adamw_8bit_weights_whose_gradient_ends_come_to_rest(dim, betas):
+    """Of every four rows of a table one keeps getting gradients, three do not after step 20, beside it in a block.  The mean of a
+    code that is rounded by chance goes as the average itself does, by beta1 a step, from 448 at most; a code that is not zero is
+    2^-9 at least, so one that lasts for k steps has a probability of 448 * 512 * beta1^k, and as many times more as its block's
+    scale has become smaller by: less than 2^-36 after `still` of them where that is less than 16.  In blocks without a row that goes
+    on the scales vanish with what they hold.  From there on the weights are where they are, to the last bit."""
+    rows, n = 64, 64 * dim
+    still = int(np.ceil(-np.log(448.0 * 512 * 2.0 ** 40 * n) / np.log(betas[0])))
+    gen = torch.Generator().manual_seed(dim)
+    param, grad = torch.randn(n, generator=gen).to(DEV), torch.empty(n, device=DEV)
+    m, v = (torch.zeros(n, dtype=torch.uint8, device=DEV) for _ in range(2))
+    plan = cv.AdamwPlan([param], [grad], [m], [v], scales=[torch.zeros(-(-n // 256), 2, device=DEV)], m_by_chance=True)
+    ended = (torch.arange(rows, device=DEV) % 4 != 0).repeat_interleave(dim)
+    blocks = torch.nn.functional.pad(~ended, (0, -n % 256)).view(-1, 256).any(1)      # with a row that goes on
+    beside = ended & blocks.repeat_interleave(256)[:n]
+    gen = torch.Generator(DEV).manual_seed(1)
+    start = param.clone()
+    for step in range(1, 20 + still + 400):
+        grad.normal_(generator=gen)
+        if step > 20:
+            grad[ended] = 0.0
+        cv.adamw(plan, step, 1e-3, betas=betas, seed=5)
+        if step == 20:
+            assert bool((m[beside] & 127).any())
+        if step == 20 + still:
+            assert not bool((m[beside] & 127).any())
+            rest = param.clone()
+    assert torch.equal(param[ended], rest[ended])
+    assert (param[~ended] != rest[~ended]).float().mean() > 0.99 and (param[ended] != start[ended]).float().mean() > 0.99
+
+
+@gpu
+def test_adamw_8bit_m_moves_on_average():
+    """A gradient that is 0.7 of the average: m must come down to it, by less than half a code a step."""
+    n, held, b1 = 256 * 64, 64.0, 0.9
+    t = Tensors([n], 8, F32, None, offset=0, seed=1)
+    t.m[0].fill_(int(ref.nearest(np.array([held]))[0]))
+    t.m[0][::256] = 0x7E                                               # the blocks' largest, which holds the scale where it is
+    t.v[0].zero_()
+    t.scales[0].fill_(1.0)
+    t.grad[0].fill_(0.7 * held)
+    t.grad[0][::256] = 448.0
+    plan = cv.AdamwPlan(t.param, t.grad, t.m, t.v, scales=t.scales, m_by_chance=True)
+    for k, want in ((3, 0.7 * held + 0.3 * held * b1 ** 3), (100, 0.7 * held)):
+        for step in range(1, k + 1):
+            cv.adamw(plan, step + 100 * k, 0.0, betas=(b1, 0.99), seed=3)
+        got = (ref.values(t.m[0].cpu()) * ref.spread(f64(t.scales[0]), n)[:, 0]).reshape(-1, 256)[:, 1:]
+        # Between 32 and 64 codes are 4 apart: a rounding's variance is 4 at most, and what is left of all before it adds up to
+        # 4 / (1 - b1^2); 6 deviations of the mean, a chance's step of 2^-16 of 4 for each of 1 / (1 - b1) roundings, what is left
+        # of the start after the steps, and fp32's roundings.
+        tol = 6 * np.sqrt(4 / (1 - b1 ** 2) / got.size) + 4 * 2.0 ** -16 / (1 - b1) + (0.3 * held * b1 ** 103 if k == 100 else 0) + 1e-4
+        assert abs(got.mean() - want) <= tol
+
+
+@gpu
+def test_adamw_m_by_chance_is_a_choice():
+    """A warning where averages in 8 bits come without it; flags that are not there are refused."""
+    t = Tensors([300], 8, F32, None, offset=0, seed=1)
+    lists, other = (t.param, t.grad, t.m, t.v), Tensors([300], 32, F32, None, offset=0, seed=1)
+    with pytest.warns(UserWarning, match="m_by_chance"):
+        cv.AdamwPlan(*lists, scales=t.scales)
+    with warnings.catch_warnings():
+        warnings.simplefilter("error")
+        for on in (True, False):
+            cv.AdamwPlan(*lists, scales=t.scales, m_by_chance=on)
+        for on in (None, True):
+            cv.AdamwPlan(other.param, other.grad, other.m, other.v, m_by_chance=on)
+
+
+def test_adamw_flags_that_are_not_there():
+    ok, data = 1 << 20, cv.AdamwPlanData()
+    for flags, want in ((2, cv.ERR_ARG), (1 << 8, cv.ERR_ARG), (3, cv.ERR_ARG)):
+        t = (cv.AdamwTensor * 1)(cv.AdamwTensor(100, ok, ok + 4096, ok + 8192, ok + 16384, ok + 32768, None, 1, 0, 8, 0.0, flags))
+        assert cv.lib().cvlc_adamw_plan(1, t, ok + (1 << 20), 1 << 20, C.byref(data), None) == want
