@@ -555,8 +555,9 @@ int cvlc_gated_scan_step(uint32_t n, uint32_t dim, const void* d_x, uint64_t x_s
  * grad_scale and t the step's number, element by element,
  *   m <- beta1 m + (1 - beta1) g,   v <- beta2 v + (1 - beta2) g^2,
  *   p <- p (1 - lr weight_decay) - lr / (1 - beta1^t) * m / (sqrt(v) / sqrt(1 - beta2^t) + eps).
- * An element whose g^2 is not finite in fp32 keeps its weight and averages and
- * sets CVLC_DEV_NONFINITE.
+ * An element whose g^2, m, v or new weight is not finite in fp32 keeps its weight
+ * and averages (of 8 bits as near as its block's new scale has them) and sets
+ * CVLC_DEV_NONFINITE.
  *
  * Averages of 8 bits are codes of e4m3 (bias 7, largest value 448, no infinity),
  * of m and of sqrt(v), times a scale for each per CVLC_ADAMW_BLOCK values of the

@@ -216,17 +216,23 @@ __device__ __forceinline__ void step_each(const Entry& e, uint32_t tensor, const
     for (uint32_t i = 0; i < kEach; ++i) v[i] *= v[i];
   }
   const float keep = 1.0f - r.lr * e.decay;
+  bool some = false;
 #pragma unroll
   for (uint32_t i = 0; i < kEach; ++i) {
     const float gi = g[i] * r.grad_scale;
     const float mi = m[i] * r.b1 + gi * r.rest1, vi = v[i] * r.b2 + gi * gi * r.rest2;
-    const bool fine = vi < INFINITY;  // neither is a NaN
-    bad |= !fine;
+    q[i] = sqrtf(vi);
+    const float to = p[i] * keep - r.rate * (mi / (q[i] * r.root + r.eps));
+    const bool fine = fabsf(to) + vi < INFINITY;  // and neither they nor m is a NaN
+    some |= !fine;
     m[i] = fine ? mi : m[i];
     v[i] = fine ? vi : v[i];
-    q[i] = sqrtf(v[i]);
-    const float to = p[i] * keep - r.rate * (m[i] / (q[i] * r.root + r.eps));
     p[i] = fine ? to : p[i];
+  }
+  if (some) {
+    bad = true;
+#pragma unroll
+    for (uint32_t i = 0; i < kEach; ++i) q[i] = sqrtf(v[i]);
   }
   store_each<ONCE>(e.param + at, count, p);
   if (e.copy) {

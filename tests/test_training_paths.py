@@ -225,3 +225,36 @@ def test_adamw_flags_that_are_not_there():
     for flags, want in ((2, cv.ERR_ARG), (1 << 8, cv.ERR_ARG), (3, cv.ERR_ARG)):
         t = (cv.AdamwTensor * 1)(cv.AdamwTensor(100, ok, ok + 4096, ok + 8192, ok + 16384, ok + 32768, None, 1, 0, 8, 0.0, flags))
         assert cv.lib().cvlc_adamw_plan(1, t, ok + (1 << 20), 1 << 20, C.byref(data), None) == want
+
+
+@gpu
+@pytest.mark.parametrize("bits", [32, 8])
+def test_adamw_keeps_weights_from_what_is_not_finite(bits):
+    """Rates from the device that are no numbers, averages and weights that are none, steps beyond fp32: told of, and such elements
+    stay; the others go on."""
+    t = Tensors([600], bits, F32, None, offset=0, seed=2)
+    plan = cv.AdamwPlan(t.param, t.grad, t.m, t.v, scales=t.scales, m_by_chance=True)
+    status = torch.zeros(1, dtype=torch.int32, device=DEV)
+    start = t.param[0].clone()
+    for now in ((5.0, float("nan"), 1.0), (5.0, float("inf"), 1.0), (5.0, 1e-3, float("nan")), (1.0, 3e38, 1.0)):       # the last: a rate of 3e38 / (1 - 0.9)
+        cv.adamw(plan, 0, 0.0, now=torch.tensor(now, device=DEV), status=status)
+        assert status.item() == cv.DEV_NONFINITE
+        assert torch.equal(t.param[0], start)
+        status.zero_()
+    t.param[0][7] = float("inf")
+    if bits == 32:
+        t.m[0][9], t.m[0][11], t.v[0][13] = float("nan"), -float("inf"), float("nan")
+    else:
+        t.m[0][9] = t.v[0][13] = 0x7F
+        t.m[0][11] = 0xFF
+    odd = [7, 9, 11, 13]
+    start = t.param[0].clone()
+    cv.adamw(plan, 5, 1e-3, status=status)
+    others = [i for i in range(600) if i not in odd]
+    assert status.item() == cv.DEV_NONFINITE and torch.equal(t.param[0][odd], start[odd])
+    assert bool(torch.isfinite(t.param[0][others]).all()) and (t.param[0][others] != start[others]).float().mean() > 0.9
+    t.param[0][7] = 1.0
+    status.zero_()
+    if bits == 8:                                                      # codes that stood for nothing do no longer
+        cv.adamw(plan, 6, 1e-3, status=status)
+        assert status.item() == 0
