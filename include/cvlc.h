@@ -453,7 +453,7 @@ int cvlc_distill_grad(uint32_t n, uint32_t vocab, const void* d_logits, uint32_t
  *   d_labels   n tokens of id_bytes = 4 or 8 bytes, signed.  A negative one is
  *              padding; one at or beyond `vocab` sets CVLC_DEV_INDEX and counts as
  *              padding too
- *   d_weights  n fp32 w_i, finite, or NULL (all 1)
+ *   d_weights  n fp32 w_i, finite, scale w_i too, or NULL (all 1)
  *   d_loss     NULL, or n fp32
  *   d_stats    NULL, or n times {m, S}, fp32, 8-byte aligned, for
  *              cvlc_linear_xent_grad: the largest logit and the sum of exp(z - m)
@@ -488,7 +488,7 @@ int cvlc_linear_xent(uint32_t n, uint32_t vocab, uint32_t dim, const void* d_hid
  *              (without d_dtable: of the table's type); holds no status word
  * G is rounded to the type of 16-bit results; for fp32 results to 2^-18 of itself
  * beside bfloat16 matrices, else to 2^-23.  Beside others than bfloat16 it loses
- * what is below 2^-38 of scale times the largest weight. */
+ * what is below 2^-38 of scale times the largest weight, or below 2^-150. */
 size_t cvlc_linear_xent_grad_workspace_bytes(uint32_t n, uint32_t vocab, uint32_t dim, uint32_t type, uint32_t dtable_type);
 int cvlc_linear_xent_grad(uint32_t n, uint32_t vocab, uint32_t dim, const void* d_hidden, uint64_t hidden_stride,
                           const void* d_table, uint64_t table_stride, uint32_t type, const void* d_labels,

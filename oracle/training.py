@@ -176,13 +176,13 @@ def linear_xent(hidden, table, labels, scale=1.0, weights=None, cut=0.0):
 
 def linear_xent_grad(G, off_G, h, t, round_h, round_t, cut=0.0, start=None):
     """dh and dT and how far off: G is rounded (`round_h`, `round_t` of itself, beside what fp16 may lose below), terms are
-    added in fp32 in any order, in pieces that are added in turn."""
+    added in fp32 in any order, in pieces that are added in turn; results have steps of 2^-149."""
     n, vocab = G.shape
-    lost = 2.0 ** -37 * np.abs(G).max() if G.size else 0.0
+    lost = 2.0 ** -37 * np.abs(G).max() + 2.0 ** -150 if G.size else 0.0
     dh, dt = G @ t, G.T @ h
     size = np.abs(G)
-    off_h = (off_G + round_h * size + lost) @ np.abs(t) + ((vocab + 8) * U + cut) * (size @ np.abs(t)) + 3 * U * np.abs(dh)
-    off_t = (off_G + round_t * size + lost).T @ np.abs(h) + ((n + 8) * U + cut) * (size.T @ np.abs(h)) + 3 * U * np.abs(dt)
+    off_h = (off_G + round_h * size + lost) @ np.abs(t) + ((vocab + 8) * U + cut) * (size @ np.abs(t)) + 3 * U * np.abs(dh) + 2.0 ** -149
+    off_t = (off_G + round_t * size + lost).T @ np.abs(h) + ((n + 8) * U + cut) * (size.T @ np.abs(h)) + 3 * U * np.abs(dt) + 2.0 ** -149
     if cut:
         off_h = off_h + 2.0 ** -38 * np.abs(t).max() * size.sum(1)[:, None]
         off_t = off_t + 2.0 ** -38 * np.abs(h).max() * size.sum(0)[:, None]

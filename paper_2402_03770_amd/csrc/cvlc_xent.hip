@@ -11,8 +11,8 @@
 //     2^-23 of itself or 2^-39 of the largest.  An fp32 matrix instruction has a sixteenth of the rate.
 //   - G, in one plane where the result is of 16 bits (its rounding of 2^-9 or 2^-12 of a term is what the result's own is), in
 //     two for fp32 results (2^-18 in bfloat16, 2^-23 in fp16).
-// G is scaled so that the largest weight becomes 2^13: then neither tiny weights nor fp16 lose its small entries, and the
-// label's entry, softmax - 1, is next to a value that every type has.
+// G is scaled so that the largest weight becomes 2^13, by 2^126 at most: then neither tiny weights nor fp16 lose its small
+// entries, and the label's entry, softmax - 1, is next to a value that every type has.
 //
 // The loss's product ends in every tile's (max, sum of exponentials) per row, joined in order by a second launch.  The
 // gradients go over the vocabulary in pieces of a few thousand tokens whose G fits the last-level cache.
@@ -34,7 +34,8 @@ typedef uint16_t Half;  // 16 bits of either type
 constexpr uint32_t kDepth = 64;    // K is padded to whole ones of the deepest tiles
 constexpr uint32_t kStep = 32;     // K of a matrix instruction
 constexpr uint32_t kPadTo = 256;   // vocabulary pieces are whole tiles
-constexpr float kLift = 0x1p13f;   // G's largest entries
+constexpr float kLift = 0x1p13f;   // G's largest entries ...
+constexpr float kMostLift = 0x1p126f;   // ... where they do not take more than this; its inverse is a normal value
 
 uint64_t pad_to(uint64_t x, uint64_t to) { return (x + to - 1) / to * to; }
 
@@ -71,6 +72,9 @@ struct Factors {
   float back;               // ... and by which its products are then
   float up[2], down[2];     // the same of hidden rows and table, powers of two
 };
+
+// What takes a product of G and one of the scaled matrices back; not infinite, which 0 times it would show.
+__device__ __forceinline__ float back_of(const Factors& f, uint32_t side) { return fminf(f.back * f.down[side], 0x1.fffffep127f); }
 
 constexpr uint32_t kSurveyBlock = 256, kSurveyGrid = 1024, kSurveyEach = 4096, kSurveyAlone = 1u << 14;
 struct Matrix {
@@ -136,9 +140,9 @@ __global__ __launch_bounds__(1024) void factors_kernel(Rows who, float scale, co
   if (threadIdx.x) return;
   for (uint32_t k = 0; k < 3; ++k)
     for (uint32_t w = 1; w < 16; ++w) m[k] = fmaxf(m[k], most[k][w]);
-  const bool some = m[0] >= 0x1p-100f && m[0] <= 0x1p100f;
-  factors->grad = some ? kLift / m[0] : 1.0f;
-  factors->back = some ? m[0] / kLift : 1.0f;
+  const bool some = m[0] > 0.0f && m[0] < INFINITY, tiny = !(kLift / m[0] < kMostLift);
+  factors->grad = !some ? 1.0f : tiny ? kMostLift : kLift / m[0];
+  factors->back = !some ? 1.0f : tiny ? 1.0f / kMostLift : m[0] / kLift;
   for (uint32_t k = 0; k < 2; ++k) {
     const float top = m[k + 1];
     const int e = top > 0.0f && top < INFINITY ? min(max(14 - ilogbf(top), -100), 100) : 0;
@@ -717,7 +721,7 @@ struct TableEnd {
 
   template <class S>
   __device__ __forceinline__ void operator()(const Four (&acc)[S::MT][S::NT], const Spot& s, uint8_t*) const {
-    const float f = scaled ? factors->back * factors->down[0] : factors->back;
+    const float f = scaled ? back_of(*factors, 0) : factors->back;
 #pragma unroll
     for (uint32_t j = 0; j < S::NT; ++j) {
       const uint32_t v = s.n + j * 16;
@@ -765,7 +769,7 @@ __global__ __launch_bounds__(256) void join_kernel(JoinArgs a, TO* out) {
   const uint32_t blocks = (a.dim + 1023) / 1024;
   const uint32_t c = blockIdx.x % blocks * 1024 + threadIdx.x * 4;
   if (c >= a.dim) return;
-  const float f = a.side < 2 ? a.factors->back * a.factors->down[a.side] : a.factors->back;
+  const float f = a.side < 2 ? back_of(*a.factors, a.side) : a.factors->back;
   for (uint32_t i = blockIdx.x / blocks; i < a.rows; i += gridDim.x / blocks) {
     float x[4] = {};
     if (!a.of_hidden || a.who.live(i)) {

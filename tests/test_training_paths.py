@@ -10,7 +10,7 @@ import torch
 import paper_2402_03770_amd.cvlc as cv
 from oracle import training as ref
 from test_local_step import BF16, DEV, F16, F32, f64
-from test_training import Scan, Tensors, check_adamw, cuts
+from test_training import Scan, Tensors, Xent, check_adamw, cuts
 
 gpu = pytest.mark.gpu
 
@@ -258,3 +258,19 @@ def test_adamw_keeps_weights_from_what_is_not_finite(bits):
     if bits == 8:                                                      # codes that stood for nothing do no longer
         cv.adamw(plan, 6, 1e-3, status=status)
         assert status.item() == 0
+
+
+# ----------------------------------------------------------------------------- the loss over a vocabulary
+@gpu
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("n", [20, 80])
+@pytest.mark.parametrize("weight,scale", [(1e32, 1.0), (3e36, -0.5), (1e-32, 1.0), (1e-36, -0.5), (1e-39, 1.0), (1e-44, 1.0)])
+def test_linear_xent_of_weights_at_the_ends_of_fp32(dtype, n, weight, scale):
+    """Whatever finite weights are, fp32 results are where fp32 has them; in fp16 dhidden of large ones is beyond the type."""
+    x = Xent(n, 64, 300, dtype, F32, padding=0.0)
+    x.weights = torch.full((n,), weight, device=DEV)
+    x.weights[::3] *= 1e-3
+    x.forward(scale)
+    with_hidden = dtype != F16 or weight < 1
+    x.backward(scale, dhidden=with_hidden)
+    x.check(scale, dhidden=with_hidden)
