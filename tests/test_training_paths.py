@@ -9,7 +9,7 @@ import torch
 
 import paper_2402_03770_amd.cvlc as cv
 from oracle import training as ref
-from test_local_step import BF16, DEV, F16, F32, f64
+from test_local_step import BF16, DEV, F16, F32, assert_near, f64
 from test_training import Scan, Tensors, Xent, check_adamw, cuts
 
 gpu = pytest.mark.gpu
@@ -274,3 +274,83 @@ def test_linear_xent_of_weights_at_the_ends_of_fp32(dtype, n, weight, scale):
     with_hidden = dtype != F16 or weight < 1
     x.backward(scale, dhidden=with_hidden)
     x.check(scale, dhidden=with_hidden)
+
+
+@gpu
+@pytest.mark.parametrize("dtype,dtable,n,dim,vocab,extra", [(BF16, F32, 70_001, 40, 300, 3), (F16, F16, 70_001, 40, 300, 0), (F32, F32, 66_000, 24, 130, 1),
+                                                            (BF16, F32, 20_001, 1030, 2100, 0)])
+def test_linear_xent_of_very_many_tokens(dtype, dtable, n, dim, vocab, extra):
+    x = Xent(n, dim, vocab, dtype, dtable, extra)
+    x.forward()
+    x.backward()
+    x.check()
+
+
+# ----------------------------------------------------------------------------- more than the caches hold
+@gpu
+@pytest.mark.parametrize("bits,grad,copy,by_chance,n", [(32, F32, None, False, 5_500_001), (32, BF16, F16, False, 6_500_003), (8, F32, BF16, True, 9_500_001),
+                                                        (8, BF16, None, False, 11_000_007)])
+def test_adamw_of_more_than_the_caches_hold(bits, grad, copy, by_chance, n):
+    """Three tensors at odd addresses whose step goes past the caches' order, bit by bit as each of them by itself, where it does not."""
+    g = torch.Generator(DEV).manual_seed(n)
+
+    def new(dtype, make):
+        flat = torch.zeros(n + 3, dtype=dtype, device=DEV)
+        flat[3:] = make.to(dtype)
+        return flat[3:]
+
+    def averages():
+        if bits == 32:
+            return [new(F32, torch.randn(n, device=DEV, generator=g)), new(F32, torch.rand(n, device=DEV, generator=g) + 0.3), None]
+        codes = [new(torch.uint8, torch.randint(0, 127, (n,), device=DEV, generator=g)) for _ in range(2)]
+        return codes + [torch.rand(-(-n // 256), 2, device=DEV, generator=g) * 1e-2]
+
+    def tensors():
+        return [new(F32, torch.randn(n, device=DEV, generator=g)), new(grad, torch.randn(n, device=DEV, generator=g)), *averages(),
+                new(copy, torch.zeros(n, device=DEV)) if copy is not None else None]
+
+    def step(parts):
+        lists = [list(x) for x in zip(*parts)]
+        plan = cv.AdamwPlan(*lists[:4], scales=lists[4], copies=lists[5], weight_decays=[0.1] * len(parts), m_by_chance=by_chance)
+        for t in (1, 2):
+            cv.adamw(plan, t, 1e-2, seed=77)
+        return plan.data.moved
+
+    together = [tensors() for _ in range(3)]
+    alone = [[None if t is None else t.clone() for t in x] for x in together]
+    empty = [None if t is None else t[:0].clone() for t in alone[0]]   # keep the others' numbers, which their chances go by
+    assert step(together) > 256_000_000
+    for i, x in enumerate(alone):
+        assert step([empty] * i + [x]) < 256_000_000
+        for a, b in zip(together[i], x):
+            assert a is None or torch.equal(a, b)
+
+
+@gpu
+@pytest.mark.parametrize("dtype,sequences,length,starts", [(BF16, 16, 2810, False), (F32, 8, 2750, False), (F16, 7, 45_000, True), (F32, 5, 22_000, True)])
+def test_gated_scan_of_more_than_the_caches_hold(dtype, sequences, length, starts):
+    """Every row once, and ranges, past the caches' order, rows at odd addresses: some channels against the formulas, no byte beside them."""
+    dim = 1001
+    rng = np.random.default_rng(3)
+    lengths = [length] * sequences if not starts else np.diff([0, *np.sort(rng.integers(0, length, sequences - 1)), length]).tolist()
+    at, bounds = cuts(lengths)
+    n = int(at[-1])
+    s = Scan(n, dim, dtype, sequences, extra=2, offset=1)
+    assert n * dim * s.x.element_size() * 3 > 256_000_000
+    cut = dict(starts=torch.from_numpy(at).to(DEV)) if starts else dict(sequences=sequences)
+    s.forward(**cut)
+    s.backward(**cut)
+    some = [0, 1, 7, 8, 500, 993, 999, 1000]
+    x, gate, dy, h = (f64(t[:, some]) for t in (s.x, s.gate, s.dy, s.h))
+    h0, dlast = f64(s.h0[:, some]), f64(s.dlast[:, some])
+    want, off, last, off_last = ref.gated_scan(x, gate, bounds, h0)
+    assert_near(s.h[:, some], want, off, dtype, "h")
+    assert_near(s.last[:, some], last, off_last, F32, "last")
+    dx, off_x, dgate, off_g, dh0, off_0 = ref.gated_scan_grad(dy, x, gate, h, bounds, h0, dlast)
+    assert_near(s.dx[:, some], dx, off_x, dtype, "dx")
+    assert_near(s.dgate[:, some], dgate, off_g, dtype, "dgate")
+    assert_near(s.dh0[:, some], dh0, off_0, F32, "dh0")
+    for m, flat in ((s.h, s.h_flat), (s.dx, s.dx_flat), (s.dgate, s.dgate_flat)):
+        assert bool(torch.isfinite(m).all()) and (m == 5.0).float().mean() < 1e-2      # every entry was written
+        m[:] = 5.0
+        assert bool((flat == 5.0).all())
