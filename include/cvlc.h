@@ -486,8 +486,9 @@ int cvlc_linear_xent(uint32_t n, uint32_t vocab, uint32_t dim, const void* d_hid
  *   d_workspace  device, 256-byte aligned, ws_bytes >=
  *              cvlc_linear_xent_grad_workspace_bytes(n, vocab, dim, type, dtable_type)
  *              (without d_dtable: of the table's type); holds no status word
- * G is rounded to the type of 16-bit results; for fp32 results to 2^-18 of itself
- * beside bfloat16 matrices, else to 2^-23.  Beside others than bfloat16 it loses
+ * G is rounded: for dhidden of 16 bits to their type, but for the label's entry;
+ * else to 2^-17 of itself beside bfloat16 matrices, to 2^-23 beside others and for
+ * an fp32 dtable of fewer than 4096 rows.  Beside others than bfloat16 it loses
  * what is below 2^-38 of scale times the largest weight, or below 2^-150. */
 size_t cvlc_linear_xent_grad_workspace_bytes(uint32_t n, uint32_t vocab, uint32_t dim, uint32_t type, uint32_t dtable_type);
 int cvlc_linear_xent_grad(uint32_t n, uint32_t vocab, uint32_t dim, const void* d_hidden, uint64_t hidden_stride,

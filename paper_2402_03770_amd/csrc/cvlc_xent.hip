@@ -9,8 +9,13 @@
 //   - fp32 as two planes of fp16 (11 + 11 bits) of the matrix times a power of two that brings its largest element to about 2^14;
 //     three of the four products of planes are added.  What is left out is below 2^-22 of a term, and an element is held to
 //     2^-23 of itself or 2^-39 of the largest.  An fp32 matrix instruction has a sixteenth of the rate.
-//   - G, in one plane where the result is of 16 bits (its rounding of 2^-9 or 2^-12 of a term is what the result's own is), in
-//     two for fp32 results (2^-18 in bfloat16, 2^-23 in fp16).
+//   - G for dh of 16 bits in one plane of its type, whose rounding, but for the label's entry, is what the result's own is; what it
+//     leaves of the label's entry is added (join_kernel).
+//   - G for dT in two planes (2^-17 of an entry in bfloat16, 2^-23 in fp16).  dT adds up labels' entries of about -1 and others'
+//     shares of them, which may nearly cancel: in one plane, half the product, values of 263 x 128 x 99 137 bf16 were 12 % off that
+//     now are rounded.  Three for fp32 dT of bfloat16 matrices of fewer than kManyTokens rows: 2-norms of the error of 1, 24, 600,
+//     2000 and 4096 tokens are 3.4e-6, 1.9e-6, 1.4e-6, 1.2e-6 and 1.1e-6 with two, where sums in fp32 alone have 4e-8, 2e-7, 4e-7,
+//     8e-7 and 1.1e-6.
 // G is scaled so that the largest weight becomes 2^13, by 2^126 at most: then neither tiny weights nor fp16 lose its small
 // entries, and the label's entry, softmax - 1, is next to a value that every type has.
 //
@@ -40,12 +45,12 @@ constexpr float kMostLift = 0x1p126f;   // ... where they do not take more than 
 uint64_t pad_to(uint64_t x, uint64_t to) { return (x + to - 1) / to * to; }
 
 // ------------------------------------------------------------------------------ planes
-// x as a sum of P values of a 16-bit type.  Three cut bits off, which leaves the rest exact; one or two round.
-template <class H, uint32_t P>
+// x as a sum of P values of a 16-bit type, each rounded or (CUT) with the bits behind it cut off; the rest is exact both ways.
+template <class H, uint32_t P, bool CUT = false>
 __device__ __forceinline__ void split(float x, Half (&out)[P]) {
 #pragma unroll
   for (uint32_t p = 0; p < P; ++p) {
-    const H h = P == 3 ? __builtin_bit_cast(H, (Half)(__float_as_uint(x) >> 16)) : (H)x;
+    const H h = CUT ? __builtin_bit_cast(H, (Half)(__float_as_uint(x) >> 16)) : (H)x;
     out[p] = __builtin_bit_cast(Half, h);
     x -= (float)h;
   }
@@ -174,7 +179,7 @@ __global__ __launch_bounds__(kPackBlock) void pack_kernel(PackArgs first, PackAr
     if (row < a.from.rows && !(a.masked && !who.live(row))) load_row<8>(static_cast<const T*>(a.from.p) + row * a.from.stride, c, a.cols, 0.0f, x);
     Half h[8][P];
 #pragma unroll
-    for (uint32_t i = 0; i < 8; ++i) split<H, P>(P == 2 ? x[i] * up : x[i], h[i]);
+    for (uint32_t i = 0; i < 8; ++i) split<H, P, P == 3>(P == 2 ? x[i] * up : x[i], h[i]);
 #pragma unroll
     for (uint32_t p = 0; p < P; ++p) {
       Quad q;
@@ -1041,6 +1046,7 @@ constexpr uint32_t kSlicesMost = 64;         // ... and slices, at most ...
 constexpr uint64_t kSumsMost = 64ull << 20;  // ... and bytes of dT's slices; of which there is one where it has more small tiles than
 constexpr uint64_t kTilesFew = kCus / 2;     // this: 2048 x 768 x 32 000 fp32 takes 1190 us so, 1310 with slices of a last piece's dT
 constexpr uint64_t kLaunchCost = 30000;      // a launch's own time, about 10 us
+constexpr uint32_t kManyTokens = 4096;       // from which on sums in fp32 are further off than two planes of bfloat16
 
 // Into how many slices K of a product is cut, and what it costs then.  A slice's results are written and read again, 8 bytes
 // a value at 5 TB/s, and added up in turn.
@@ -1064,17 +1070,24 @@ Slices table_slices(uint64_t rows, uint64_t dim, uint64_t depth, uint64_t tokens
   const bool few = tiles(dim, rows, Small::TM, Small::TN) <= kTilesFew;
   return slices_for(dim, rows, tokens, products, few ? kSumsMost / (rows * depth * 4) : 1);
 }
-Sizes sizes_for(uint32_t n, uint32_t vocab, uint32_t dim, uint32_t type, uint32_t dtable_type, bool grad) {
+// G's planes; dtable: whether it is asked for.
+uint32_t planes_of_g(uint32_t n, uint32_t type, uint32_t dtable_type, bool dtable) {
+  if (type == CVLC_F32) return 2;
+  if (!dtable) return 1;
+  return type == CVLC_BF16 && dtable_type == CVLC_F32 && n < kManyTokens ? 3 : 2;
+}
+// g_planes: 0 for the loss.
+Sizes sizes_for(uint32_t n, uint32_t vocab, uint32_t dim, uint32_t type, uint32_t g_planes) {
   Sizes z{};
   z.depth = pad_to(dim, kDepth);
   z.tokens = pad_to(n, kDepth);
   z.planes = type == CVLC_F32 ? 2 : 1;
-  z.g_planes = dtable_type == CVLC_F32 ? 2 : 1;
+  z.g_planes = g_planes;
   z.slices = 1;
-  const uint64_t each = z.depth * z.planes * 2 + (grad ? z.tokens * z.g_planes * 2 : 0);
+  const uint64_t each = z.depth * z.planes * 2 + z.tokens * z.g_planes * 2;
   const uint64_t whole = pad_to(vocab, kPadTo) / kPadTo, most = std::min(whole, std::max<uint64_t>(1, kBudget / each / kPadTo));
   z.piece = most * kPadTo;
-  if (!grad) return z;
+  if (!g_planes) return z;
   // A launch lasts as long as its fullest CU: of the pieces' sizes the one whose launches take least together.
   const uint64_t of_z = z.planes == 1 ? 1 : 3, of_g = z.planes == 1 ? z.g_planes : 3;
   auto of_piece = [&](uint64_t t, uint32_t* slices) {
@@ -1272,11 +1285,11 @@ void join(const JoinArgs& a, TO* out, hipStream_t stream) {
   hipLaunchKernelGGL((join_kernel<T, TO>), dim3(std::min(a.rows, std::max(1u, 8192u / blocks)) * blocks), dim3(256), 0, stream, a, out);
 }
 
-template <class T, class TO>
+template <class T, class TO, uint32_t PG>
 void grad_of(const Call& c, const Sizes& z, const GradParts& parts, const float2* stats, T* dhidden, uint64_t dhidden_stride, TO* dtable,
              uint64_t dtable_stride, bool accumulate, uint32_t* status, hipStream_t stream) {
   using H = typename Kind<T>::H;
-  constexpr uint32_t P = Kind<T>::P, PG = sizeof(TO) == 4 ? 2 : 1;
+  constexpr uint32_t P = Kind<T>::P;
   const bool table_goes = as_it_is(c.table, c.table_stride, c.dim, c.type), few = few_tokens(c);
   find_factors(c, z, parts, status, stream);
   PackArgs hidden{c.hidden_matrix(), c.dim, (uint32_t)z.tokens, parts.hidden, z.depth, z.tokens * z.depth, parts.factors->up, 1};
@@ -1365,7 +1378,7 @@ extern "C" {
 size_t cvlc_linear_xent_workspace_bytes(uint32_t n, uint32_t vocab, uint32_t dim, uint32_t type) {
   using namespace cvlc;
   if (!n || !vocab || !dim) return 256;
-  return (size_t)LossParts(Room{}, sizes_for(n, vocab, dim, type, type, false), n, vocab).bytes;
+  return (size_t)LossParts(Room{}, sizes_for(n, vocab, dim, type, 0), n, vocab).bytes;
 }
 
 int cvlc_linear_xent(uint32_t n, uint32_t vocab, uint32_t dim, const void* d_hidden, uint64_t hidden_stride, const void* d_table,
@@ -1378,7 +1391,7 @@ int cvlc_linear_xent(uint32_t n, uint32_t vocab, uint32_t dim, const void* d_hid
   if (n && !d_loss && !d_stats) return CVLC_ERR_ARG;
   if (ws_bytes < cvlc_linear_xent_workspace_bytes(n, vocab, dim, type)) return CVLC_ERR_CAPACITY;
   if (n == 0) return CVLC_OK;
-  const Sizes z = sizes_for(n, vocab, dim, type, type, false);
+  const Sizes z = sizes_for(n, vocab, dim, type, 0);
   const LossParts room(Room{static_cast<uint8_t*>(d_workspace), 0}, z, n, vocab);
   by_type(type, [&](auto t) {
     loss_of<decltype(t)>(c, z, room, d_loss, reinterpret_cast<float2*>(d_stats), d_status, static_cast<hipStream_t>(hip_stream));
@@ -1389,7 +1402,9 @@ int cvlc_linear_xent(uint32_t n, uint32_t vocab, uint32_t dim, const void* d_hid
 size_t cvlc_linear_xent_grad_workspace_bytes(uint32_t n, uint32_t vocab, uint32_t dim, uint32_t type, uint32_t dtable_type) {
   using namespace cvlc;
   if (!n || !vocab || !dim) return 256;
-  return (size_t)GradParts(Room{}, sizes_for(n, vocab, dim, type, dtable_type, true), n, vocab).bytes;
+  uint64_t most = 0;
+  for (bool dtable : {false, true}) most = std::max(most, GradParts(Room{}, sizes_for(n, vocab, dim, type, planes_of_g(n, type, dtable_type, dtable)), n, vocab).bytes);
+  return (size_t)most;
 }
 
 int cvlc_linear_xent_grad(uint32_t n, uint32_t vocab, uint32_t dim, const void* d_hidden, uint64_t hidden_stride, const void* d_table,
@@ -1417,19 +1432,30 @@ int cvlc_linear_xent_grad(uint32_t n, uint32_t vocab, uint32_t dim, const void* 
     });
     return hip_check(hipGetLastError());
   }
-  const Sizes z = sizes_for(n, vocab, dim, type, out_type, true);
+  const Sizes z = sizes_for(n, vocab, dim, type, planes_of_g(n, type, out_type, d_dtable));
   const GradParts room(Room{static_cast<uint8_t*>(d_workspace), 0}, z, n, vocab);
   by_type(type, [&](auto t) {
     using T = decltype(t);
-    auto go = [&](auto to) {
+    auto go = [&](auto to, auto planes) {
       using TO = decltype(to);
-      grad_of<T, TO>(c, z, room, reinterpret_cast<const float2*>(d_stats), static_cast<T*>(d_dhidden), dhidden_stride,
-                     static_cast<TO*>(d_dtable), dtable_stride, accumulate, d_status, stream);
+      grad_of<T, TO, decltype(planes)::value>(c, z, room, reinterpret_cast<const float2*>(d_stats), static_cast<T*>(d_dhidden), dhidden_stride,
+                                              static_cast<TO*>(d_dtable), dtable_stride, accumulate, d_status, stream);
     };
-    if (out_type == type)
-      go(T{});
-    else
-      go(0.0f);
+    using One = std::integral_constant<uint32_t, 1>;
+    using Two = std::integral_constant<uint32_t, 2>;
+    using Three = std::integral_constant<uint32_t, 3>;
+    if constexpr (sizeof(T) == 4) {
+      go(T{}, Two{});
+    } else {
+      if (!d_dtable)
+        go(T{}, One{});
+      else if (out_type == type)
+        go(T{}, Two{});
+      else if (z.g_planes == 2)
+        go(0.0f, Two{});
+      else if constexpr (std::is_same_v<T, bf16_t>)
+        go(0.0f, Three{});
+    }
   });
   return hip_check(hipGetLastError());
 }

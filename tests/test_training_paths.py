@@ -286,6 +286,47 @@ def test_linear_xent_of_very_many_tokens(dtype, dtable, n, dim, vocab, extra):
     x.check()
 
 
+PLANES = {("bf16", "bf16"): 2.0 ** -17, ("bf16", "f32"): 2.0 ** -17, ("f16", "f16"): 2.0 ** -23, ("f16", "f32"): 2.0 ** -23}
+
+
+@gpu
+@pytest.mark.parametrize("dtype,dtable", [(BF16, BF16), (BF16, F32), (F16, F16), (F16, F32)])
+@pytest.mark.parametrize("n,dim,vocab", [(18, 24, 57), (40, 24, 20_000), (263, 16, 9000), (4100, 16, 30)])
+@pytest.mark.parametrize("alone", [False, True])
+def test_linear_xent_dtable_of_entries_that_cancel(dtype, dtable, n, dim, vocab, alone):
+    """A few words are most of the labels, and the hidden rows know them: a row of dtable is the difference of sums of many times
+    its size.  Two planes round an entry of G by half a step of half a step of 16 bits."""
+    x = Xent(n, dim, vocab, dtype, dtable, padding=0.0, weights=False)
+    x.labels %= 3
+    x.hidden.copy_((x.hidden.float() * 0.5 + 2.0 * x.table[x.labels].float()).to(dtype))
+    x.forward()
+    x.backward(dhidden=not alone)
+    _, _, _, _, G, off_G, h, t = ref.linear_xent(f64(x.hidden), f64(x.table), x.labels.cpu().numpy())
+    name = {F32: "f32", BF16: "bf16", F16: "f16"}
+    _, _, want, off = ref.linear_xent_grad(G, off_G, h, t, 0.0, PLANES[name[dtype], name[dtable]])
+    assert_near(x.dtable, want, off, dtable, "dtable")
+
+
+@gpu
+@pytest.mark.parametrize("n", [1, 2])
+@pytest.mark.parametrize("vocab", [300, 7777, 20_001])
+def test_linear_xent_dtable_in_fp32_of_few_bfloat16_rows(n, vocab):
+    """Equal logits: an entry of G is 1 / vocab, whose bits two planes of bfloat16 do not hold, off by the division's rounding, the
+    label's subtraction and the planes' 2^-26; a sum of 3 n products adds a rounding for each, and its scale one."""
+    x = Xent(n, 40, vocab, BF16, F32, padding=0.0, weights=False)
+    x.table.zero_()
+    x.forward()
+    x.backward(dhidden=False)
+    G = np.full((n, vocab), 1.0 / vocab)
+    G[np.arange(n), x.labels.cpu().numpy()] -= 1.0
+    h = f64(x.hidden)
+    tol = (8 + 3 * n) * ref.U * (np.abs(G).T @ np.abs(h))
+    assert_near(x.dtable, G.T @ h, tol, F32, "dtable")
+    two = torch.tensor(8192.0 / vocab, dtype=torch.float32)
+    rest = two - two.bfloat16().float()
+    assert abs((rest - rest.bfloat16().float()).item()) > 15 * ref.U * two.item()      # what two planes would have left
+
+
 # ----------------------------------------------------------------------------- more than the caches hold
 @gpu
 @pytest.mark.parametrize("bits,grad,copy,by_chance,n", [(32, F32, None, False, 5_500_001), (32, BF16, F16, False, 6_500_003), (8, F32, BF16, True, 9_500_001),
