@@ -328,10 +328,11 @@ int cvlc_device_status(const void* d_workspace, void* hip_stream, uint32_t* stat
  * Matrices are rows of elements of one type, `stride` elements from one row to
  * the next (at least the row's length); they need no more alignment than their
  * elements.  Everything is computed in 32 bits and rounded to the output's type
- * once, to nearest.  Sums have a fixed order: the same call on the same device
- * gives the same bits.  n = 0 is allowed everywhere (its matrices may be NULL).
- * Buffers that a call writes must not overlap others of the call, except where
- * it says so. */
+ * once, to nearest, but for the products of cvlc_linear_xent and its gradients,
+ * which say what they are rounded to, and averages in 8 bits.  Sums have a fixed
+ * order: the same call on the same device gives the same bits.  n = 0 is allowed
+ * everywhere (its matrices may be NULL).  Buffers that a call writes must not
+ * overlap others of the call, except where it says so. */
 #define CVLC_F32 0u
 #define CVLC_BF16 1u
 #define CVLC_F16 2u

@@ -20,7 +20,8 @@
 // entries, and the label's entry, softmax - 1, is next to a value that every type has.
 //
 // The loss's product ends in every tile's (max, sum of exponentials) per row, joined in order by a second launch.  The
-// gradients go over the vocabulary in pieces of a few thousand tokens whose G fits the last-level cache.
+// gradients go over the vocabulary in pieces, G's and a copied table's part of which take kBudget at most: a workspace that does not
+// grow with the vocabulary, and much of it still in the last-level cache (256 MB) when it is read.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -1040,7 +1041,9 @@ struct Sizes {
   uint64_t depth, tokens, piece;      // dim and n in whole tiles of K; tokens of the vocabulary at a time
   uint32_t planes, g_planes, slices;
 };
-constexpr uint64_t kBudget = 320ull << 20;   // bytes of a piece's G and table, about; less would end dh's sums too often
+// Bytes of a piece's G and table, about.  More than the last-level cache holds, since fewer tokens of the vocabulary at a time end
+// dh's sums, which every piece reads and writes, too often.
+constexpr uint64_t kBudget = 320ull << 20;
 constexpr uint64_t kSliceMin = 128;          // K that a product's slice has, at least ...
 constexpr uint32_t kSlicesMost = 64;         // ... and slices, at most ...
 constexpr uint64_t kSumsMost = 64ull << 20;  // ... and bytes of dT's slices; of which there is one where it has more small tiles than
